@@ -51,7 +51,8 @@ typedef enum {
     BT_ERR_WORKSPACE = 4, /* workspace smaller than bt_workspace_bytes(n, dtype) */
     BT_ERR_HIP = 5,       /* the HIP runtime refused the launch */
     BT_ERR_SIZE = 6,      /* n is beyond BT_MAX_ELEMENTS, or a size the call does not take */
-    BT_ERR_UNSUPPORTED = 7 /* the call exists only in another build of the library */
+    BT_ERR_UNSUPPORTED = 7, /* the call exists only in another build of the library */
+    BT_ERR_ARGUMENT = 8   /* a number or a combination of arguments that the call does not take */
 } bt_status;
 
 /* Largest number of tensors in one batched call. */
@@ -379,6 +380,129 @@ bt_status bt_decompress_batch_indexed(const bt_decompress_item *items, size_t co
  * completed on it since it was initialised.  d_status: two uint32 of device memory, valid
  * once `stream` has reached this call.  Errors: BT_ERR_NULL, BT_ERR_ALIGN, BT_ERR_HIP. */
 bt_status bt_workspace_status(const void *d_workspace, uint32_t *d_status, bt_stream stream);
+
+/* ---- the operators of a feed-forward sublayer -----------------------------------
+ *
+ * What stands around the activations that the codec keeps, in a step that trains such a sublayer or in a call that
+ * answers with it: the gated projections whose output is the activation, the norms, gate and residual sum between two
+ * sublayers, and the clipping of the step's gradients.  BT_F32, BT_F16 and BT_BF16.  All sums, statistics and
+ * activations are computed in 32 bits or more and rounded once, to the tensors' type, where they are stored.
+ *
+ * Tensors are row-major and contiguous, and are aligned to their elements; those that are aligned to 16 bytes and whose
+ * rows are whole 16-byte vectors go faster.  A workspace is scratch memory of the call: 128-byte aligned, of the size that the
+ * call's size function gives, in any state, free again once the stream has passed the call; two calls that can be in
+ * flight at the same time must not share one.  It may be NULL where that size is 0.  Results do not depend on
+ * what else runs: equal inputs give equal bits. */
+
+typedef enum {
+    BT_ACT_RELU = 0,     /* act(g) = g where g > 0 (or g is a NaN), else 0 */
+    BT_ACT_SILU = 1,     /* act(g) = g / (1 + exp(-g)) */
+    BT_ACT_GELU_TANH = 2 /* act(g) = g / 2 * (1 + tanh(sqrt(2 / pi) * (g + 0.044715 g^3))) */
+} bt_activation;
+
+/* Largest numbers of rows and of features that these calls accept. */
+#define BT_MAX_ROWS (((uint64_t)1 << 31) - 1)
+#define BT_MAX_FEATURES (((uint64_t)1 << 24))
+/* Largest number of columns of the residual norms. */
+#define BT_MAX_NORM_COLS 16384
+
+/* Bytes of workspace for bt_gated_forward (backward == 0) or bt_gated_backward (else).  0 for an unknown dtype or sizes the calls refuse. */
+size_t bt_gated_workspace_bytes(uint64_t rows, uint64_t d, uint64_t f, bt_dtype dtype, int backward);
+
+/* The gated projections: h = act(x w_gate^T) * (x w_up^T), in one kernel.
+ *   d_x               [rows, d]
+ *   d_w_gate, d_w_up  [f, d] each
+ *   d_h               [rows, f]
+ *   d_gate, d_up      [rows, f] each, or NULL both: what bt_gated_backward needs of this pass, rounded to the
+ *                     tensors' type: the pre-activations x w_gate^T and x w_up^T.  With BT_ACT_RELU act(x w_gate^T) and, where
+ *                     that is not 0, x w_up^T, else +0: then h, gate and up are all +0 wherever a gate is closed and
+ *                     compress as one.
+ * With BT_ACT_RELU h is +0 where the gate is closed, whatever the other factor is there (a select, never a multiply).
+ * rows == 0 or f == 0 does nothing; with d == 0 the products are 0.  No output may overlap an input or another output.
+ * Errors: BT_ERR_NULL, BT_ERR_DTYPE (BT_F64 too), BT_ERR_ALIGN, BT_ERR_SIZE, BT_ERR_WORKSPACE, BT_ERR_HIP, BT_ERR_ARGUMENT
+ * (unknown activation, or only one of d_gate and d_up). */
+bt_status bt_gated_forward(const void *d_x, const void *d_w_gate, const void *d_w_up,
+                           uint64_t rows, uint64_t d, uint64_t f, bt_dtype dtype, bt_activation activation,
+                           void *d_h, void *d_gate, void *d_up,
+                           void *d_workspace, size_t workspace_bytes, bt_stream stream);
+
+/* Its backward pass.  With g and u the two products, dg = grad_h * u * act'(g) and du = grad_h * act(g) (selects where a ReLU's gate
+ * is closed), rounded to the tensors' type as the factors of the products
+ *   grad_x = dg w_gate + du w_up      grad_w_gate = dg^T x      grad_w_up = du^T x
+ *   d_gate, d_up                  as bt_gated_forward left them, for the same activation
+ *   d_grad_x                      [rows, d], or NULL: not wanted (d_w_gate and d_w_up are not read then and may be NULL)
+ *   d_grad_w_gate, d_grad_w_up    [f, d] each, or NULL both: not wanted (d_x is not read then and may be NULL)
+ * Gradients are written, not added to.  rows == 0 writes zeros to the weights' gradients, f == 0 to grad_x.
+ * Errors as for bt_gated_forward; BT_ERR_ARGUMENT also for only one of the weights' gradients. */
+bt_status bt_gated_backward(const void *d_grad_h, const void *d_x, const void *d_w_gate, const void *d_w_up,
+                            const void *d_gate, const void *d_up,
+                            uint64_t rows, uint64_t d, uint64_t f, bt_dtype dtype, bt_activation activation,
+                            void *d_grad_x, void *d_grad_w_gate, void *d_grad_w_up,
+                            void *d_workspace, size_t workspace_bytes, bt_stream stream);
+
+/* What stands between two blocks, in one pass over the rows:
+ *   out = residual_scale * x + scale * gate * norm(block) * post_weight       y = norm(out) * pre_weight
+ *   norm(t) = t / sqrt(mean(t^2) + eps) over a row of `cols`
+ *   d_x            [rows, cols], the residual stream
+ *   d_block        [rows, cols], the output of the block before; NULL: there is none, out is x itself and is not written
+ *                  (d_out, d_post_weight and d_gate must be NULL then, and the two scales are not used)
+ *   d_post_weight  [cols], or NULL: block goes in as it is, without its norm
+ *   d_gate         [gate_rows, cols], or NULL: 1.  gate_rows divides rows: row r takes gate row r / (rows / gate_rows), so 1 is one
+ *                  gate for all rows, the number of sequences one for each of them, and rows one for each row
+ *   d_pre_weight   [cols], or NULL: y is not wanted (d_y must be NULL then)
+ *   d_out, d_y     [rows, cols]; y is computed from out before out is rounded.  d_out may be d_x or d_block itself; else no overlap
+ *   d_stats        NULL, or 2 * rows floats for bt_residual_norm_backward: 1 / sqrt(...) of block's rows (1 without
+ *                  post_weight), then of out's
+ * rows == 0 or cols == 0 does nothing.  Errors: BT_ERR_NULL, BT_ERR_DTYPE (BT_F64 too), BT_ERR_ALIGN, BT_ERR_SIZE, BT_ERR_HIP, BT_ERR_ARGUMENT
+ * (a combination that is excluded above, gate_rows that does not divide rows, eps negative or not finite, a scale that is not finite). */
+bt_status bt_residual_norm_forward(const void *d_x, const void *d_block, const void *d_post_weight, const void *d_gate,
+                                   const void *d_pre_weight, uint64_t rows, uint64_t cols, uint64_t gate_rows, bt_dtype dtype,
+                                   double eps, double scale, double residual_scale,
+                                   void *d_out, void *d_y, float *d_stats, bt_stream stream);
+
+/* Bytes of workspace for bt_residual_norm_backward; gate_rows 0 if there is no gate.  0 for an unknown dtype or sizes the call refuses. */
+size_t bt_residual_norm_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t gate_rows, bt_dtype dtype);
+
+/* The backward pass: the gradients of x, block, post_weight, gate and pre_weight from those of out and y.
+ *   d_grad_out          [rows, cols], or NULL: 0
+ *   d_grad_y            [rows, cols], or NULL: 0 (d_pre_weight and d_grad_pre_weight must be NULL then)
+ *   d_out               out as the forward pass left it (x, if there was no block)
+ *   d_block ... d_pre_weight, gate_rows, scale, residual_scale, d_stats    as in the forward pass
+ *   d_grad_x            [rows, cols], or NULL: not wanted
+ *   d_grad_block        [rows, cols]; d_grad_post_weight, d_grad_pre_weight [cols]; d_grad_gate [gate_rows, cols]: each NULL if not
+ *                       wanted, and NULL if its tensor is
+ * Gradients are written, not added to; d_grad_x may be d_grad_out itself, d_grad_block may be d_block or d_grad_y itself; else no
+ * overlap.  A gradient that several rows share is summed in 32 bits, in an order that the sizes alone decide.
+ * rows == 0 writes zeros to the weights' gradients.  Errors as for the forward pass, and BT_ERR_WORKSPACE. */
+bt_status bt_residual_norm_backward(const void *d_grad_out, const void *d_grad_y, const void *d_out, const void *d_block,
+                                    const void *d_post_weight, const void *d_gate, const void *d_pre_weight, const float *d_stats,
+                                    uint64_t rows, uint64_t cols, uint64_t gate_rows, bt_dtype dtype, double scale, double residual_scale,
+                                    void *d_grad_x, void *d_grad_block, void *d_grad_post_weight, void *d_grad_gate, void *d_grad_pre_weight,
+                                    void *d_workspace, size_t workspace_bytes, bt_stream stream);
+
+/* A gradient among others (host memory, read before the call returns). */
+typedef struct {
+    const void *d_in;   /* n elements (may be NULL when n == 0) */
+    void *d_out;        /* bt_clip_grads: n elements; d_in itself, or memory that overlaps no item's */
+    uint64_t n;
+    bt_dtype dtype;     /* BT_F32, BT_F16 or BT_BF16, of each item its own */
+} bt_clip_item;
+
+/* Bytes of workspace for bt_grad_norm and bt_clip_grads on `count` items, whatever their sizes. */
+size_t bt_clip_workspace_bytes(size_t count);
+
+/* *d_norm = sqrt(sum of the squares of all elements of all items), the sum in 64 bits: it neither overflows nor depends on the order.
+ * (An infinity or a NaN among them makes it one.)  count == 0 writes 0.
+ * Errors: BT_ERR_NULL, BT_ERR_DTYPE, BT_ERR_ALIGN, BT_ERR_SIZE (n beyond BT_MAX_ELEMENTS), BT_ERR_WORKSPACE, BT_ERR_HIP. */
+bt_status bt_grad_norm(const bt_clip_item *items, size_t count, float *d_norm,
+                       void *d_workspace, size_t workspace_bytes, bt_stream stream);
+
+/* The same, and every gradient scaled so that their norm is at most max_norm: d_out = d_in * min(1, max_norm / (norm + eps)), the
+ * product in 32 bits.  Nothing waits for the host: the factor stays on the device.  A norm of infinity makes the factor 0 and a NaN makes
+ * it a NaN, as the formula has it; the caller sees either in *d_norm.  max_norm >= 0 (infinity: no clipping), eps >= 0.
+ * Errors: as bt_grad_norm, and BT_ERR_ARGUMENT. */
+bt_status bt_clip_grads(const bt_clip_item *items, size_t count, double max_norm, double eps, float *d_norm,
+                        void *d_workspace, size_t workspace_bytes, bt_stream stream);
 
 #ifdef __cplusplus
 }

@@ -4,10 +4,13 @@ import os
 import re
 import subprocess
 import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "bittrain.hip")
+# the operators of a feed-forward sublayer, which both libraries hold beside their own source
+BLOCK_SRCS = [os.path.join(HERE, "csrc", name) for name in ("block.hip", "gated.hip")]
 LIB = os.path.join(HERE, "libbittrain.so")
 # measurement aids for bench.py: the same kernels with per-tile time stamps compiled in, plus a plain stream
 BENCH_SRC = os.path.join(HERE, "csrc", "bench_aids.hip")
@@ -17,7 +20,7 @@ CALL_SRC = os.path.join(HERE, "csrc", "call.cpp")
 CALL_LIB = os.path.join(HERE, "_call.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",
     # packed fp32 VALU forms are kept out of the device code: some of them have given wrong results
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
@@ -25,19 +28,33 @@ HIPCC_FLAGS = [
 
 def build(verbose=False, extra_flags=(), lib=LIB, src=SRC):
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + list(extra_flags) + ["-I", os.path.join(ROOT, "include"), src, "-o", lib]
-    if verbose:
-        print(" ".join(cmd))
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    # the host pass warns that it does not know the packed-fp32 feature: harmless
-    out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
-        print(out)
+    flags = HIPCC_FLAGS + list(extra_flags) + ["-I", os.path.join(ROOT, "include")]
+    with tempfile.TemporaryDirectory() as tmp:      # (the sources side by side: they take half a minute each)
+        objects = [os.path.join(tmp, os.path.basename(f) + ".o") for f in [src] + BLOCK_SRCS]
+        _run([[hipcc] + flags + ["-c", f, "-o", o] for f, o in zip([src] + BLOCK_SRCS, objects)], verbose)
+        _run([[hipcc] + flags + ["-shared"] + objects + ["-o", lib]], verbose)
     if lib == LIB:
         build_call(verbose)
     return lib
+
+
+def _run(commands, verbose):
+    """Commands side by side; raises if one fails, once all have ended."""
+    started = []
+    for cmd in commands:
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        started.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+    failed = ""
+    for p in started:
+        # the host pass warns that it does not know the packed-fp32 feature: harmless
+        out = "\n".join(l for l in p.communicate()[0].splitlines() if "packed-fp32-ops" not in l)
+        if p.returncode != 0:
+            failed += "hipcc failed:\n" + out
+        elif verbose and out.strip():
+            print(out)
+    if failed:
+        raise RuntimeError(failed)
 
 
 def build_bench_aids(verbose=False, extra_flags=()):

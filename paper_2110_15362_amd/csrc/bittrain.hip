@@ -2419,6 +2419,7 @@ const char *bt_status_str(bt_status status) {
         case BT_ERR_HIP: return "HIP launch failed";
         case BT_ERR_SIZE: return "element count too large";
         case BT_ERR_UNSUPPORTED: return "not available in this build of the library";
+        case BT_ERR_ARGUMENT: return "an argument the call does not take";
     }
     return "unknown status";
 }

@@ -1,0 +1,133 @@
+// What the kernels of a feed-forward sublayer share (block.hip, gated.hip): elements and their 16-byte vectors, reductions, launches.
+#ifndef BT_BLOCK_H
+#define BT_BLOCK_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <type_traits>
+
+#include "bittrain.h"
+
+namespace btb {
+
+constexpr int kWave = 64;
+constexpr int kVec = 16;                  // bytes of a vector load
+
+typedef uint32_t raw16 __attribute__((ext_vector_type(4)));      // a vector's bits
+typedef float float2v __attribute__((ext_vector_type(2)));
+
+struct bf16 { uint16_t bits; };
+struct f16 { _Float16 v; };
+
+// A vector at any address that its elements may have: the hardware takes such accesses, at full speed where they happen to be aligned.
+template <class T> struct __attribute__((packed, aligned(sizeof(T)))) Unaligned { raw16 v; };
+
+template <class T> constexpr int kPer = kVec / (int)sizeof(T);     // elements of a vector
+
+__device__ inline float widen(float x) { return x; }
+__device__ inline float widen(f16 x) { return (float)x.v; }
+__device__ inline float widen(bf16 x) { return __builtin_bit_cast(float, (uint32_t)x.bits << 16); }
+
+// The one rounding of a result, to nearest even.
+template <class T> __device__ inline T narrow(float x);
+template <> __device__ inline float narrow<float>(float x) { return x; }
+template <> __device__ inline f16 narrow<f16>(float x) { return f16{(_Float16)x}; }
+template <> __device__ inline bf16 narrow<bf16>(float x) { return bf16{__builtin_bit_cast(uint16_t, (__bf16)x)}; }
+
+// The elements of a vector as floats, and back.
+template <class T> __device__ inline void unpack(const raw16 v, float (&x)[kPer<T>]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(float, (uint32_t)v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (std::is_same_v<T, bf16>) {
+                x[2 * i] = __builtin_bit_cast(float, v[i] << 16);
+                x[2 * i + 1] = __builtin_bit_cast(float, v[i] & 0xffff0000u);
+            } else {
+                x[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)v[i]);
+                x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(v[i] >> 16));
+            }
+        }
+    }
+}
+
+template <class T> __device__ inline uint32_t pack2(const float a, const float b) {
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    if constexpr (std::is_same_v<T, bf16>) return __builtin_bit_cast(uint32_t, bf2{(__bf16)a, (__bf16)b});
+    else return __builtin_bit_cast(uint32_t, h2{(_Float16)a, (_Float16)b});
+}
+
+template <class T> __device__ inline raw16 pack(const float (&x)[kPer<T>]) {
+    raw16 v;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
+    }
+    return v;
+}
+
+// Elements [0, left) of the vector at p, zeros behind them.
+template <class T> __device__ inline raw16 load_vec(const T *p, const int64_t left) {
+    if (left >= kPer<T>) return reinterpret_cast<const Unaligned<T> *>(p)->v;
+    raw16 v = {0, 0, 0, 0};
+    if (left <= 0) return v;
+#pragma unroll
+    for (int i = 0; i < kPer<T>; ++i)
+        if (i < left) {
+            if constexpr (sizeof(T) == 4) v[i] = __builtin_bit_cast(uint32_t, p[i]);
+            else v[i / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, p[i]) << (16 * (i & 1));
+        }
+    return v;
+}
+
+template <class T> __device__ inline void store_vec(T *p, const int64_t left, const raw16 v) {
+    if (left >= kPer<T>) {
+        reinterpret_cast<Unaligned<T> *>(p)->v = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer<T>; ++i)
+        if (i < left) {
+            if constexpr (sizeof(T) == 4) p[i] = __builtin_bit_cast(float, (uint32_t)v[i]);
+            else p[i] = __builtin_bit_cast(T, (uint16_t)(v[i / 2] >> (16 * (i & 1))));
+        }
+}
+
+template <class T> static __global__ __launch_bounds__(256) void zero_kernel(T *p, const uint64_t n) {
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) p[i] = narrow<T>(0.0f);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------
+
+inline int width_of(const bt_dtype dt) { return dt == BT_F32 ? 4 : dt == BT_F16 || dt == BT_BF16 ? 2 : 0; }
+
+inline bool misaligned(const void *p, const size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+// hipLaunchKernel's status is this launch's own.
+template <class... P>
+bt_status launch(void (*kernel)(P...), const dim3 grid, const int block, hipStream_t hs, const std::common_type_t<P> &...args) {
+    void *where[] = {const_cast<void *>(static_cast<const void *>(&args))...};
+    if (hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3((unsigned)block), where, 0, hs) == hipSuccess) return BT_OK;
+    (void)hipGetLastError();
+    return BT_ERR_HIP;
+}
+
+template <class Go> bt_status with_type(const bt_dtype dt, Go go) {
+    if (dt == BT_F32) return go(float{});
+    if (dt == BT_F16) return go(f16{});
+    return go(bf16{});
+}
+
+template <class T> bt_status zeros(void *p, const uint64_t n, hipStream_t hs) {
+    const uint64_t blocks = (n + 255) / 256;
+    return n == 0 ? BT_OK : launch(zero_kernel<T>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), 256, hs, (T *)p, n);
+}
+
+}  // namespace btb
+#endif  // BT_BLOCK_H

@@ -1,5 +1,5 @@
 /*
- * paper_2110_15362_amd/_call.so: the calls of libbittrain on torch tensors, for bittrain.py.
+ * paper_2110_15362_amd/_call.so: the calls of libbittrain on torch tensors, for bittrain.py and block.py.
  *
  * What a small call costs is the host's work, not the GPU's: the three calls of a training step on one image's
  * layer (fp32, 200,704 elements) keep the GPU busy for 10 us, and checking the tensors and marshalling the arguments with
@@ -537,21 +537,316 @@ static PyObject *py_relu_gradient(PyObject *self, PyObject *const *args, Py_ssiz
     END_HANDLE_TH_ERRORS
 }
 
+/* ---- the operators of a feed-forward sublayer, for block.py ------------------------------------------- */
+
+static struct {
+    size_t (*gated_workspace_bytes)(uint64_t, uint64_t, uint64_t, bt_dtype, int);
+    bt_status (*gated_forward)(const void *, const void *, const void *, uint64_t, uint64_t, uint64_t, bt_dtype, bt_activation, void *, void *,
+                               void *, void *, size_t, bt_stream);
+    bt_status (*gated_backward)(const void *, const void *, const void *, const void *, const void *, const void *, uint64_t, uint64_t, uint64_t,
+                                bt_dtype, bt_activation, void *, void *, void *, void *, size_t, bt_stream);
+    size_t (*residual_norm_workspace_bytes)(uint64_t, uint64_t, uint64_t, bt_dtype);
+    bt_status (*residual_norm_forward)(const void *, const void *, const void *, const void *, const void *, uint64_t, uint64_t, uint64_t,
+                                       bt_dtype, double, double, double, void *, void *, float *, bt_stream);
+    bt_status (*residual_norm_backward)(const void *, const void *, const void *, const void *, const void *, const void *, const void *,
+                                        const float *, uint64_t, uint64_t, uint64_t, bt_dtype, double, double, void *, void *, void *, void *,
+                                        void *, void *, size_t, bt_stream);
+    size_t (*clip_workspace_bytes)(size_t);
+    bt_status (*grad_norm)(const bt_clip_item *, size_t, float *, void *, size_t, bt_stream);
+    bt_status (*clip_grads)(const bt_clip_item *, size_t, double, double, float *, void *, size_t, bt_stream);
+} block;
+
+static int expect_block(const Py_ssize_t got, const Py_ssize_t want) {
+    if (block.clip_grads == NULL) return fail(PyExc_RuntimeError, "the library is not loaded");
+    return got == want ? 0 : fail(PyExc_TypeError, "wrong number of arguments");
+}
+
+/* As `take`, of arguments that may be None: those stay without an address, and of no size. */
+static int take_some(tensor *a, PyObject *const *args, const char *const *names, const int count) {
+    PyObject *there[16];
+    tensor got[16];
+    const char *called[16];
+    int n = 0;
+    for (int i = 0; i < count; ++i)
+        if (args[i] != Py_None) {
+            there[n] = args[i];
+            called[n++] = names[i];
+        }
+    if (take(got, there, called, n) != 0) return -1;
+    n = 0;
+    for (int i = 0; i < count; ++i) {
+        if (args[i] != Py_None) a[i] = got[n++];
+        else a[i] = tensor{NULL, NULL, -1, 0, 0, {NULL}};
+    }
+    return 0;
+}
+
+static int refuse(const char *name, const char *what) {
+    PyErr_Format(PyExc_ValueError, "%s %s", name, what);
+    return -1;
+}
+
+/* The last dimension of a tensor, and the elements before it: [rows, last]. */
+static int matrix_of(const tensor *a, const char *name, uint64_t *rows, uint64_t *last) {
+    uint64_t dims = 0, n = 1;
+    if (THPVariable_Check(a->t)) {
+        const at::Tensor &t = THPVariable_Unpack(a->t);
+        dims = (uint64_t)t.dim();
+        if (dims != 0) *last = (uint64_t)t.size(-1);
+        for (uint64_t i = 0; i + 1 < dims; ++i) n *= (uint64_t)t.size((int64_t)i);
+    } else {
+        PyObject *const shape = PyObject_GetAttrString(a->t, "shape");
+        PyObject *const items = shape != NULL ? PySequence_Tuple(shape) : NULL;
+        Py_XDECREF(shape);
+        if (items == NULL) return -1;
+        dims = (uint64_t)PyTuple_GET_SIZE(items);
+        for (uint64_t i = 0; i < dims; ++i) {
+            const uint64_t v = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(items, (Py_ssize_t)i));
+            if (v == (uint64_t)-1 && PyErr_Occurred()) {
+                Py_DECREF(items);
+                return -1;
+            }
+            if (i + 1 == dims) *last = v;
+            else n *= v;
+        }
+        Py_DECREF(items);
+    }
+    if (dims == 0) return refuse(name, "must have a last dimension");
+    *rows = n;
+    return 0;
+}
+
+static int same_type(const tensor *a, const tensor *x, const char *name) {
+    if (a->t != NULL && a->dtype != x->dtype) {
+        PyErr_Format(PyExc_TypeError, "%s must have the dtype of the others", name);
+        return -1;
+    }
+    return 0;
+}
+
+/* All tensors that are there have x's type; `elements` of each as listed. */
+static int check_all(const tensor *a, const char *const *names, const int count, const tensor *x, const uint64_t *elements) {
+    for (int i = 0; i < count; ++i)
+        if (a[i].t != NULL && (same_type(&a[i], x, names[i]) != 0 || (a[i].numel != elements[i] && refuse(names[i], "does not have the shape that goes with the others") != 0)))
+            return -1;
+    return 0;
+}
+
+static int number(PyObject *o, double *v) {
+    *v = PyFloat_AsDouble(o);
+    return *v == -1.0 && PyErr_Occurred() ? -1 : 0;
+}
+
+/* 1: w_gate and w_up are [f, d] both */
+static int weights_of(const tensor *gate, const tensor *up, uint64_t *f, uint64_t *d) {
+    uint64_t f2, d2;
+    if (matrix_of(gate, "w_gate", f, d) != 0 || matrix_of(up, "w_up", &f2, &d2) != 0) return -1;
+    if (f2 != *f || d2 != *d) return refuse("w_up", "must have the shape of w_gate");
+    return 0;
+}
+
+/* The rows of x, whose last dimension is `last`. */
+static int rows_of(const tensor *x, const char *name, const uint64_t last, uint64_t *rows) {
+    uint64_t l = 0;
+    if (matrix_of(x, name, rows, &l) != 0) return -1;
+    return l == last ? 0 : refuse(name, "has another last dimension than goes with the others");
+}
+
+/* (x, w_gate, w_up, h, gate, up, workspace, activation, stream) */
+static PyObject *py_gated_forward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"x", "w_gate", "w_up", "h", "gate", "up", "workspace"};
+    tensor a[7];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    uint64_t rows, d, f;
+    if (expect_block(nargs, 9) != 0) return NULL;
+    for (int i = 0; i < 4; ++i)
+        if (args[i] == Py_None) return fail(PyExc_TypeError, "x, w_gate, w_up and h are needed"), nullptr;
+    if (take_some(a, args, names, 7) != 0 || weights_of(&a[1], &a[2], &f, &d) != 0 || rows_of(&a[0], "x", d, &rows) != 0) return NULL;
+    const uint64_t elements[] = {rows * d, f * d, f * d, rows * f, rows * f, rows * f};
+    if (check_all(a, names, 6, &a[0], elements) != 0 || code_of(&a[0], &code) != 0) return NULL;
+    const long activation = PyLong_AsLong(args[7]);
+    if ((activation == -1 && PyErr_Occurred()) || stream_of(args[8], &stream) != 0) return NULL;
+    CALL("bt_gated_forward", block.gated_forward(a[0].ptr, a[1].ptr, a[2].ptr, rows, d, f, code, (bt_activation)activation, a[3].ptr, a[4].ptr, a[5].ptr,
+                                                 a[6].ptr, a[6].numel * a[6].width, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* (grad_h, x, w_gate, w_up, gate, up, grad_x, grad_w_gate, grad_w_up, workspace, activation, stream) */
+static PyObject *py_gated_backward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"grad_h", "x", "w_gate", "w_up", "gate", "up", "grad_x", "grad_w_gate", "grad_w_up", "workspace"};
+    tensor a[10];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    uint64_t rows, d, f;
+    if (expect_block(nargs, 12) != 0) return NULL;
+    for (int i = 0; i < 6; ++i)
+        if (args[i] == Py_None) return fail(PyExc_TypeError, "grad_h, x, w_gate, w_up, gate and up are needed"), nullptr;
+    if (take_some(a, args, names, 10) != 0 || weights_of(&a[2], &a[3], &f, &d) != 0 || rows_of(&a[1], "x", d, &rows) != 0) return NULL;
+    const uint64_t elements[] = {rows * f, rows * d, f * d, f * d, rows * f, rows * f, rows * d, f * d, f * d};
+    if (check_all(a, names, 9, &a[1], elements) != 0 || code_of(&a[1], &code) != 0) return NULL;
+    const long activation = PyLong_AsLong(args[10]);
+    if ((activation == -1 && PyErr_Occurred()) || stream_of(args[11], &stream) != 0) return NULL;
+    CALL("bt_gated_backward", block.gated_backward(a[0].ptr, a[1].ptr, a[2].ptr, a[3].ptr, a[4].ptr, a[5].ptr, rows, d, f, code, (bt_activation)activation,
+                                                   a[6].ptr, a[7].ptr, a[8].ptr, a[9].ptr, a[9].numel * a[9].width, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* The gate rows of a gate that may not be there. */
+static int gate_rows_of(const tensor *gate, const uint64_t cols, const uint64_t rows, uint64_t *gate_rows) {
+    *gate_rows = 0;
+    if (gate->t == NULL) return 0;
+    if (rows_of(gate, "gate", cols, gate_rows) != 0) return -1;
+    if (rows != 0 && (*gate_rows == 0 || rows % *gate_rows != 0)) return refuse("gate", "must have a number of rows that divides those of x");
+    return 0;
+}
+
+static int check_stats(const tensor *stats, const uint64_t rows) {
+    if (stats->t != NULL && (stats->code != BT_F32 || stats->numel != 2 * rows)) return refuse("stats", "must hold two single-precision numbers for each row");
+    return 0;
+}
+
+/* dtypes of plain and other tensors are told apart by the code */
+static int code_and_stats(const tensor *x, const tensor *stats, const uint64_t rows, bt_dtype *code) {
+    return code_of(x, code) != 0 || check_stats(stats, rows) != 0 ? -1 : 0;
+}
+
+/* (x, block, post_weight, gate, pre_weight, out, y, stats, eps, scale, residual_scale, stream) */
+static PyObject *py_residual_norm_forward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"x", "block", "post_weight", "gate", "pre_weight", "out", "y", "stats"};
+    tensor a[8];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    uint64_t rows, cols = 0, gate_rows;
+    double eps, scale, residual_scale;
+    if (expect_block(nargs, 12) != 0) return NULL;
+    if (args[0] == Py_None) return fail(PyExc_TypeError, "x is needed"), nullptr;
+    if (take_some(a, args, names, 8) != 0 || matrix_of(&a[0], "x", &rows, &cols) != 0 || gate_rows_of(&a[3], cols, rows, &gate_rows) != 0) return NULL;
+    const uint64_t elements[] = {rows * cols, rows * cols, cols, gate_rows * cols, cols, rows * cols, rows * cols};
+    if (check_all(a, names, 7, &a[0], elements) != 0 || code_and_stats(&a[0], &a[7], rows, &code) != 0 || number(args[8], &eps) != 0 ||
+        number(args[9], &scale) != 0 || number(args[10], &residual_scale) != 0 || stream_of(args[11], &stream) != 0)
+        return NULL;
+    CALL("bt_residual_norm_forward", block.residual_norm_forward(a[0].ptr, a[1].ptr, a[2].ptr, a[3].ptr, a[4].ptr, rows, cols, gate_rows, code, eps, scale,
+                                                                 residual_scale, a[5].ptr, a[6].ptr, a[7].ptr, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* (grad_out, grad_y, out, block, post_weight, gate, pre_weight, stats, grad_x, grad_block, grad_post_weight, grad_gate, grad_pre_weight, workspace,
+ * scale, residual_scale, stream) */
+static PyObject *py_residual_norm_backward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"grad_out", "grad_y", "out", "block", "post_weight", "gate", "pre_weight", "stats", "grad_x", "grad_block",
+                                        "grad_post_weight", "grad_gate", "grad_pre_weight", "workspace"};
+    tensor a[14];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    uint64_t rows, cols = 0, gate_rows;
+    double scale, residual_scale;
+    if (expect_block(nargs, 17) != 0) return NULL;
+    if (args[2] == Py_None) return fail(PyExc_TypeError, "out is needed"), nullptr;
+    if (take_some(a, args, names, 14) != 0 || matrix_of(&a[2], "out", &rows, &cols) != 0 || gate_rows_of(&a[5], cols, rows, &gate_rows) != 0) return NULL;
+    const uint64_t cells = rows * cols;
+    const uint64_t before[] = {cells, cells, cells, cells, cols, gate_rows * cols, cols}, behind[] = {cells, cells, cols, gate_rows * cols, cols};
+    if (check_all(a, names, 7, &a[2], before) != 0 || check_all(a + 8, names + 8, 5, &a[2], behind) != 0 || code_and_stats(&a[2], &a[7], rows, &code) != 0 ||
+        number(args[14], &scale) != 0 || number(args[15], &residual_scale) != 0 || stream_of(args[16], &stream) != 0)
+        return NULL;
+    CALL("bt_residual_norm_backward", block.residual_norm_backward(a[0].ptr, a[1].ptr, a[2].ptr, a[3].ptr, a[4].ptr, a[5].ptr, a[6].ptr, a[7].ptr, rows, cols,
+                                                                   gate_rows, code, scale, residual_scale, a[8].ptr, a[9].ptr, a[10].ptr, a[11].ptr,
+                                                                   a[12].ptr, a[13].ptr, a[13].numel * a[13].width, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* The tensors of a list (or tuple) as clip items, and with `outs` those that they go to. */
+static int clip_items(PyObject *grads, PyObject *outs, std::vector<bt_clip_item> &items) {
+    static const char *const names[] = {"grads", "outs"};
+    if (!PyList_Check(grads) && !PyTuple_Check(grads)) return fail(PyExc_TypeError, "grads must be a list or a tuple of tensors");
+    if (outs != NULL && !PyList_Check(outs) && !PyTuple_Check(outs)) return fail(PyExc_TypeError, "outs must be a list or a tuple of tensors");
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(grads);
+    if (outs != NULL && PySequence_Fast_GET_SIZE(outs) != count) return fail(PyExc_ValueError, "outs: one for each gradient");
+    items.resize((size_t)count);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        if (i >= PySequence_Fast_GET_SIZE(grads) || (outs != NULL && i >= PySequence_Fast_GET_SIZE(outs))) return fail(PyExc_RuntimeError, "a list changed meanwhile");
+        PyObject *const pair[] = {PySequence_Fast_GET_ITEM(grads, i), outs != NULL ? PySequence_Fast_GET_ITEM(outs, i) : NULL};
+        tensor a[2];
+        bt_dtype code = BT_F32;
+        if (take(a, pair, names, outs != NULL ? 2 : 1) != 0) return -1;
+        if (outs != NULL && (a[1].dtype != a[0].dtype || a[1].numel != a[0].numel)) return fail(PyExc_TypeError, "an output must match its gradient");
+        if (code_of(&a[0], &code) != 0) return -1;
+        items[(size_t)i] = {a[0].ptr, outs != NULL ? a[1].ptr.p : NULL, a[0].numel, code};
+    }
+    return 0;
+}
+
+static int check_norm(const tensor *norm) {
+    return norm->code == BT_F32 && norm->numel >= 1 ? 0 : refuse("norm", "must be a single-precision number");
+}
+
+/* (grads, norm, workspace, stream) */
+static PyObject *py_grad_norm(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"norm", "workspace"};
+    tensor a[2];
+    bt_stream stream = NULL;
+    std::vector<bt_clip_item> items;
+    if (expect_block(nargs, 4) != 0 || clip_items(args[0], NULL, items) != 0 || take(a, args + 1, names, 2) != 0 || check_norm(&a[0]) != 0 ||
+        stream_of(args[3], &stream) != 0)
+        return NULL;
+    CALL("bt_grad_norm", block.grad_norm(items.data(), items.size(), a[0].ptr, a[1].ptr, a[1].numel * a[1].width, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* (grads, outs, norm, workspace, max_norm, eps, stream) */
+static PyObject *py_clip_grads(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"norm", "workspace"};
+    tensor a[2];
+    bt_stream stream = NULL;
+    double max_norm, eps;
+    std::vector<bt_clip_item> items;
+    if (expect_block(nargs, 7) != 0 || clip_items(args[0], args[1], items) != 0 || take(a, args + 2, names, 2) != 0 || check_norm(&a[0]) != 0 ||
+        number(args[4], &max_norm) != 0 || number(args[5], &eps) != 0 || stream_of(args[6], &stream) != 0)
+        return NULL;
+    CALL("bt_clip_grads", block.clip_grads(items.data(), items.size(), max_norm, eps, a[0].ptr, a[1].ptr, a[1].numel * a[1].width, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* The addresses of a tuple into the `count` pointers at `slots`, all or none. */
+static int take_addresses(PyObject *addresses, void **slots, const int count) {
+    std::vector<uint64_t> at((size_t)count);
+    if (PyTuple_GET_SIZE(addresses) != count) return fail(PyExc_TypeError, "one address per call");
+    for (int i = 0; i < count; ++i) {
+        at[(size_t)i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(addresses, i));
+        if (at[(size_t)i] == (uint64_t)-1 && PyErr_Occurred()) return -1;
+    }
+    for (int i = 0; i < count; ++i) slots[i] = (void *)(uintptr_t)at[(size_t)i];
+    return 0;
+}
+
+/* (addresses of the calls in the order of `block`) */
+static PyObject *py_bind_block(PyObject *self, PyObject *args) {
+    (void)self;
+    PyObject *addresses;
+    if (!PyArg_ParseTuple(args, "O!", &PyTuple_Type, &addresses)) return NULL;
+    if (take_addresses(addresses, (void **)(void *)&block, (int)(sizeof(block) / sizeof(void *))) != 0) return NULL;
+    Py_RETURN_NONE;
+}
+
 /* (addresses of the calls in the order of `lib`, the objects above in their order) */
 static PyObject *py_bind(PyObject *self, PyObject *args) {
     (void)self;
     PyObject *addresses, *o[4];
     int devices;
     if (!PyArg_ParseTuple(args, "O!O!OOOp", &PyTuple_Type, &addresses, &PyDict_Type, &o[0], &o[1], &o[2], &o[3], &devices)) return NULL;
-    void **const slots = (void **)(void *)&lib;
-    enum { kSlots = sizeof(lib) / sizeof(void *) };
-    uint64_t at[kSlots];
-    if (PyTuple_GET_SIZE(addresses) != kSlots) return fail(PyExc_TypeError, "one address per call"), nullptr;
-    for (int i = 0; i < kSlots; ++i) {
-        at[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(addresses, i));
-        if (at[i] == (uint64_t)-1 && PyErr_Occurred()) return NULL;
-    }
-    for (int i = 0; i < kSlots; ++i) slots[i] = (void *)(uintptr_t)at[i];
+    if (take_addresses(addresses, (void **)(void *)&lib, (int)(sizeof(lib) / sizeof(void *))) != 0) return NULL;
     PyObject **const keep[4] = {&dtypes, &dtype_code, &error_class, &stream_handle};
     for (int i = 0; i < 4; ++i) {
         Py_INCREF(o[i]);
@@ -566,7 +861,8 @@ static PyMethodDef methods[] = {
     FAST(compress), FAST(compress_static), FAST(compress_pruned), FAST(activation_compress), FAST(compress_indexed),
     FAST(decompress), FAST(decompress_indexed), FAST(relu_backward), FAST(mask_apply), FAST(relu_forward),
     FAST(pack), FAST(unpack), FAST(relu), FAST(relu_gradient),
-    {"bind", py_bind, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL}};
+    FAST(gated_forward), FAST(gated_backward), FAST(residual_norm_forward), FAST(residual_norm_backward), FAST(grad_norm), FAST(clip_grads),
+    {"bind", py_bind, METH_VARARGS, NULL}, {"bind_block", py_bind_block, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__call(void) {
