@@ -53,40 +53,53 @@ template <class T, Order O, int N> struct Tile {      // N rows or columns of th
     static constexpr int CHUNKS = (O == kAlong ? kKBytes : N * (int)sizeof(T)) / kVec;      // of a row
     static constexpr int BYTES = ROWS * CHUNKS * kVec;
 
+    // (Of the rows that one fragment has, those of a lane share the key.)
     __device__ static int place(const int row, const int chunk) {
         int key;
         if constexpr (O == kAlong) key = row & 7;
+        else if constexpr (sizeof(T) == 2 && CHUNKS == 8) key = 2 * (((row >> 1) & 1) | ((row >> 2) & 2));
         else if constexpr (sizeof(T) == 2) key = 2 * ((row & 3) | ((row >> 1) & 4));
         else key = 4 * ((row >> 2) & 3);
         return (row * CHUNKS + (chunk ^ key)) * kVec;
     }
+};
 
-    // The fragment of rows or columns [at, at + 16) and step `step` of the summed index.
-    __device__ static raw16 fragment(const char *tile, const int at, const int step) {
+// A wave's fragments of a tile: F times 16 rows or columns from `first` on.  Where a lane reads depends on the step, the fragment and the tile
+// by constants alone, but for one address a step (summed index along) or a fragment (across).
+template <class T, Order O, int N, int F> struct Reader {
+    typedef Tile<T, O, N> L;
+    static constexpr int ROW = L::CHUNKS * kVec;
+    uint32_t at[O == kAlong ? 2 : F];
+
+    __device__ void start(const int first) {
         const int lane = threadIdx.x % kWave, group = lane / 16, t = lane % 16;
         if constexpr (O == kAlong) {
-            return *(const raw16 *)(tile + place(at + t, step * 4 + group));
+#pragma unroll
+            for (int step = 0; step < 2; ++step) at[step] = L::place(first + t, step * 4 + group);
+        } else {
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                const int n = first + i * 16;
+                if constexpr (sizeof(T) == 2) at[i] = L::place(group * 8 + t / 4, (n + t % 4 * 4) / 8) + t % 2 * 8;
+                else at[i] = L::place(group * 4, (n + t) / 4) + t % 4 * 4;
+            }
+        }
+    }
+
+    __device__ raw16 read(const char *tile, const int i, const int step) const {
+        if constexpr (O == kAlong) {
+            return *(const raw16 *)(tile + at[step] + i * 16 * ROW);
         } else if constexpr (sizeof(T) == 2) {
             // 16 lanes read 4 summed indices by 16 columns, 4 columns a lane, and get one column each
-            raw16 v;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int k = step * 32 + group * 8 + half * 4 + t / 4, n = at + (t % 4) * 4;
-                const char *const from = tile + place(k, n / 8) + (n % 8) * 2;
-                const short4v got = __builtin_amdgcn_ds_read_tr16_b64_v4i16((BT_LDS short4v *)from);
-                typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
-                const uint2v bits = __builtin_bit_cast(uint2v, got);
-                v[2 * half] = bits[0];
-                v[2 * half + 1] = bits[1];
-            }
-            return v;
+            typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
+            const char *const from = tile + at[i] + step * 32 * ROW;
+            const uint2v low = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((BT_LDS short4v *)from));
+            const uint2v high = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((BT_LDS short4v *)(from + 4 * ROW)));
+            return raw16{low[0], low[1], high[0], high[1]};
         } else {
             raw16 v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = step * 16 + group * 4 + j, n = at + t;
-                v[j] = *(const uint32_t *)(tile + place(k, n / 4) + (n % 4) * 4);
-            }
+            for (int j = 0; j < 4; ++j) v[j] = *(const uint32_t *)(tile + at[i] + (step * 16 + j) * ROW);
             return v;
         }
     }
@@ -99,23 +112,30 @@ struct Operand {
     uint32_t rows, cols;
 };
 
-constexpr int kTileN = 128, kThreads = 256;      // of both operands of a product; threads of a workgroup: 2 by 2 waves of 64 by 64
+// A workgroup: WP waves along P by two along Q, each of FP fragments of P by FQ of Q.
+template <int WP_, int FP_, int FQ_> struct Shape {
+    static constexpr int WP = WP_, FP = FP_, FQ = FQ_, WAVES = 2 * WP, THREADS = WAVES * kWave, NP = WP * FP * 16, NQ = 2 * FQ * 16;
+};
+typedef Shape<4, 4, 8> Large;      // 256 by 256, 8 waves
+typedef Shape<2, 4, 4> Middle;     // 128 by 128, 4 waves
+typedef Shape<2, 2, 2> Small;      // 64 by 64, 4 waves
 
-// Chunks of a tile on their way from memory to LDS, in registers.
-template <class T, Order O> struct Staged {
-    typedef Tile<T, O, kTileN> L;
+// Chunks of a tile on their way from memory to LDS, in registers.  (F: of the forward pass, fragments of a wave.)
+template <class T, Order O, int N, int F, int kThreads> struct Staged {
+    typedef Tile<T, O, N> L;
     static constexpr int PER = L::ROWS * L::CHUNKS / kThreads;
     raw16 v[PER];
 
-    // `n`: the product's row or column that the tile begins at (of 64 of two operands in turn, where `other` is given), `k`: the summed index.
+    // `n`: the product's row or column that the tile begins at, `k`: the summed index.  `two`: the forward pass, each wave's rows half of one
+    // weight and half of the other.
     __device__ void load(const Operand &a, const Operand &other, const bool two, const uint32_t n, const uint32_t k) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int q = i * kThreads + threadIdx.x, row = q / L::CHUNKS, col = (q % L::CHUNKS) * kPer<T>;
             if constexpr (O == kAlong) {
-                // the forward pass: 32 rows of one weight and 32 of the other for each wave
-                const Operand &from = two && (row & 32) ? other : a;
-                const uint32_t r = n + (two ? (row / 64) * 32 + row % 32 : row);
+                constexpr int kHalf = F * 8;      // rows of a wave that belong to one weight
+                const Operand &from = two && (row / kHalf) % 2 ? other : a;
+                const uint32_t r = n + (two ? row / (2 * kHalf) * kHalf + row % kHalf : row);
                 v[i] = raw16{0, 0, 0, 0};
                 if (r < from.rows) v[i] = load_vec((const T *)from.p + r * from.pitch + k + col, (int64_t)from.cols - k - col);
             } else {
@@ -188,63 +208,46 @@ struct GatedJob {
 template <class T, Product K> constexpr Order kOrderP = K == kForward ? kAlong : kAcross;
 template <class T, Product K> constexpr Order kOrderQ = K == kGradW ? kAcross : kAlong;
 
-template <class T, Product K> __global__ __launch_bounds__(kThreads) void gated_kernel(const GatedJob a) {
-    typedef Tile<T, kOrderP<T, K>, kTileN> P;
-    typedef Tile<T, kOrderQ<T, K>, kTileN> Q;
-    __shared__ __align__(16) char tiles[P::BYTES + Q::BYTES];
-    char *const tile_p = tiles, *const tile_q = tiles + P::BYTES;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, wp = wave % 2, wq = wave / 2;
-    constexpr int kCols = K == kForward ? kTileN / 2 : kTileN;      // columns of the output in a tile
-    uint32_t tile = blockIdx.x;
-    const int part = K == kGradW ? tile / (a.tiles_m * a.tiles_n) : 0;
-    tile -= part * a.tiles_m * a.tiles_n;
-    const uint32_t m = (tile / a.tiles_n) * kTileN, n = (tile % a.tiles_n) * kCols;
-    acc4 acc[4][4];
+// Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn, each of which has an L2 of its own: an XCD's are neighbours, in bands
+// of four rows of tiles, so that those that run at once share what they read.
+struct Place {
+    uint32_t m, n, part;
+};
+
+template <Product K> __device__ inline Place place_of(const GatedJob &a, const uint32_t tile_m, const uint32_t tile_n) {
+    constexpr uint32_t kXcds = 8, kBand = 4;
+    const uint32_t total = gridDim.x, xcd = blockIdx.x % kXcds, more = total % kXcds;
+    uint32_t tile = xcd * (total / kXcds) + (xcd < more ? xcd : more) + blockIdx.x / kXcds;
+    Place at;
+    at.part = K == kGradW ? tile / (a.tiles_m * a.tiles_n) : 0;
+    tile -= at.part * a.tiles_m * a.tiles_n;
+    const uint32_t band = tile / (kBand * a.tiles_n), left = a.tiles_m - band * kBand, high = left < kBand ? left : kBand;
+    tile -= band * kBand * a.tiles_n;
+    at.m = (band * kBand + tile % high) * tile_m;
+    at.n = tile / high * tile_n;
+    return at;
+}
+
+// What becomes of a wave's sums: rows from m on, FQ fragments of 16; columns from n on, FP fragments, of the forward pass half of them columns
+// of the gate's product and half the same columns of the other.
+template <class T, Product K, int FP, int FQ> __device__ inline void finish(const GatedJob &a, const acc4 (&acc)[FP][FQ], const uint32_t m, const uint32_t n, const uint32_t part) {
+    const int lane = threadIdx.x % kWave;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = acc4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int sum = 0; sum < (K == kGradX ? 2 : 1); ++sum) {
-        const Operand &op = a.p[K == kGradX ? sum : 0], &oq = a.q[K == kGradX ? sum : part];
-        for (uint32_t k = 0; k < a.k; k += kK<T>) {
-            Staged<T, kOrderP<T, K>> sp;
-            Staged<T, kOrderQ<T, K>> sq;
-            sp.load(op, a.p[1], K == kForward, n, k);
-            sq.load(oq, oq, false, m, k);
-            __syncthreads();
-            sp.store(tile_p);
-            sq.store(tile_q);
-            __syncthreads();
-#pragma unroll
-            for (int step = 0; step < kK<T> / kKStep<T>; ++step) {
-                raw16 p[4], q[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = P::fragment(tile_p, wp * 64 + i * 16, step);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) q[i] = Q::fragment(tile_q, wq * 64 + i * 16, step);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] = multiply<T>(p[i], q[j], acc[i][j]);
-            }
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t row = m + wq * 64 + j * 16 + lane % 16;
+    for (int j = 0; j < FQ; ++j) {
+        const uint32_t row = m + j * 16 + lane % 16;
         if (row >= a.m) continue;
-        if constexpr (K == kForward) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t col = n + wp * 32 + i * 16 + lane / 16 * 4;
-                const int64_t left = (int64_t)a.n - col;
-                const uint64_t at = row * a.pitch + col;
-                if (left <= 0) continue;
+        for (int i = 0; i < (K == kForward ? FP / 2 : FP); ++i) {
+            const uint32_t col = n + i * 16 + lane / 16 * 4;
+            const int64_t left = (int64_t)a.n - col;
+            const uint64_t at = row * a.pitch + col;
+            if (left <= 0) continue;
+            if constexpr (K == kForward) {
                 float g[4], u[4], h[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     g[r] = acc[i][j][r];
-                    u[r] = acc[i + 2][j][r];
+                    u[r] = acc[i + FP / 2][j][r];
                     if (a.activation == BT_ACT_RELU) {
                         const bool closed = g[r] <= 0.0f;
                         h[r] = closed ? 0.0f : g[r] * u[r];
@@ -257,17 +260,209 @@ template <class T, Product K> __global__ __launch_bounds__(kThreads) void gated_
                     store4((T *)a.gate + at, left, g);
                     store4((T *)a.up + at, left, u);
                 }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t col = n + wp * 64 + i * 16 + lane / 16 * 4;
-                const int64_t left = (int64_t)a.n - col;
+            } else {
                 const float x[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                if (left > 0) store4((T *)a.out[part] + row * a.pitch + col, left, x);
+                store4((T *)a.out[part] + at, left, x);
             }
         }
     }
+}
+
+// What the two kernels below share: their waves, tiles and steps.
+template <class T, Product K, class S> struct Work {
+    typedef Tile<T, kOrderP<T, K>, S::NP> P;
+    typedef Tile<T, kOrderQ<T, K>, S::NQ> Q;
+    typedef acc4 Sums[S::FP][S::FQ];
+    static constexpr int COLS = K == kForward ? S::NP / 2 : S::NP;      // columns of the output in a tile
+    static constexpr int SUMS = K == kGradX ? 2 : 1;
+
+    Reader<T, kOrderP<T, K>, S::NP, S::FP> rp;
+    Reader<T, kOrderQ<T, K>, S::NQ, S::FQ> rq;
+    raw16 p[2][S::FP], q[S::FQ];      // fragments: of P of a step and the next one, of Q of a step, the halves in turn
+
+    __device__ Work() {
+        const int wave = threadIdx.x / kWave;
+        rp.start((wave / 2) * S::FP * 16);
+        rq.start((wave % 2) * S::FQ * 16);
+    }
+    __device__ void read_p(const char *tile, const int step) {
+#pragma unroll
+        for (int i = 0; i < S::FP; ++i) p[step][i] = rp.read(tile, i, step);
+    }
+    __device__ void read_q(const char *tile, const int step, const int half) {
+#pragma unroll
+        for (int j = half * S::FQ / 2; j < (half + 1) * S::FQ / 2; ++j) q[j] = rq.read(tile, j, step);
+    }
+    __device__ void multiply(Sums &acc, const int step, const int half) {
+#pragma unroll
+        for (int i = 0; i < S::FP; ++i)
+#pragma unroll
+            for (int j = half * S::FQ / 2; j < (half + 1) * S::FQ / 2; ++j) acc[i][j] = btb::multiply<T>(p[step][i], q[j], acc[i][j]);
+    }
+
+    // The tiles that begin at k of the summed index through registers, and their products.
+    __device__ void staged(const GatedJob &a, const Operand &op, const Operand &oq, const Place &at, const uint32_t k, char *tile_p, char *tile_q, Sums &acc) {
+        __syncthreads();
+        {
+            Staged<T, kOrderP<T, K>, S::NP, S::FP, S::THREADS> sp;
+            sp.load(op, a.p[1], K == kForward, at.n, k);
+            sp.store(tile_p);
+        }
+        {
+            Staged<T, kOrderQ<T, K>, S::NQ, S::FQ, S::THREADS> sq;
+            sq.load(oq, oq, false, at.m, k);
+            sq.store(tile_q);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            read_p(tile_p, step);
+            read_q(tile_q, step, 0);
+            read_q(tile_q, step, 1);
+            multiply(acc, step, 0);
+            multiply(acc, step, 1);
+        }
+    }
+
+    __device__ static void end(const GatedJob &a, const Sums &acc, const Place &at) {
+        const int wave = threadIdx.x / kWave;
+        finish<T, K, S::FP, S::FQ>(a, acc, at.m + (wave % 2) * S::FQ * 16, at.n + (wave / 2) * (COLS / S::WP), at.part);
+    }
+};
+
+// Any alignment and any size: tiles go through registers, one at a time.
+template <class T, Product K> __global__ __launch_bounds__(Middle::THREADS) void gated_any_kernel(const GatedJob a) {
+    typedef Work<T, K, Middle> W;
+    __shared__ __align__(16) char tiles[W::P::BYTES + W::Q::BYTES];
+    const Place at = place_of<K>(a, Middle::NQ, W::COLS);
+    typename W::Sums acc = {};
+    W w;
+    for (int sum = 0; sum < W::SUMS; ++sum)
+        for (uint32_t k = 0; k < a.k; k += kK<T>) w.staged(a, a.p[sum], a.q[sum + at.part], at, k, tiles, tiles + W::P::BYTES, acc);
+    W::end(a, acc, at);
+}
+
+// An operand's tiles straight from memory to LDS, 1 KiB an instruction of a wave, an equal part of the tile a wave.  Needs rows of whole vectors on
+// 16-byte boundaries; what lies beyond the operand's end is not read (the descriptor has its size), what is read beyond a row's end belongs
+// to rows or columns that are not stored.
+template <class T, Order O, int N, int WAVES> struct Direct {
+    typedef Tile<T, O, N> L;
+    static constexpr int S = (int)sizeof(T), PER = N / 8 / WAVES;
+    uint32_t offset[PER];        // of the lane's vector in each instruction's KiB, from the tile's first
+    const char *base;
+    uint64_t left, advance;      // bytes of the operand from `base` on; and from one tile to the next
+
+    // `n`: the product's row or column that the tile begins at.
+    __device__ void start(const Operand &a, const uint32_t n) {
+        const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int q = (wave * PER + i) * kWave + lane, row = q / L::CHUNKS, chunk = (L::place(row, q % L::CHUNKS) / kVec) % L::CHUNKS;
+            offset[i] = (uint32_t)(row * a.pitch * S) + chunk * kVec;
+        }
+        if constexpr (O == kAlong) {
+            base = (const char *)a.p + (uint64_t)n * a.pitch * S;
+            left = ((uint64_t)(a.rows - n) * a.pitch - (a.pitch - a.cols)) * S;
+            advance = kK<T> * S;
+        } else {
+            base = (const char *)a.p + (uint64_t)n * S;
+            left = ((uint64_t)a.rows * a.pitch - (a.pitch - a.cols) - n) * S;
+            advance = kK<T> * a.pitch * S;
+        }
+    }
+    // The forward pass: rows of the two weights in turn, 8 F of each.  The loading wave's part of the tile is one such run.
+    template <int F> __device__ void start_pair(const Operand &gate, const Operand &up, const uint32_t n) {
+        static_assert(PER == F, "a wave's part belongs to one weight");
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        const uint32_t first = n + wave / 2 * F * 8;         // row of the weight that the part begins with
+        const Operand &a = wave % 2 ? up : gate;
+        const bool there = first < a.rows;
+        start(a, there ? first : 0);
+        if (!there) left = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) offset[i] -= (uint32_t)(wave * F * 8 * a.pitch * S);
+    }
+    __device__ void fetch(char *tile) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)(left < 0x7ffffff0u ? left : 0x7ffffff0u), 0x00020000);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (BT_LDS void *)(tile + (wave * PER + i) * 1024), 16, (int)offset[i], 0, 0, 0);
+        base += advance;
+        left = left > advance ? left - advance : 0;
+    }
+};
+
+__device__ inline void wait_for_tiles() {
+    asm volatile("" ::: "memory");           // (the barrier itself keeps the compiler's loads and stores from nothing)
+    __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): this wave's parts of the tiles have landed
+    __builtin_amdgcn_s_barrier();            // and those of the others, which have also read what they need of the tiles before
+    asm volatile("" ::: "memory");
+}
+
+// Two tiles of either operand in LDS: while one is multiplied, the next one is on its way.  A tile is two steps, a step two halves of Q's
+// fragments; the fragments of a half (and with the first, P's) are read while the half before is multiplied.  Behind the one barrier of a tile,
+// at its last half, the place of the tile has been read by all and is free for the tile after the next.
+template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, S::THREADS >= 512 ? 2 : 1) void gated_kernel(const GatedJob a) {
+    typedef Work<T, K, S> W;
+    constexpr int PB = W::P::BYTES, QB = W::Q::BYTES;
+    __shared__ __align__(1024) char tiles[2 * (PB + QB)];
+    const Place at = place_of<K>(a, S::NQ, W::COLS);
+    typename W::Sums acc = {};
+    W w;
+    const uint32_t count = a.k / kK<T>;      // whole tiles
+    for (int sum = 0; sum < W::SUMS; ++sum) {
+        const Operand &op = a.p[sum], &oq = a.q[sum + at.part];
+        if (count != 0) {
+            Direct<T, kOrderP<T, K>, S::NP, S::WAVES> dp;
+            Direct<T, kOrderQ<T, K>, S::NQ, S::WAVES> dq;
+            if constexpr (K == kForward) dp.template start_pair<S::FP>(a.p[0], a.p[1], at.n);
+            else dp.start(op, at.n);
+            dq.start(oq, at.m);
+            const auto tile_p = [&](const int b) { return tiles + b * PB; };
+            const auto tile_q = [&](const int b) { return tiles + 2 * PB + b * QB; };
+            const auto fetch = [&](const int b) {
+                dp.fetch(tile_p(b));
+                dq.fetch(tile_q(b));
+            };
+            // Tile t, which lies in place b.
+            const auto tile = [&](const uint32_t t, const int b) {
+                w.read_q(tile_q(b), 0, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                w.multiply(acc, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                w.read_p(tile_p(b), 1);
+                w.read_q(tile_q(b), 1, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                w.multiply(acc, 0, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                w.read_q(tile_q(b), 1, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                w.multiply(acc, 1, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the last fragments of this tile are here
+                wait_for_tiles();
+                if (t + 2 < count) fetch(b);
+                w.read_p(tile_p(b ^ 1), 0);              // (behind the last tile: what lies there, unused)
+                w.read_q(tile_q(b ^ 1), 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                w.multiply(acc, 1, 1);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            if (sum != 0) __syncthreads();
+            fetch(0);
+            wait_for_tiles();
+            if (count > 1) fetch(1);
+            w.read_p(tile_p(0), 0);
+            w.read_q(tile_q(0), 0, 0);
+            for (uint32_t t = 0; t < count; t += 2) {
+                tile(t, 0);
+                if (t + 1 < count) tile(t + 1, 1);
+            }
+        }
+        // The rest of the summed index, less than a tile, through registers.
+        if (count * kK<T> < a.k) w.staged(a, op, oq, at, count * kK<T>, tiles, tiles + 2 * PB, acc);
+    }
+    W::end(a, acc, at);
 }
 
 // dg = grad_h u act'(g) and du = grad_h act(g), rounded to the type: they are factors of the products, whose matrix instructions take them
@@ -315,12 +510,32 @@ bool known(const bt_activation a) { return a == BT_ACT_RELU || a == BT_ACT_SILU 
 
 uint32_t ceil_div(const uint64_t a, const uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
+template <Product K, class S> uint64_t tiles_of(GatedJob &a) {
+    a.tiles_m = ceil_div(a.m, S::NQ);
+    a.tiles_n = ceil_div(a.n, K == kForward ? S::NP / 2 : S::NP);
+    return (uint64_t)a.tiles_m * a.tiles_n * (K == kGradW ? 2 : 1);
+}
+
+// Rows of whole vectors on 16-byte boundaries, and a tile within 32 bits of offsets.
+template <class T> bool direct(const Operand &a) {
+    return !misaligned(a.p, kVec) && a.pitch % kPer<T> == 0 && a.pitch * sizeof(T) * 320 < 1u << 31;
+}
+
 template <class T, Product K> bt_status run_product(GatedJob &a, hipStream_t hs) {
-    a.tiles_m = ceil_div(a.m, kTileN);
-    a.tiles_n = ceil_div(a.n, K == kForward ? kTileN / 2 : kTileN);
-    const uint64_t tiles = (uint64_t)a.tiles_m * a.tiles_n * (K == kGradW ? 2 : 1);
-    if (tiles >= 1u << 24) return BT_ERR_SIZE;      // (a grid holds less than 2^32 threads)
-    return launch(gated_kernel<T, K>, dim3((unsigned)tiles), kThreads, hs, a);
+    bool straight = direct<T>(a.p[0]) && direct<T>(a.q[0]);
+    if (K != kGradW) straight = straight && direct<T>(a.p[1]);
+    if (K != kForward) straight = straight && direct<T>(a.q[1]);
+    const auto go = [&](auto kernel, auto shape) {
+        typedef decltype(shape) S;
+        const uint64_t tiles = tiles_of<K, S>(a);
+        if (tiles >= 1u << 23) return BT_ERR_SIZE;      // (a grid holds less than 2^32 threads)
+        return launch(kernel, dim3((unsigned)tiles), S::THREADS, hs, a);
+    };
+    if (!straight) return go(gated_any_kernel<T, K>, Middle{});
+    if constexpr (sizeof(T) == 2)
+        if (tiles_of<K, Large>(a) >= 256) return go(gated_kernel<T, K, Large>, Large{});
+    if (tiles_of<K, Middle>(a) >= 256) return go(gated_kernel<T, K, Middle>, Middle{});
+    return go(gated_kernel<T, K, Small>, Small{});
 }
 
 }  // namespace
