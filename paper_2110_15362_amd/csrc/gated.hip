@@ -25,7 +25,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // Q) in element r of lane l: with P the operand along which the output is contiguous, a lane holds four neighbours of a row.
 
 template <class T> constexpr int kKStep = 4 * kPer<T>;       // 32 or, in single precision, 16
-constexpr int kKBytes = 128;                                 // of the summed index in a tile
+constexpr int kKBytes = 64;                                  // of the summed index in a tile: one step
 template <class T> constexpr int kK = kKBytes / (int)sizeof(T);
 
 template <class T> __device__ inline acc4 multiply(const raw16 p, const raw16 q, acc4 c) {
@@ -42,7 +42,7 @@ template <class T> __device__ inline acc4 multiply(const raw16 p, const raw16 q,
 // ---- tiles in LDS ----------------------------------------------------------------------------------------------
 //
 // An operand comes in one of two orders: with the summed index contiguous in memory (K rows: an LDS row is one row or column of the
-// product, 128 bytes of the summed index) or with it across the rows (N rows: an LDS row is one summed index, the tile's rows or
+// product, 64 bytes of the summed index) or with it across the rows (N rows: an LDS row is one summed index, the tile's rows or
 // columns lie along it).  16-byte chunks of an LDS row are stored in an order that depends on the row, so that the lanes that read one
 // fragment meet different banks.
 
@@ -56,7 +56,7 @@ template <class T, Order O, int N> struct Tile {      // N rows or columns of th
     // (Of the rows that one fragment has, those of a lane share the key.)
     __device__ static int place(const int row, const int chunk) {
         int key;
-        if constexpr (O == kAlong) key = row & 7;
+        if constexpr (O == kAlong) key = (row >> 2) & 3;
         else if constexpr (sizeof(T) == 2 && CHUNKS == 8) key = 2 * (((row >> 1) & 1) | ((row >> 2) & 2));
         else if constexpr (sizeof(T) == 2) key = 2 * ((row & 3) | ((row >> 1) & 4));
         else key = 4 * ((row >> 2) & 3);
@@ -64,19 +64,17 @@ template <class T, Order O, int N> struct Tile {      // N rows or columns of th
     }
 };
 
-// A wave's fragments of a tile: F times 16 rows or columns from `first` on.  Where a lane reads depends on the step, the fragment and the tile
-// by constants alone, but for one address a step (summed index along) or a fragment (across).
+// A wave's fragments of a tile: F times 16 rows or columns from `first` on.  Where a lane reads depends on the fragment and the tile by constants
+// alone, but for one address (summed index along) or one a fragment (across).
 template <class T, Order O, int N, int F> struct Reader {
     typedef Tile<T, O, N> L;
-    static constexpr int ROW = L::CHUNKS * kVec;
-    uint32_t at[O == kAlong ? 2 : F];
+    static constexpr int ROW = L::CHUNKS * kVec, READS = O == kAlong ? 1 : sizeof(T) == 2 ? 2 : 4;      // instructions a fragment
+    uint32_t at[O == kAlong ? 1 : F];
 
     __device__ void start(const int first) {
         const int lane = threadIdx.x % kWave, group = lane / 16, t = lane % 16;
-        if constexpr (O == kAlong) {
-#pragma unroll
-            for (int step = 0; step < 2; ++step) at[step] = L::place(first + t, step * 4 + group);
-        } else {
+        if constexpr (O == kAlong) at[0] = L::place(first + t, group);
+        else {
 #pragma unroll
             for (int i = 0; i < F; ++i) {
                 const int n = first + i * 16;
@@ -86,20 +84,20 @@ template <class T, Order O, int N, int F> struct Reader {
         }
     }
 
-    __device__ raw16 read(const char *tile, const int i, const int step) const {
+    __device__ raw16 read(const char *tile, const int i) const {
         if constexpr (O == kAlong) {
-            return *(const raw16 *)(tile + at[step] + i * 16 * ROW);
+            return *(const raw16 *)(tile + at[0] + i * 16 * ROW);
         } else if constexpr (sizeof(T) == 2) {
             // 16 lanes read 4 summed indices by 16 columns, 4 columns a lane, and get one column each
             typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
-            const char *const from = tile + at[i] + step * 32 * ROW;
+            const char *const from = tile + at[i];
             const uint2v low = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((BT_LDS short4v *)from));
             const uint2v high = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((BT_LDS short4v *)(from + 4 * ROW)));
             return raw16{low[0], low[1], high[0], high[1]};
         } else {
             raw16 v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = *(const uint32_t *)(tile + at[i] + (step * 16 + j) * ROW);
+            for (int j = 0; j < 4; ++j) v[j] = *(const uint32_t *)(tile + at[i] + j * ROW);
             return v;
         }
     }
@@ -278,26 +276,26 @@ template <class T, Product K, class S> struct Work {
 
     Reader<T, kOrderP<T, K>, S::NP, S::FP> rp;
     Reader<T, kOrderQ<T, K>, S::NQ, S::FQ> rq;
-    raw16 p[2][S::FP], q[S::FQ];      // fragments: of P of a step and the next one, of Q of a step, the halves in turn
+    raw16 p[2][S::FP], q[S::FQ];      // fragments: of P of a tile and the next one, of Q the halves in turn
 
     __device__ Work() {
         const int wave = threadIdx.x / kWave;
         rp.start((wave / 2) * S::FP * 16);
         rq.start((wave % 2) * S::FQ * 16);
     }
-    __device__ void read_p(const char *tile, const int step) {
+    __device__ void read_p(const char *tile, const int parity) {
 #pragma unroll
-        for (int i = 0; i < S::FP; ++i) p[step][i] = rp.read(tile, i, step);
+        for (int i = 0; i < S::FP; ++i) p[parity][i] = rp.read(tile, i);
     }
-    __device__ void read_q(const char *tile, const int step, const int half) {
+    __device__ void read_q(const char *tile, const int half) {
 #pragma unroll
-        for (int j = half * S::FQ / 2; j < (half + 1) * S::FQ / 2; ++j) q[j] = rq.read(tile, j, step);
+        for (int j = half * S::FQ / 2; j < (half + 1) * S::FQ / 2; ++j) q[j] = rq.read(tile, j);
     }
-    __device__ void multiply(Sums &acc, const int step, const int half) {
+    __device__ void multiply(Sums &acc, const int parity, const int half) {
 #pragma unroll
         for (int i = 0; i < S::FP; ++i)
 #pragma unroll
-            for (int j = half * S::FQ / 2; j < (half + 1) * S::FQ / 2; ++j) acc[i][j] = btb::multiply<T>(p[step][i], q[j], acc[i][j]);
+            for (int j = half * S::FQ / 2; j < (half + 1) * S::FQ / 2; ++j) acc[i][j] = btb::multiply<T>(p[parity][i], q[j], acc[i][j]);
     }
 
     // The tiles that begin at k of the summed index through registers, and their products.
@@ -314,14 +312,11 @@ template <class T, Product K, class S> struct Work {
             sq.store(tile_q);
         }
         __syncthreads();
-#pragma unroll
-        for (int step = 0; step < 2; ++step) {
-            read_p(tile_p, step);
-            read_q(tile_q, step, 0);
-            read_q(tile_q, step, 1);
-            multiply(acc, step, 0);
-            multiply(acc, step, 1);
-        }
+        read_p(tile_p, 0);
+        read_q(tile_q, 0);
+        read_q(tile_q, 1);
+        multiply(acc, 0, 0);
+        multiply(acc, 0, 1);
     }
 
     __device__ static void end(const GatedJob &a, const Sums &acc, const Place &at) {
@@ -343,69 +338,87 @@ template <class T, Product K> __global__ __launch_bounds__(Middle::THREADS) void
 }
 
 // An operand's tiles straight from memory to LDS, 1 KiB an instruction of a wave, an equal part of the tile a wave.  Needs rows of whole vectors on
-// 16-byte boundaries; what lies beyond the operand's end is not read (the descriptor has its size), what is read beyond a row's end belongs
-// to rows or columns that are not stored.
+// 16-byte boundaries.  What a tile has beyond the operand's rows (or, where the summed index lies across, columns) is read from inside of it: it
+// belongs to rows or columns of the product that are not stored.
 template <class T, Order O, int N, int WAVES> struct Direct {
     typedef Tile<T, O, N> L;
-    static constexpr int S = (int)sizeof(T), PER = N / 8 / WAVES;
+    static constexpr int S = (int)sizeof(T), PER = N / 16 / WAVES;
     uint32_t offset[PER];        // of the lane's vector in each instruction's KiB, from the tile's first
     const char *base;
-    uint64_t left, advance;      // bytes of the operand from `base` on; and from one tile to the next
+    uint64_t advance;            // bytes from one tile to the next
 
-    // `n`: the product's row or column that the tile begins at.
-    __device__ void start(const Operand &a, const uint32_t n) {
+    // `n`: the product's row or column that the tile begins at, `skip` rows of the tile being others'.
+    __device__ void start(const Operand &a, const uint32_t n, const int skip = 0) {
         const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int q = (wave * PER + i) * kWave + lane, row = q / L::CHUNKS, chunk = (L::place(row, q % L::CHUNKS) / kVec) % L::CHUNKS;
-            offset[i] = (uint32_t)(row * a.pitch * S) + chunk * kVec;
+            const int q = (wave * PER + i) * kWave + lane, chunk = (L::place(q / L::CHUNKS, q % L::CHUNKS) / kVec) % L::CHUNKS;
+            uint32_t row = q / L::CHUNKS - skip, col = chunk * kPer<T>;
+            if (O == kAlong && n + row >= a.rows) row = 0;
+            if (O == kAcross && n + col >= a.cols) col = 0;
+            offset[i] = (uint32_t)(row * a.pitch + col) * S;
         }
-        if constexpr (O == kAlong) {
-            base = (const char *)a.p + (uint64_t)n * a.pitch * S;
-            left = ((uint64_t)(a.rows - n) * a.pitch - (a.pitch - a.cols)) * S;
-            advance = kK<T> * S;
-        } else {
-            base = (const char *)a.p + (uint64_t)n * S;
-            left = ((uint64_t)a.rows * a.pitch - (a.pitch - a.cols) - n) * S;
-            advance = kK<T> * a.pitch * S;
-        }
+        base = (const char *)a.p + (O == kAlong ? n * a.pitch : (uint64_t)n) * S;
+        advance = (O == kAlong ? kK<T> : kK<T> * a.pitch) * S;
     }
     // The forward pass: rows of the two weights in turn, 8 F of each.  The loading wave's part of the tile is one such run.
     template <int F> __device__ void start_pair(const Operand &gate, const Operand &up, const uint32_t n) {
-        static_assert(PER == F, "a wave's part belongs to one weight");
+        static_assert(2 * PER == F, "a wave's part belongs to one weight");
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const uint32_t first = n + wave / 2 * F * 8;         // row of the weight that the part begins with
         const Operand &a = wave % 2 ? up : gate;
-        const bool there = first < a.rows;
-        start(a, there ? first : 0);
-        if (!there) left = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) offset[i] -= (uint32_t)(wave * F * 8 * a.pitch * S);
+        start(a, first < a.rows ? first : 0, wave * F * 8);
     }
     __device__ void fetch(char *tile) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)(left < 0x7ffffff0u ? left : 0x7ffffff0u), 0x00020000);
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00020000);
 #pragma unroll
         for (int i = 0; i < PER; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (BT_LDS void *)(tile + (wave * PER + i) * 1024), 16, (int)offset[i], 0, 0, 0);
         base += advance;
-        left = left > advance ? left - advance : 0;
     }
 };
 
-__device__ inline void wait_for_tiles() {
+// Until all but the last `LEFT` of this wave's fetches have landed, then for the other waves: their fetches have landed too, and they have read
+// what they need of the tiles before.
+template <int LEFT> __device__ inline void wait_for_tiles() {
+    static_assert(LEFT < 64);
     asm volatile("" ::: "memory");           // (the barrier itself keeps the compiler's loads and stores from nothing)
-    __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): this wave's parts of the tiles have landed
-    __builtin_amdgcn_s_barrier();            // and those of the others, which have also read what they need of the tiles before
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (LEFT & 15) | (LEFT >> 4) << 14);      // vmcnt
+    __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
-// Two tiles of either operand in LDS: while one is multiplied, the next one is on its way.  A tile is two steps, a step two halves of Q's
-// fragments; the fragments of a half (and with the first, P's) are read while the half before is multiplied.  Behind the one barrier of a tile,
-// at its last half, the place of the tile has been read by all and is free for the tile after the next.
+// Four tiles of either operand in LDS: while one is multiplied, the next three are on their way.  A tile's products are made in two halves (of
+// Q's fragments).  While the first is made, the second's fragments are read and the tile three further on is asked for, while the second is made,
+// the next tile's; behind the barrier between them a tile's place has been read by all.  The instructions of either kind are spread among the
+// products: each waits for the unit that takes it, and a wave that waits for that multiplies nothing.
+constexpr int kPlaces = 4;
+
+template <int KIND, int COUNT, int PRODUCTS, int GROUPS, int G = 0> __device__ inline void spread_kind() {
+    if constexpr (G < GROUPS) {
+        constexpr int c = COUNT * (G + 1) / GROUPS - COUNT * G / GROUPS, m = PRODUCTS * (G + 1) / GROUPS - PRODUCTS * G / GROUPS;
+        __builtin_amdgcn_sched_group_barrier(KIND, c, 0);
+        if constexpr (m != 0) __builtin_amdgcn_sched_group_barrier(0x8, m, 0);
+        spread_kind<KIND, COUNT, PRODUCTS, GROUPS, G + 1>();
+    }
+}
+
+// The schedule of a half: `READS` reads of LDS, then `FETCHES` fetches (which the compiler takes for writes to what is read), among `PRODUCTS`
+// products.
+template <int READS, int FETCHES, int PRODUCTS> __device__ inline void spread() {
+    constexpr int kFirst = PRODUCTS * READS / (READS + FETCHES), kSecond = PRODUCTS - kFirst;
+    spread_kind<0x100, READS, kFirst, (READS < kFirst ? READS : kFirst)>();
+    if constexpr (FETCHES != 0) spread_kind<0x10, FETCHES, kSecond, (FETCHES < kSecond ? FETCHES : kSecond)>();
+}
+
 template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, S::THREADS >= 512 ? 2 : 1) void gated_kernel(const GatedJob a) {
     typedef Work<T, K, S> W;
-    constexpr int PB = W::P::BYTES, QB = W::Q::BYTES;
-    __shared__ __align__(1024) char tiles[2 * (PB + QB)];
+    typedef Direct<T, kOrderP<T, K>, S::NP, S::WAVES> FetchP;
+    typedef Direct<T, kOrderQ<T, K>, S::NQ, S::WAVES> FetchQ;
+    constexpr int PB = W::P::BYTES, QB = W::Q::BYTES, kFetches = FetchP::PER + FetchQ::PER;
+    constexpr int kReadsP = S::FP * Reader<T, kOrderP<T, K>, S::NP, S::FP>::READS, kReadsQ = S::FQ / 2 * Reader<T, kOrderQ<T, K>, S::NQ, S::FQ>::READS;
+    constexpr int kProducts = S::FP * S::FQ / 2 * (sizeof(T) == 4 ? 4 : 1);
+    __shared__ __align__(1024) char tiles[kPlaces * (PB + QB)];
     const Place at = place_of<K>(a, S::NQ, W::COLS);
     typename W::Sums acc = {};
     W w;
@@ -413,54 +426,58 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
     for (int sum = 0; sum < W::SUMS; ++sum) {
         const Operand &op = a.p[sum], &oq = a.q[sum + at.part];
         if (count != 0) {
-            Direct<T, kOrderP<T, K>, S::NP, S::WAVES> dp;
-            Direct<T, kOrderQ<T, K>, S::NQ, S::WAVES> dq;
+            FetchP dp;
+            FetchQ dq;
             if constexpr (K == kForward) dp.template start_pair<S::FP>(a.p[0], a.p[1], at.n);
             else dp.start(op, at.n);
             dq.start(oq, at.m);
-            const auto tile_p = [&](const int b) { return tiles + b * PB; };
-            const auto tile_q = [&](const int b) { return tiles + 2 * PB + b * QB; };
-            const auto fetch = [&](const int b) {
-                dp.fetch(tile_p(b));
-                dq.fetch(tile_q(b));
+            const auto tile_p = [&](const int place) { return tiles + place * PB; };
+            const auto tile_q = [&](const int place) { return tiles + kPlaces * PB + place * QB; };
+            const auto fetch = [&](const int place) {
+                dp.fetch(tile_p(place));
+                dq.fetch(tile_q(place));
             };
-            // Tile t, which lies in place b.
-            const auto tile = [&](const uint32_t t, const int b) {
-                w.read_q(tile_q(b), 0, 1);
-                __builtin_amdgcn_sched_barrier(0);
-                w.multiply(acc, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-                w.read_p(tile_p(b), 1);
-                w.read_q(tile_q(b), 1, 0);
-                __builtin_amdgcn_sched_barrier(0);
-                w.multiply(acc, 0, 1);
-                __builtin_amdgcn_sched_barrier(0);
-                w.read_q(tile_q(b), 1, 1);
-                __builtin_amdgcn_sched_barrier(0);
-                w.multiply(acc, 1, 0);
+            // The tile that lies in `place`; `more`: there is one three further on.
+            const auto tile = [&](const int place, const bool more) {
+                w.read_q(tile_q(place), 1);
+                if (more) fetch((place + 3) % kPlaces);
+                w.multiply(acc, place & 1, 0);
+                spread<kReadsQ, kFetches, kProducts>();
                 __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the last fragments of this tile are here
-                wait_for_tiles();
-                if (t + 2 < count) fetch(b);
-                w.read_p(tile_p(b ^ 1), 0);              // (behind the last tile: what lies there, unused)
-                w.read_q(tile_q(b ^ 1), 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-                w.multiply(acc, 1, 1);
+                if (more) wait_for_tiles<2 * kFetches>();
+                else wait_for_tiles<0>();
+                w.read_p(tile_p((place + 1) % kPlaces), (place + 1) & 1);      // (behind the last tile: what lies there, unused)
+                w.read_q(tile_q((place + 1) % kPlaces), 0);
+                w.multiply(acc, place & 1, 1);
+                spread<kReadsP + kReadsQ, 0, kProducts>();
                 __builtin_amdgcn_sched_barrier(0);
             };
             if (sum != 0) __syncthreads();
-            fetch(0);
-            wait_for_tiles();
-            if (count > 1) fetch(1);
+#pragma unroll
+            for (int t = 0; t < 3; ++t)
+                if ((uint32_t)t < count) fetch(t);
+            if (count >= 3) wait_for_tiles<2 * kFetches>();
+            else wait_for_tiles<0>();
             w.read_p(tile_p(0), 0);
-            w.read_q(tile_q(0), 0, 0);
-            for (uint32_t t = 0; t < count; t += 2) {
-                tile(t, 0);
-                if (t + 1 < count) tile(t + 1, 1);
+            w.read_q(tile_q(0), 0);
+            __builtin_amdgcn_sched_barrier(0);
+            uint32_t t = 0;
+            for (; t + 7 <= count; t += 4) {
+                tile(0, true);
+                tile(1, true);
+                tile(2, true);
+                tile(3, true);
+            }
+            for (; t < count; t += 4) {
+                tile(0, t + 3 < count);
+                if (t + 1 < count) tile(1, t + 4 < count);
+                if (t + 2 < count) tile(2, t + 5 < count);
+                if (t + 3 < count) tile(3, t + 6 < count);
             }
         }
         // The rest of the summed index, less than a tile, through registers.
-        if (count * kK<T> < a.k) w.staged(a, op, oq, at, count * kK<T>, tiles, tiles + 2 * PB, acc);
+        if (count * kK<T> < a.k) w.staged(a, op, oq, at, count * kK<T>, tiles, tiles + kPlaces * PB, acc);
     }
     W::end(a, acc, at);
 }
