@@ -56,7 +56,7 @@ template <class T, Order O, int N> struct Tile {      // N rows or columns of th
     // (Of the rows that one fragment has, those of a lane share the key.)
     __device__ static int place(const int row, const int chunk) {
         int key;
-        if constexpr (O == kAlong) key = (row >> 2) & 3;
+        if constexpr (O == kAlong) key = (row >> 1) & 2;
         else if constexpr (sizeof(T) == 2 && CHUNKS == 8) key = 2 * (((row >> 1) & 1) | ((row >> 2) & 2));
         else if constexpr (sizeof(T) == 2) key = 2 * ((row & 3) | ((row >> 1) & 4));
         else key = 4 * ((row >> 2) & 3);
@@ -118,6 +118,10 @@ typedef Shape<4, 4, 8> Large;      // 256 by 256, 8 waves
 typedef Shape<2, 4, 4> Middle;     // 128 by 128, 4 waves
 typedef Shape<2, 2, 2> Small;      // 64 by 64, 4 waves
 
+// The forward pass: which row of a weight, of the 8 F that a wave has of it, lies in row r of them in LDS, the wave having F fragments, F / 2 of each
+// weight.  In this order a lane's results of all fragments are 2 F neighbours of h.
+template <int F> __device__ inline int weight_row(const int r) { return r % 16 / 4 * (2 * F) + r / 16 * 4 + r % 4; }
+
 // Chunks of a tile on their way from memory to LDS, in registers.  (F: of the forward pass, fragments of a wave.)
 template <class T, Order O, int N, int F, int kThreads> struct Staged {
     typedef Tile<T, O, N> L;
@@ -133,7 +137,7 @@ template <class T, Order O, int N, int F, int kThreads> struct Staged {
             if constexpr (O == kAlong) {
                 constexpr int kHalf = F * 8;      // rows of a wave that belong to one weight
                 const Operand &from = two && (row / kHalf) % 2 ? other : a;
-                const uint32_t r = n + (two ? row / (2 * kHalf) * kHalf + row % kHalf : row);
+                const uint32_t r = n + (two ? row / (2 * kHalf) * kHalf + weight_row<F>(row % kHalf) : row);
                 v[i] = raw16{0, 0, 0, 0};
                 if (r < from.rows) v[i] = load_vec((const T *)from.p + r * from.pitch + k + col, (int64_t)from.cols - k - col);
             } else {
@@ -191,6 +195,20 @@ template <class T> __device__ inline void store4(T *p, const int64_t left, const
         if (i < left) p[i] = narrow<T>(x[i]);
 }
 
+// N neighbours, whole vectors where there are any.
+template <class T, int N> __device__ inline void store_run(T *p, const int64_t left, const float (&x)[N]) {
+    constexpr int E = kPer<T> < N ? kPer<T> : N;
+#pragma unroll
+    for (int i = 0; i < N; i += E) {
+        float y[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = x[i + e];
+        if constexpr (E == kPer<T>) {
+            if (left > i) store_vec(p + i, left - i, pack<T>(y));
+        } else if (left > i) store4(p + i, left - i, y);
+    }
+}
+
 enum Product { kForward, kGradX, kGradW };
 
 struct GatedJob {
@@ -234,33 +252,36 @@ template <class T, Product K, int FP, int FQ> __device__ inline void finish(cons
     for (int j = 0; j < FQ; ++j) {
         const uint32_t row = m + j * 16 + lane % 16;
         if (row >= a.m) continue;
-#pragma unroll
-        for (int i = 0; i < (K == kForward ? FP / 2 : FP); ++i) {
-            const uint32_t col = n + i * 16 + lane / 16 * 4;
+        if constexpr (K == kForward) {
+            constexpr int N = 2 * FP;      // neighbours that the lane has
+            const uint32_t col = n + lane / 16 * N;
             const int64_t left = (int64_t)a.n - col;
             const uint64_t at = row * a.pitch + col;
             if (left <= 0) continue;
-            if constexpr (K == kForward) {
-                float g[4], u[4], h[4];
+            float g[N], u[N], h[N];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    g[r] = acc[i][j][r];
-                    u[r] = acc[i + FP / 2][j][r];
-                    if (a.activation == BT_ACT_RELU) {
-                        const bool closed = g[r] <= 0.0f;
-                        h[r] = closed ? 0.0f : g[r] * u[r];
-                        g[r] = closed ? 0.0f : g[r];
-                        u[r] = closed ? 0.0f : u[r];
-                    } else h[r] = activate<T>(a.activation, g[r]) * u[r];
-                }
-                store4((T *)a.out[0] + at, left, h);
-                if (a.gate) {
-                    store4((T *)a.gate + at, left, g);
-                    store4((T *)a.up + at, left, u);
-                }
-            } else {
+            for (int i = 0; i < N; ++i) {
+                g[i] = acc[i / 4][j][i % 4];
+                u[i] = acc[i / 4 + FP / 2][j][i % 4];
+                if (a.activation == BT_ACT_RELU) {
+                    const bool closed = g[i] <= 0.0f;
+                    h[i] = closed ? 0.0f : g[i] * u[i];
+                    g[i] = closed ? 0.0f : g[i];
+                    u[i] = closed ? 0.0f : u[i];
+                } else h[i] = activate<T>(a.activation, g[i]) * u[i];
+            }
+            store_run<T, N>((T *)a.out[0] + at, left, h);
+            if (a.gate) {
+                store_run<T, N>((T *)a.gate + at, left, g);
+                store_run<T, N>((T *)a.up + at, left, u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < FP; ++i) {
+                const uint32_t col = n + i * 16 + lane / 16 * 4;
+                const int64_t left = (int64_t)a.n - col;
                 const float x[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                store4((T *)a.out[part] + at, left, x);
+                if (left > 0) store4((T *)a.out[part] + row * a.pitch + col, left, x);
             }
         }
     }
@@ -347,13 +368,14 @@ template <class T, Order O, int N, int WAVES> struct Direct {
     const char *base;
     uint64_t advance;            // bytes from one tile to the next
 
-    // `n`: the product's row or column that the tile begins at, `skip` rows of the tile being others'.
-    __device__ void start(const Operand &a, const uint32_t n, const int skip = 0) {
+    // `n`: the product's row or column that the tile begins at.  F: of the forward pass, whose weights' rows are those of `n` on in another order.
+    template <int F = 0> __device__ void start(const Operand &a, const uint32_t n) {
         const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int q = (wave * PER + i) * kWave + lane, chunk = (L::place(q / L::CHUNKS, q % L::CHUNKS) / kVec) % L::CHUNKS;
-            uint32_t row = q / L::CHUNKS - skip, col = chunk * kPer<T>;
+            uint32_t row = q / L::CHUNKS, col = chunk * kPer<T>;
+            if constexpr (F != 0) row = weight_row<F>(row % (8 * F));
             if (O == kAlong && n + row >= a.rows) row = 0;
             if (O == kAcross && n + col >= a.cols) col = 0;
             offset[i] = (uint32_t)(row * a.pitch + col) * S;
@@ -367,7 +389,7 @@ template <class T, Order O, int N, int WAVES> struct Direct {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const uint32_t first = n + wave / 2 * F * 8;         // row of the weight that the part begins with
         const Operand &a = wave % 2 ? up : gate;
-        start(a, first < a.rows ? first : 0, wave * F * 8);
+        start<F>(a, first < a.rows ? first : 0);
     }
     __device__ void fetch(char *tile) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
