@@ -180,6 +180,16 @@ template <class T> __device__ inline void activate(const int activation, const f
     *slope = s * (1.0f + g * (1.0f - s) * inner);
 }
 
+// h of both products; with ReLU what is kept of them where the gate is closed is 0 too.
+template <class T> __device__ inline float gated(const int activation, float &g, float &u) {
+    if (activation != BT_ACT_RELU) return activate<T>(activation, g) * u;
+    const bool closed = g <= 0.0f;
+    const float h = closed ? 0.0f : g * u;
+    g = closed ? 0.0f : g;
+    u = closed ? 0.0f : u;
+    return h;
+}
+
 template <class T> __device__ inline void store4(T *p, const int64_t left, const float (&x)[4]) {
     if (left >= 4) {
         if constexpr (sizeof(T) == 4) store_vec(p, 4, pack<T>(x));
@@ -218,6 +228,8 @@ struct GatedJob {
     uint64_t pitch;                  // of all outputs
     uint32_t m, n, k;                // rows and columns of the output (of each), and the summed index (of each sum)
     uint32_t tiles_n, tiles_m;       // of each output
+    uint32_t splits;                 // parts of the summed index, each of other workgroups
+    float *parts;                    // their sums, [splits, 2 of the forward pass and the weights' gradients, m, n]; with one split NULL
     int activation;
 };
 
@@ -227,14 +239,17 @@ template <class T, Product K> constexpr Order kOrderQ = K == kGradW ? kAcross : 
 // Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn, each of which has an L2 of its own: an XCD's are neighbours, in bands
 // of four rows of tiles, so that those that run at once share what they read.
 struct Place {
-    uint32_t m, n, part;
+    uint32_t m, n, part, split;
 };
 
 template <Product K> __device__ inline Place place_of(const GatedJob &a, const uint32_t tile_m, const uint32_t tile_n) {
     constexpr uint32_t kXcds = 8, kBand = 4;
     const uint32_t total = gridDim.x, xcd = blockIdx.x % kXcds, more = total % kXcds;
     uint32_t tile = xcd * (total / kXcds) + (xcd < more ? xcd : more) + blockIdx.x / kXcds;
+    const uint32_t a_split = a.tiles_m * a.tiles_n * (K == kGradW ? 2 : 1);
     Place at;
+    at.split = tile / a_split;
+    tile -= at.split * a_split;
     at.part = K == kGradW ? tile / (a.tiles_m * a.tiles_n) : 0;
     tile -= at.part * a.tiles_m * a.tiles_n;
     const uint32_t band = tile / (kBand * a.tiles_n), left = a.tiles_m - band * kBand, high = left < kBand ? left : kBand;
@@ -246,8 +261,9 @@ template <Product K> __device__ inline Place place_of(const GatedJob &a, const u
 
 // What becomes of a wave's sums: rows from m on, FQ fragments of 16; columns from n on, FP fragments, of the forward pass half of them columns
 // of the gate's product and half the same columns of the other.
-template <class T, Product K, int FP, int FQ> __device__ inline void finish(const GatedJob &a, const acc4 (&acc)[FP][FQ], const uint32_t m, const uint32_t n, const uint32_t part) {
+template <class T, Product K, int FP, int FQ> __device__ inline void finish(const GatedJob &a, const acc4 (&acc)[FP][FQ], const uint32_t m, const uint32_t n, const Place &of) {
     const int lane = threadIdx.x % kWave;
+    float *const parts = a.parts ? a.parts + ((uint64_t)of.split * (K == kGradX ? 1 : 2) + of.part) * a.m * a.n : nullptr;
 #pragma unroll
     for (int j = 0; j < FQ; ++j) {
         const uint32_t row = m + j * 16 + lane % 16;
@@ -263,13 +279,14 @@ template <class T, Product K, int FP, int FQ> __device__ inline void finish(cons
             for (int i = 0; i < N; ++i) {
                 g[i] = acc[i / 4][j][i % 4];
                 u[i] = acc[i / 4 + FP / 2][j][i % 4];
-                if (a.activation == BT_ACT_RELU) {
-                    const bool closed = g[i] <= 0.0f;
-                    h[i] = closed ? 0.0f : g[i] * u[i];
-                    g[i] = closed ? 0.0f : g[i];
-                    u[i] = closed ? 0.0f : u[i];
-                } else h[i] = activate<T>(a.activation, g[i]) * u[i];
             }
+            if (parts) {
+                store_run<float, N>(parts + at, left, g);
+                store_run<float, N>(parts + (uint64_t)a.m * a.n + at, left, u);
+                continue;
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) h[i] = gated<T>(a.activation, g[i], u[i]);
             store_run<T, N>((T *)a.out[0] + at, left, h);
             if (a.gate) {
                 store_run<T, N>((T *)a.gate + at, left, g);
@@ -281,7 +298,9 @@ template <class T, Product K, int FP, int FQ> __device__ inline void finish(cons
                 const uint32_t col = n + i * 16 + lane / 16 * 4;
                 const int64_t left = (int64_t)a.n - col;
                 const float x[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                if (left > 0) store4((T *)a.out[part] + row * a.pitch + col, left, x);
+                if (left <= 0) continue;
+                if (parts) store4(parts + (uint64_t)row * a.n + col, left, x);
+                else store4((T *)a.out[of.part] + row * a.pitch + col, left, x);
             }
         }
     }
@@ -319,20 +338,8 @@ template <class T, Product K, class S> struct Work {
             for (int j = half * S::FQ / 2; j < (half + 1) * S::FQ / 2; ++j) acc[i][j] = btb::multiply<T>(p[parity][i], q[j], acc[i][j]);
     }
 
-    // The tiles that begin at k of the summed index through registers, and their products.
-    __device__ void staged(const GatedJob &a, const Operand &op, const Operand &oq, const Place &at, const uint32_t k, char *tile_p, char *tile_q, Sums &acc) {
-        __syncthreads();
-        {
-            Staged<T, kOrderP<T, K>, S::NP, S::FP, S::THREADS> sp;
-            sp.load(op, a.p[1], K == kForward, at.n, k);
-            sp.store(tile_p);
-        }
-        {
-            Staged<T, kOrderQ<T, K>, S::NQ, S::FQ, S::THREADS> sq;
-            sq.load(oq, oq, false, at.m, k);
-            sq.store(tile_q);
-        }
-        __syncthreads();
+    // The products of two tiles that lie in LDS, with nothing else on its way.
+    __device__ void multiply_all(Sums &acc, const char *tile_p, const char *tile_q) {
         read_p(tile_p, 0);
         read_q(tile_q, 0);
         read_q(tile_q, 1);
@@ -340,21 +347,61 @@ template <class T, Product K, class S> struct Work {
         multiply(acc, 0, 1);
     }
 
+    // Tiles through registers.
+    typedef Staged<T, kOrderP<T, K>, S::NP, S::FP, S::THREADS> ThroughP;
+    typedef Staged<T, kOrderQ<T, K>, S::NQ, S::FQ, S::THREADS> ThroughQ;
+
+    // The tiles that begin at k of the summed index, and their products.
+    __device__ void staged(const GatedJob &a, const Operand &op, const Operand &oq, const Place &at, const uint32_t k, char *tile_p, char *tile_q, Sums &acc) {
+        __syncthreads();
+        {
+            ThroughP sp;
+            sp.load(op, a.p[1], K == kForward, at.n, k);
+            sp.store(tile_p);
+        }
+        {
+            ThroughQ sq;
+            sq.load(oq, oq, false, at.m, k);
+            sq.store(tile_q);
+        }
+        __syncthreads();
+        multiply_all(acc, tile_p, tile_q);
+    }
+
     __device__ static void end(const GatedJob &a, const Sums &acc, const Place &at) {
         const int wave = threadIdx.x / kWave;
-        finish<T, K, S::FP, S::FQ>(a, acc, at.m + (wave % 2) * S::FQ * 16, at.n + (wave / 2) * (COLS / S::WP), at.part);
+        finish<T, K, S::FP, S::FQ>(a, acc, at.m + (wave % 2) * S::FQ * 16, at.n + (wave / 2) * (COLS / S::WP), at);
     }
 };
 
-// Any alignment and any size: tiles go through registers, one at a time.
-template <class T, Product K> __global__ __launch_bounds__(Middle::THREADS) void gated_any_kernel(const GatedJob a) {
-    typedef Work<T, K, Middle> W;
+// Of `count` tiles of the summed index, in order, the first of a split.
+__device__ inline uint32_t split_start(const GatedJob &a, const uint32_t split, const uint32_t count) { return (uint32_t)((uint64_t)count * split / a.splits); }
+
+// Any alignment and any size: tiles go through registers, the next one on its way to them while one is multiplied.
+template <class T, Product K> __global__ __launch_bounds__(Small::THREADS) void gated_any_kernel(const GatedJob a) {
+    typedef Work<T, K, Small> W;
     __shared__ __align__(16) char tiles[W::P::BYTES + W::Q::BYTES];
-    const Place at = place_of<K>(a, Middle::NQ, W::COLS);
+    const Place at = place_of<K>(a, Small::NQ, W::COLS);
     typename W::Sums acc = {};
     W w;
-    for (int sum = 0; sum < W::SUMS; ++sum)
-        for (uint32_t k = 0; k < a.k; k += kK<T>) w.staged(a, a.p[sum], a.q[sum + at.part], at, k, tiles, tiles + W::P::BYTES, acc);
+    const uint32_t a_sum = (a.k + kK<T> - 1) / kK<T>, last = split_start(a, at.split + 1, a_sum * W::SUMS);
+    typename W::ThroughP sp;
+    typename W::ThroughQ sq;
+    const auto load = [&](const uint32_t t) {
+        const uint32_t sum = W::SUMS == 2 && t >= a_sum ? 1 : 0, k = (t - sum * a_sum) * kK<T>;
+        sp.load(a.p[sum], a.p[1], K == kForward, at.n, k);
+        sq.load(a.q[sum + at.part], a.q[sum + at.part], false, at.m, k);
+    };
+    uint32_t t = split_start(a, at.split, a_sum * W::SUMS);
+    if (t < last) load(t);
+    while (t < last) {
+        __syncthreads();
+        sp.store(tiles);
+        sq.store(tiles + W::P::BYTES);
+        __syncthreads();
+        if (++t < last) load(t);
+        w.multiply_all(acc, tiles, tiles + W::P::BYTES);
+    }
     W::end(a, acc, at);
 }
 
@@ -444,15 +491,20 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
     const Place at = place_of<K>(a, S::NQ, W::COLS);
     typename W::Sums acc = {};
     W w;
-    const uint32_t count = a.k / kK<T>;      // whole tiles
+    const uint32_t a_sum = a.k / kK<T>;      // whole tiles
+    const uint32_t from = split_start(a, at.split, a_sum * W::SUMS), to = split_start(a, at.split + 1, a_sum * W::SUMS);
     for (int sum = 0; sum < W::SUMS; ++sum) {
         const Operand &op = a.p[sum], &oq = a.q[sum + at.part];
-        if (count != 0) {
+        const uint32_t before = sum * a_sum, behind = before + a_sum, first = from > before ? from : before, last = to < behind ? to : behind;
+        if (first < last) {
+            const uint32_t count = last - first;
             FetchP dp;
             FetchQ dq;
             if constexpr (K == kForward) dp.template start_pair<S::FP>(a.p[0], a.p[1], at.n);
             else dp.start(op, at.n);
             dq.start(oq, at.m);
+            dp.base += (first - before) * dp.advance;
+            dq.base += (first - before) * dq.advance;
             const auto tile_p = [&](const int place) { return tiles + place * PB; };
             const auto tile_q = [&](const int place) { return tiles + kPlaces * PB + place * QB; };
             const auto fetch = [&](const int place) {
@@ -498,10 +550,52 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
                 if (t + 3 < count) tile(3, t + 6 < count);
             }
         }
-        // The rest of the summed index, less than a tile, through registers.
-        if (count * kK<T> < a.k) w.staged(a, op, oq, at, count * kK<T>, tiles, tiles + kPlaces * PB, acc);
+        // The rest of the summed index, less than a tile, through registers: of the split that has the last whole tile, or the only one.
+        if (a_sum * kK<T> < a.k && (a.splits == 1 || (from < behind && behind <= to))) w.staged(a, op, oq, at, a_sum * kK<T>, tiles, tiles + kPlaces * PB, acc);
     }
     W::end(a, acc, at);
+}
+
+// The splits' sums added up, in order, and what becomes of them.  `cells` elements of each output, which has no gaps.
+template <class T, Product K> __global__ __launch_bounds__(256) void gated_join_kernel(const GatedJob a, const uint64_t cells) {
+    constexpr int E = kPer<T>, kSums = K == kGradX ? 1 : 2;
+    const uint64_t c = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * E;
+    if (c >= cells) return;
+    const int64_t left = (int64_t)(cells - c);
+    float x[kSums][E] = {};
+    for (uint32_t split = 0; split < a.splits; ++split)
+#pragma unroll
+        for (int k = 0; k < kSums; ++k)
+#pragma unroll
+            for (int e = 0; e < E; e += 4) {
+                float y[4];
+                unpack<float>(load_vec(a.parts + (split * kSums + k) * cells + c + e, left - e), y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[k][e + i] += y[i];
+            }
+    if constexpr (K == kForward) {
+        float h[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) h[e] = gated<T>(a.activation, x[0][e], x[1][e]);
+        store_vec((T *)a.out[0] + c, left, pack<T>(h));
+        if (a.gate) {
+            store_vec((T *)a.gate + c, left, pack<T>(x[0]));
+            store_vec((T *)a.up + c, left, pack<T>(x[1]));
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) store_vec((T *)a.out[k] + c, left, pack<T>(x[k]));
+    }
+}
+
+// Rows of `cols` elements, one behind the other, to rows of `pitch`, zeros behind them: where rows are to begin on 16-byte boundaries.
+template <class T> __global__ __launch_bounds__(256) void pad_kernel(const T *from, T *to, const uint32_t cols, const uint32_t pitch, const uint64_t vectors) {
+    const uint32_t a_row = pitch / kPer<T>;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < vectors; i += (uint64_t)gridDim.x * 256) {
+        const uint64_t row = i / a_row;
+        const uint32_t col = (uint32_t)(i - row * a_row) * kPer<T>;
+        store_vec(to + i * kPer<T>, kPer<T>, load_vec(from + row * cols + col, (int64_t)cols - col));
+    }
 }
 
 // dg = grad_h u act'(g) and du = grad_h act(g), rounded to the type: they are factors of the products, whose matrix instructions take them
@@ -537,7 +631,8 @@ template <class T> __global__ __launch_bounds__(256) void gated_slopes_kernel(co
 
 // ---- host ------------------------------------------------------------------------------------------------------
 
-uint64_t padded(const uint64_t f, const int width) { return (f * width + kVec - 1) / kVec * kVec / width; }
+// Elements of a row that is padded to whole tiles of the summed index.
+uint64_t padded(const uint64_t cols, const int width) { return (cols * width + kKBytes - 1) / kKBytes * kKBytes / width; }
 
 bt_status check_sizes(const uint64_t rows, const uint64_t d, const uint64_t f, const bt_dtype dtype) {
     if (width_of(dtype) == 0) return BT_ERR_DTYPE;
@@ -547,12 +642,69 @@ bt_status check_sizes(const uint64_t rows, const uint64_t d, const uint64_t f, c
 
 bool known(const bt_activation a) { return a == BT_ACT_RELU || a == BT_ACT_SILU || a == BT_ACT_GELU_TANH; }
 
-uint32_t ceil_div(const uint64_t a, const uint64_t b) { return (uint32_t)((a + b - 1) / b); }
+uint64_t ceil_div(const uint64_t a, const uint64_t b) { return (a + b - 1) / b; }
 
-template <Product K, class S> uint64_t tiles_of(GatedJob &a) {
-    a.tiles_m = ceil_div(a.m, S::NQ);
-    a.tiles_n = ceil_div(a.n, K == kForward ? S::NP / 2 : S::NP);
-    return (uint64_t)a.tiles_m * a.tiles_n * (K == kGradW ? 2 : 1);
+// How a product of m by n with a summed index of k (of each of `sums` sums) is run, by its sizes alone.
+enum Kind { kAnyKind, kSmall, kMiddle, kLarge };
+struct Plan {
+    Kind kind;
+    uint32_t splits;
+};
+
+// By a model of the time, us, whose constants are measured: what a compute unit multiplies in tiles of either size (of 5.9 TFLOP/s in 16 bits, 0.6 in
+// single precision), a tile's step when nothing else runs beside it, and for the splits a launch and their sums' way to memory and back.
+Plan plan_of(const Product product, const uint64_t m, const uint64_t n, const uint64_t k, const int width, const bool any) {
+    struct Form {
+        Kind kind;
+        int rows, cols, together;      // rows and columns of a tile, workgroups that a compute unit holds
+        double rate;
+    };
+    const bool single = width == 4;
+    static const Form forms[] = {{kSmall, 64, 64, 4, 0.45}, {kMiddle, 128, 128, 2, 0.75}, {kLarge, 256, 256, 1, 1.0}};
+    const double peak = single ? 0.6e6 : 5.9e6;                                  // operations a us of a compute unit
+    const uint64_t steps = ceil_div(k * width, kKBytes) * (product == kGradX ? 2 : 1), outputs = product == kGradX ? 1 : 2;
+    Plan best = {kSmall, 1};
+    double least = 1e300;
+    for (const Form &f : forms) {
+        if (f.kind != kSmall && any) break;
+        if (f.kind == kLarge && single) break;
+        const uint64_t tiles = ceil_div(m, f.rows) * ceil_div(n, product == kForward ? f.cols / 2 : f.cols) * (product == kGradW ? 2 : 1);
+        for (uint32_t splits = 1; splits <= 32 && (splits == 1 || (steps / splits >= 8 && tiles * splits <= 4096)); splits *= 2) {
+            const double work = 2.0 * f.rows * f.cols * (kKBytes / width) * (double)steps / splits;      // of a workgroup
+            const double a_unit = (double)ceil_div(tiles * splits, 256);
+            const double rate = single ? 0.8 : f.rate;
+            double time = a_unit * work / (peak * rate);
+            const double alone = (double)steps / splits * 0.25 * (double)ceil_div((uint64_t)a_unit, f.together);
+            if (time < alone) time = alone;
+            if (splits > 1) time += 4.0 + (double)splits * m * n * outputs * 8.0 / 4e6;
+            if (time < least) {
+                least = time;
+                best = {f.kind, splits};
+            }
+        }
+    }
+    if (any) best.kind = kAnyKind;
+    return best;
+}
+
+// Rows from which on operands whose rows do not begin on 16-byte boundaries are copied to ones that do.  (A copy is read and written once, a weight's
+// two elements for each that a product of few rows reads anyway.)
+constexpr uint64_t kPadRows = 128;
+
+bool pads(const uint64_t rows, const uint64_t d, const int width) { return d * width % kVec != 0 && rows >= kPadRows; }
+bool any_way(const uint64_t rows, const uint64_t d, const int width) { return d * width % kVec != 0 && rows < kPadRows; }
+
+uint64_t whole(const uint64_t bytes) { return (bytes + 127) / 128 * 128; }
+
+uint64_t parts_bytes(const Product product, const uint64_t m, const uint64_t n, const uint64_t k, const int width, const bool any) {
+    const uint32_t splits = plan_of(product, m, n, k, width, any).splits;
+    return splits == 1 ? 0 : whole(4 * m * n * splits * (product == kGradX ? 1 : 2));
+}
+
+template <class T> void pad(const void *from, T *to, const uint64_t rows, const uint64_t cols, const uint64_t pitch, bt_status *st, hipStream_t hs) {
+    const uint64_t vectors = rows * pitch / kPer<T>, blocks = ceil_div(vectors, 256);
+    if (*st == BT_OK)
+        *st = launch(pad_kernel<T>, dim3((unsigned)(blocks < 1u << 16 ? blocks : 1u << 16)), 256, hs, (const T *)from, to, (uint32_t)cols, (uint32_t)pitch, vectors);
 }
 
 // Rows of whole vectors on 16-byte boundaries, and a tile within 32 bits of offsets.
@@ -560,21 +712,29 @@ template <class T> bool direct(const Operand &a) {
     return !misaligned(a.p, kVec) && a.pitch % kPer<T> == 0 && a.pitch * sizeof(T) * 320 < 1u << 31;
 }
 
-template <class T, Product K> bt_status run_product(GatedJob &a, hipStream_t hs) {
+template <class T, Product K> bt_status run_product(GatedJob &a, const Plan &plan, float *parts, hipStream_t hs) {
     bool straight = direct<T>(a.p[0]) && direct<T>(a.q[0]);
     if (K != kGradW) straight = straight && direct<T>(a.p[1]);
     if (K != kForward) straight = straight && direct<T>(a.q[1]);
+    a.splits = plan.splits;
+    a.parts = plan.splits > 1 ? parts : nullptr;
     const auto go = [&](auto kernel, auto shape) {
         typedef decltype(shape) S;
-        const uint64_t tiles = tiles_of<K, S>(a);
-        if (tiles >= 1u << 23) return BT_ERR_SIZE;      // (a grid holds less than 2^32 threads)
-        return launch(kernel, dim3((unsigned)tiles), S::THREADS, hs, a);
+        const uint64_t tiles_m = ceil_div(a.m, S::NQ), tiles_n = ceil_div(a.n, K == kForward ? S::NP / 2 : S::NP);
+        const uint64_t groups = tiles_m * tiles_n * (K == kGradW ? 2 : 1) * a.splits;
+        if (groups >= 1u << 23) return BT_ERR_SIZE;      // (a grid holds less than 2^32 threads)
+        a.tiles_m = (uint32_t)tiles_m;
+        a.tiles_n = (uint32_t)tiles_n;
+        return launch(kernel, dim3((unsigned)groups), S::THREADS, hs, a);
     };
-    if (!straight) return go(gated_any_kernel<T, K>, Middle{});
-    if constexpr (sizeof(T) == 2)
-        if (tiles_of<K, Large>(a) >= 256) return go(gated_kernel<T, K, Large>, Large{});
-    if (tiles_of<K, Middle>(a) >= 256) return go(gated_kernel<T, K, Middle>, Middle{});
-    return go(gated_kernel<T, K, Small>, Small{});
+    bt_status st = BT_OK;
+    if (!straight || plan.kind == kAnyKind) st = go(gated_any_kernel<T, K>, Small{});
+    else if (plan.kind == kSmall) st = go(gated_kernel<T, K, Small>, Small{});
+    else if (plan.kind == kMiddle) st = go(gated_kernel<T, K, Middle>, Middle{});
+    else if constexpr (sizeof(T) == 2) st = go(gated_kernel<T, K, Large>, Large{});
+    if (st != BT_OK || a.splits == 1) return st;
+    const uint64_t cells = (uint64_t)a.m * a.n;
+    return launch(gated_join_kernel<T, K>, dim3((unsigned)ceil_div(cells, 256 * kPer<T>)), 256, hs, a, cells);
 }
 
 }  // namespace
@@ -586,7 +746,14 @@ extern "C" {
 
 size_t bt_gated_workspace_bytes(uint64_t rows, uint64_t d, uint64_t f, bt_dtype dtype, int backward) {
     if (check_sizes(rows, d, f, dtype) != BT_OK || rows == 0 || f == 0) return 0;
-    return backward ? (size_t)(2 * rows * padded(f, width_of(dtype)) * (uint64_t)width_of(dtype)) : 0;
+    const int w = width_of(dtype);
+    const bool copies = pads(rows, d, w), any = any_way(rows, d, w);
+    const uint64_t pitch = padded(d, w);
+    uint64_t bytes = copies ? whole(rows * pitch * w) + 2 * whole(f * pitch * w) : 0;
+    if (!backward) return (size_t)(bytes + parts_bytes(kForward, rows, f, copies ? pitch : d, w, any));
+    bytes += 2 * whole(rows * padded(f, w) * w);
+    const uint64_t x = parts_bytes(kGradX, rows, d, f, w, any), weights = parts_bytes(kGradW, f, d, rows, w, any);
+    return (size_t)(bytes + (x > weights ? x : weights));
 }
 
 bt_status bt_gated_forward(const void *d_x, const void *d_w_gate, const void *d_w_up,
@@ -606,19 +773,37 @@ bt_status bt_gated_forward(const void *d_x, const void *d_w_gate, const void *d_
     if (workspace_bytes < need) return BT_ERR_WORKSPACE;
     return with_type(dtype, [&](auto type) {
         using T = decltype(type);
+        const hipStream_t hs = (hipStream_t)stream;
+        char *ws = (char *)d_workspace;
+        const void *x = d_x, *w_gate = d_w_gate, *w_up = d_w_up;
+        uint64_t pitch = d;
+        bt_status s = BT_OK;
+        if (pads(rows, d, sizeof(T))) {
+            pitch = padded(d, sizeof(T));
+            const auto copy = [&](const void *from, const uint64_t n) {
+                T *const to = (T *)ws;
+                ws += whole(n * pitch * sizeof(T));
+                pad(from, to, n, d, pitch, &s, hs);
+                return to;
+            };
+            x = copy(d_x, rows);
+            w_gate = copy(d_w_gate, f);
+            w_up = copy(d_w_up, f);
+            if (s != BT_OK) return s;
+        }
         GatedJob a = {};
-        a.p[0] = {d_w_gate, d, (uint32_t)f, (uint32_t)d};
-        a.p[1] = {d_w_up, d, (uint32_t)f, (uint32_t)d};
-        a.q[0] = {d_x, d, (uint32_t)rows, (uint32_t)d};
+        a.p[0] = {w_gate, pitch, (uint32_t)f, (uint32_t)pitch};
+        a.p[1] = {w_up, pitch, (uint32_t)f, (uint32_t)pitch};
+        a.q[0] = {x, pitch, (uint32_t)rows, (uint32_t)pitch};
         a.out[0] = d_h;
         a.gate = d_gate;
         a.up = d_up;
         a.pitch = f;
         a.m = (uint32_t)rows;
         a.n = (uint32_t)f;
-        a.k = (uint32_t)d;
+        a.k = (uint32_t)pitch;
         a.activation = activation;
-        return run_product<T, kForward>(a, (hipStream_t)stream);
+        return run_product<T, kForward>(a, plan_of(kForward, rows, f, pitch, sizeof(T), any_way(rows, d, sizeof(T))), (float *)ws, hs);
     });
 }
 
@@ -636,12 +821,11 @@ bt_status bt_gated_backward(const void *d_grad_h, const void *d_x, const void *d
     if (misaligned(d_workspace, 128)) return BT_ERR_ALIGN;
     const hipStream_t hs = (hipStream_t)stream;
     if (d == 0 || (d_grad_x == nullptr && d_grad_w_gate == nullptr)) return BT_OK;
-    const size_t need = bt_gated_workspace_bytes(rows, d, f, dtype, 1);
     if (rows != 0 && f != 0) {
         if (d_grad_h == nullptr || d_gate == nullptr || d_up == nullptr || d_workspace == nullptr ||
             (d_grad_x && (d_w_gate == nullptr || d_w_up == nullptr)) || (d_grad_w_gate && d_x == nullptr))
             return BT_ERR_NULL;
-        if (workspace_bytes < need) return BT_ERR_WORKSPACE;
+        if (workspace_bytes < bt_gated_workspace_bytes(rows, d, f, dtype, 1)) return BT_ERR_WORKSPACE;
     }
     return with_type(dtype, [&](auto type) {
         using T = decltype(type);
@@ -651,36 +835,56 @@ bt_status bt_gated_backward(const void *d_grad_h, const void *d_x, const void *d
             if (s == BT_OK && d_grad_w_up) s = zeros<T>(d_grad_w_up, f * d, hs);
             return s;
         }
-        const uint64_t pitch = padded(f, sizeof(T)), vectors = rows * pitch / kPer<T>;
-        T *const dg = (T *)d_workspace, *const du = dg + rows * pitch;
-        const uint64_t blocks = (vectors + 255) / 256;
+        char *ws = (char *)d_workspace;
+        const auto take = [&](const uint64_t elements) {
+            T *const p = (T *)ws;
+            ws += whole(elements * sizeof(T));
+            return p;
+        };
+        const uint64_t pitch_f = padded(f, sizeof(T)), vectors = rows * pitch_f / kPer<T>, blocks = ceil_div(vectors, 256);
+        T *const dg = take(rows * pitch_f), *const du = take(rows * pitch_f);
         bt_status s = launch(gated_slopes_kernel<T>, dim3((unsigned)(blocks < 1u << 20 ? blocks : 1u << 20)), 256, hs, (const T *)d_grad_h, (const T *)d_gate,
-                             (const T *)d_up, dg, du, (uint32_t)f, (uint32_t)pitch, vectors, (int)activation);
+                             (const T *)d_up, dg, du, (uint32_t)f, (uint32_t)pitch_f, vectors, (int)activation);
+        const bool copies = pads(rows, d, sizeof(T)), any = any_way(rows, d, sizeof(T));
+        uint64_t pitch = d;
+        const void *x = d_x, *w_gate = d_w_gate, *w_up = d_w_up;
+        if (copies) {
+            pitch = padded(d, sizeof(T));
+            T *const to_x = take(rows * pitch), *const to_gate = take(f * pitch), *const to_up = take(f * pitch);
+            if (d_grad_w_gate) pad(d_x, to_x, rows, d, pitch, &s, hs);
+            if (d_grad_x) {
+                pad(d_w_gate, to_gate, f, d, pitch, &s, hs);
+                pad(d_w_up, to_up, f, d, pitch, &s, hs);
+            }
+            x = to_x;
+            w_gate = to_gate;
+            w_up = to_up;
+        }
         if (s == BT_OK && d_grad_x) {
             GatedJob a = {};
-            a.p[0] = {d_w_gate, d, (uint32_t)f, (uint32_t)d};
-            a.p[1] = {d_w_up, d, (uint32_t)f, (uint32_t)d};
-            a.q[0] = {dg, pitch, (uint32_t)rows, (uint32_t)f};
-            a.q[1] = {du, pitch, (uint32_t)rows, (uint32_t)f};
+            a.p[0] = {w_gate, pitch, (uint32_t)f, (uint32_t)d};
+            a.p[1] = {w_up, pitch, (uint32_t)f, (uint32_t)d};
+            a.q[0] = {dg, pitch_f, (uint32_t)rows, (uint32_t)f};
+            a.q[1] = {du, pitch_f, (uint32_t)rows, (uint32_t)f};
             a.out[0] = d_grad_x;
             a.pitch = d;
             a.m = (uint32_t)rows;
             a.n = (uint32_t)d;
             a.k = (uint32_t)f;
-            s = run_product<T, kGradX>(a, hs);
+            s = run_product<T, kGradX>(a, plan_of(kGradX, rows, d, f, sizeof(T), any), (float *)ws, hs);
         }
         if (s == BT_OK && d_grad_w_gate) {
             GatedJob a = {};
-            a.p[0] = {d_x, d, (uint32_t)rows, (uint32_t)d};
-            a.q[0] = {dg, pitch, (uint32_t)rows, (uint32_t)f};
-            a.q[1] = {du, pitch, (uint32_t)rows, (uint32_t)f};
+            a.p[0] = {x, pitch, (uint32_t)rows, (uint32_t)d};
+            a.q[0] = {dg, pitch_f, (uint32_t)rows, (uint32_t)f};
+            a.q[1] = {du, pitch_f, (uint32_t)rows, (uint32_t)f};
             a.out[0] = d_grad_w_gate;
             a.out[1] = d_grad_w_up;
             a.pitch = d;
             a.m = (uint32_t)f;
             a.n = (uint32_t)d;
             a.k = (uint32_t)rows;
-            s = run_product<T, kGradW>(a, hs);
+            s = run_product<T, kGradW>(a, plan_of(kGradW, f, d, rows, sizeof(T), any), (float *)ws, hs);
         }
         return s;
     });
