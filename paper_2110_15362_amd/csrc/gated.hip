@@ -556,6 +556,93 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
     W::end(a, acc, at);
 }
 
+// Few rows (tokens to answer with): the weights are read once and bound the time, so they go from memory to the registers that multiply them, as many
+// vectors at once as those hold.  A workgroup has 16 columns of h, its waves take units of 128 bytes of the summed index in turn; their sums
+// meet in LDS.  In a unit a lane holds 32 bytes in a row of each operand: which summed index belongs to which lane does not matter as long as both
+// have the same.  Any alignment.
+constexpr int kTokenWaves = 8;
+template <class T> constexpr int kUnit = 128 / (int)sizeof(T);
+
+template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) void gated_tokens_kernel(const GatedJob a) {
+    constexpr int kUnits = FQ <= 2 ? 4 : 2;      // on their way at once
+    __shared__ float sums[kTokenWaves][2][FQ][kWave][4];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / 16, t = lane % 16;
+    const uint32_t n = blockIdx.x * 16;
+    const T *p[2], *q[FQ];
+    // (Rows that are not there are others again: their results are not stored.)
+    const uint32_t row = n + t < a.n ? n + t : a.n - 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p[i] = (const T *)a.p[i].p + row * a.p[i].pitch + group * (2 * kPer<T>);
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) q[j] = (const T *)a.q[0].p + (uint64_t)((uint32_t)(j * 16 + t) < a.m ? j * 16 + t : a.m - 1) * a.q[0].pitch + group * (2 * kPer<T>);
+    acc4 acc[2][FQ] = {};
+    const uint32_t whole = a.k / kUnit<T>;
+    uint32_t unit = wave;
+    const auto take = [&](auto many) {
+        constexpr int N = decltype(many)::value;
+        raw16 w[N][2][2], x[N][FQ][2];
+#pragma unroll
+        for (int s = 0; s < N; ++s) {
+            const uint64_t k = (uint64_t)(unit + s * kTokenWaves) * kUnit<T>;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) w[s][i][h] = reinterpret_cast<const Unaligned<T> *>(p[i] + k + h * kPer<T>)->v;
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) x[s][j][h] = reinterpret_cast<const Unaligned<T> *>(q[j] + k + h * kPer<T>)->v;
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < N; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < FQ; ++j) acc[i][j] = multiply<T>(w[s][i][h], x[s][j][h], acc[i][j]);
+        unit += N * kTokenWaves;
+    };
+    while (unit + (kUnits - 1) * kTokenWaves < whole) take(std::integral_constant<int, kUnits>{});
+    while (unit < whole) take(std::integral_constant<int, 1>{});
+    if (unit == whole && whole * kUnit<T> < a.k) {      // the wave whose turn it is has the rest, less than a unit
+        const uint32_t k = whole * kUnit<T>;
+        const int64_t left = (int64_t)a.k - k - group * (2 * kPer<T>);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            raw16 w[2], x[FQ];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) w[i] = load_vec(p[i] + k + h * kPer<T>, left - h * kPer<T>);
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) x[j] = load_vec(q[j] + k + h * kPer<T>, left - h * kPer<T>);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) acc[i][j] = multiply<T>(w[i], x[j], acc[i][j]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) *(acc4 *)sums[wave][i][j][lane] = acc[i][j];
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < FQ * 256; c += kTokenWaves * kWave) {
+        const uint32_t col = c % 16, token = c / 16, from = col / 4 * 16 + token % 16, r = col % 4, j = token / 16;
+        float g = 0.0f, u = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kTokenWaves; ++w) {
+            g += sums[w][0][j][from][r];
+            u += sums[w][1][j][from][r];
+        }
+        if (token >= a.m || n + col >= a.n) continue;
+        const uint64_t at = token * a.pitch + n + col;
+        ((T *)a.out[0])[at] = narrow<T>(gated<T>(a.activation, g, u));
+        if (a.gate) {
+            ((T *)a.gate)[at] = narrow<T>(g);
+            ((T *)a.up)[at] = narrow<T>(u);
+        }
+    }
+}
+
 // The splits' sums added up, in order, and what becomes of them.  `cells` elements of each output, which has no gaps.
 template <class T, Product K> __global__ __launch_bounds__(256) void gated_join_kernel(const GatedJob a, const uint64_t cells) {
     constexpr int E = kPer<T>, kSums = K == kGradX ? 1 : 2;
@@ -687,6 +774,9 @@ Plan plan_of(const Product product, const uint64_t m, const uint64_t n, const ui
     return best;
 }
 
+// Rows of x up to which the forward pass reads the weights straight to registers.
+constexpr uint64_t kTokens = 64;
+
 // Rows from which on operands whose rows do not begin on 16-byte boundaries are copied to ones that do.  (A copy is read and written once, a weight's
 // two elements for each that a product of few rows reads anyway.)
 constexpr uint64_t kPadRows = 128;
@@ -750,6 +840,7 @@ size_t bt_gated_workspace_bytes(uint64_t rows, uint64_t d, uint64_t f, bt_dtype 
     const bool copies = pads(rows, d, w), any = any_way(rows, d, w);
     const uint64_t pitch = padded(d, w);
     uint64_t bytes = copies ? whole(rows * pitch * w) + 2 * whole(f * pitch * w) : 0;
+    if (!backward && rows <= kTokens) return 0;
     if (!backward) return (size_t)(bytes + parts_bytes(kForward, rows, f, copies ? pitch : d, w, any));
     bytes += 2 * whole(rows * padded(f, w) * w);
     const uint64_t x = parts_bytes(kGradX, rows, d, f, w, any), weights = parts_bytes(kGradW, f, d, rows, w, any);
@@ -803,6 +894,11 @@ bt_status bt_gated_forward(const void *d_x, const void *d_w_gate, const void *d_
         a.n = (uint32_t)f;
         a.k = (uint32_t)pitch;
         a.activation = activation;
+        if (rows <= kTokens) {
+            const dim3 grid((unsigned)ceil_div(f, 16));
+            const auto go = [&](auto kernel) { return launch(kernel, grid, kTokenWaves * kWave, hs, a); };
+            return rows <= 16 ? go(gated_tokens_kernel<T, 1>) : rows <= 32 ? go(gated_tokens_kernel<T, 2>) : rows <= 48 ? go(gated_tokens_kernel<T, 3>) : go(gated_tokens_kernel<T, 4>);
+        }
         return run_product<T, kForward>(a, plan_of(kForward, rows, f, pitch, sizeof(T), any_way(rows, d, sizeof(T))), (float *)ws, hs);
     });
 }
