@@ -408,12 +408,13 @@ template <class T, Product K> __global__ __launch_bounds__(Small::THREADS) void 
 // An operand's tiles straight from memory to LDS, 1 KiB an instruction of a wave, an equal part of the tile a wave.  Needs rows of whole vectors on
 // 16-byte boundaries.  What a tile has beyond the operand's rows (or, where the summed index lies across, columns) is read from inside of it: it
 // belongs to rows or columns of the product that are not stored.
-template <class T, Order O, int N, int WAVES> struct Direct {
+template <class T, Order O, int N, int WAVES, bool ROUND> struct Direct {
     typedef Tile<T, O, N> L;
     static constexpr int S = (int)sizeof(T), PER = N / 16 / WAVES;
     uint32_t offset[PER];        // of the lane's vector in each instruction's KiB, from the tile's first
     const char *base;
-    uint64_t advance;            // bytes from one tile to the next
+    uint64_t advance, round;     // bytes from one tile to the next; of all tiles
+    uint32_t ahead;              // tiles before the first one is next
 
     // `n`: the product's row or column that the tile begins at.  F: of the forward pass, whose weights' rows are those of `n` on in another order.
     template <int F = 0> __device__ void start(const Operand &a, const uint32_t n) {
@@ -444,6 +445,13 @@ template <class T, Order O, int N, int WAVES> struct Direct {
 #pragma unroll
         for (int i = 0; i < PER; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (BT_LDS void *)(tile + (wave * PER + i) * 1024), 16, (int)offset[i], 0, 0, 0);
         base += advance;
+        if (ROUND && --ahead == 0) base -= round;
+    }
+    // Begin at tile `at` of the `count` from `first` on; with ROUND the tiles before it come last.
+    __device__ void rotate(const uint32_t first, const uint32_t at, const uint32_t count) {
+        base += (uint64_t)(first + at) * advance;
+        ahead = count - at;
+        round = (uint64_t)count * advance;
     }
 };
 
@@ -482,8 +490,12 @@ template <int READS, int FETCHES, int PRODUCTS> __device__ inline void spread() 
 
 template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, S::THREADS >= 512 ? 2 : 1) void gated_kernel(const GatedJob a) {
     typedef Work<T, K, S> W;
-    typedef Direct<T, kOrderP<T, K>, S::NP, S::WAVES> FetchP;
-    typedef Direct<T, kOrderQ<T, K>, S::NQ, S::WAVES> FetchQ;
+    // Rows of a power of two of bytes all begin in the same channel of the memory, and workgroups in step would ask one after the other: each XCD
+    // begins elsewhere in the summed index (us: forward [16384, 2048] x 8192 1045 -> 970, grad_x 915 -> 885), or with few rows each of 64
+    // workgroups.  The weights' gradients sum over rows, and have no registers for it.
+    constexpr bool kRound = K != kGradW;
+    typedef Direct<T, kOrderP<T, K>, S::NP, S::WAVES, kRound> FetchP;
+    typedef Direct<T, kOrderQ<T, K>, S::NQ, S::WAVES, kRound> FetchQ;
     constexpr int PB = W::P::BYTES, QB = W::Q::BYTES, kFetches = FetchP::PER + FetchQ::PER;
     constexpr int kReadsP = S::FP * Reader<T, kOrderP<T, K>, S::NP, S::FP>::READS, kReadsQ = S::FQ / 2 * Reader<T, kOrderQ<T, K>, S::NQ, S::FQ>::READS;
     constexpr int kProducts = S::FP * S::FQ / 2 * (sizeof(T) == 4 ? 4 : 1);
@@ -492,6 +504,7 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
     typename W::Sums acc = {};
     W w;
     const uint32_t a_sum = a.k / kK<T>;      // whole tiles
+    const uint32_t phases = a.tiles_m == 1 ? 64 : 8;
     const uint32_t from = split_start(a, at.split, a_sum * W::SUMS), to = split_start(a, at.split + 1, a_sum * W::SUMS);
     for (int sum = 0; sum < W::SUMS; ++sum) {
         const Operand &op = a.p[sum], &oq = a.q[sum + at.part];
@@ -503,8 +516,9 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
             if constexpr (K == kForward) dp.template start_pair<S::FP>(a.p[0], a.p[1], at.n);
             else dp.start(op, at.n);
             dq.start(oq, at.m);
-            dp.base += (first - before) * dp.advance;
-            dq.base += (first - before) * dq.advance;
+            const uint32_t phase = kRound ? (uint32_t)((uint64_t)(blockIdx.x % phases) * count / phases) : 0;
+            dp.rotate(first - before, phase, count);
+            dq.rotate(first - before, phase, count);
             const auto tile_p = [&](const int place) { return tiles + place * PB; };
             const auto tile_q = [&](const int place) { return tiles + kPlaces * PB + place * QB; };
             const auto fetch = [&](const int place) {
@@ -559,31 +573,36 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
 // Few rows (tokens to answer with): the weights are read once and bound the time, so they go from memory to the registers that multiply them, as many
 // vectors at once as those hold.  A workgroup has 16 columns of h, its waves take units of 128 bytes of the summed index in turn; their sums
 // meet in LDS.  In a unit a lane holds 32 bytes in a row of each operand: which summed index belongs to which lane does not matter as long as both
-// have the same.  Any alignment.
+// have the same.  Any alignment.  (bf16, weights of [4096, 1024], 1 row: 4.9 us, 3.4 TB/s; of [16384, 4096], 52.8 us, 5.1 TB/s; of [11008, 4096], 16 rows:
+// 42 us, 4.3 TB/s.  32 columns a workgroup, which read x half as often: 59 and 63.  From 33 rows on tiles in LDS are faster.)
 constexpr int kTokenWaves = 8;
 template <class T> constexpr int kUnit = 128 / (int)sizeof(T);
 
 template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) void gated_tokens_kernel(const GatedJob a) {
-    constexpr int kUnits = FQ <= 2 ? 4 : 2;      // on their way at once
+    constexpr int kUnits = 4;      // on their way at once
     __shared__ float sums[kTokenWaves][2][FQ][kWave][4];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / 16, t = lane % 16;
     const uint32_t n = blockIdx.x * 16;
     const T *p[2], *q[FQ];
     // (Rows that are not there are others again: their results are not stored.)
-    const uint32_t row = n + t < a.n ? n + t : a.n - 1;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) p[i] = (const T *)a.p[i].p + row * a.p[i].pitch + group * (2 * kPer<T>);
+    for (int i = 0; i < 2; ++i) {
+        p[i] = (const T *)a.p[i].p + (n + t < a.n ? n + t : a.n - 1) * a.p[i].pitch + group * (2 * kPer<T>);
+    }
 #pragma unroll
     for (int j = 0; j < FQ; ++j) q[j] = (const T *)a.q[0].p + (uint64_t)((uint32_t)(j * 16 + t) < a.m ? j * 16 + t : a.m - 1) * a.q[0].pitch + group * (2 * kPer<T>);
     acc4 acc[2][FQ] = {};
-    const uint32_t whole = a.k / kUnit<T>;
+    // The workgroups begin in different places of the summed index, or all would ask the same channels of the memory at a time.
+    const uint32_t whole = a.k / kUnit<T>, shift = whole == 0 ? 0 : blockIdx.x * kTokenWaves % whole;
     uint32_t unit = wave;
     const auto take = [&](auto many) {
         constexpr int N = decltype(many)::value;
         raw16 w[N][2][2], x[N][FQ][2];
 #pragma unroll
         for (int s = 0; s < N; ++s) {
-            const uint64_t k = (uint64_t)(unit + s * kTokenWaves) * kUnit<T>;
+            uint32_t at = unit + s * kTokenWaves + shift;
+            if (at >= whole) at -= whole;
+            const uint64_t k = (uint64_t)at * kUnit<T>;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -592,6 +611,7 @@ template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) voi
                 for (int j = 0; j < FQ; ++j) x[s][j][h] = reinterpret_cast<const Unaligned<T> *>(q[j] + k + h * kPer<T>)->v;
             }
         }
+        __builtin_amdgcn_sched_barrier(0);      // (all of them before the first product)
 #pragma unroll
         for (int s = 0; s < N; ++s)
 #pragma unroll
@@ -604,7 +624,7 @@ template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) voi
     };
     while (unit + (kUnits - 1) * kTokenWaves < whole) take(std::integral_constant<int, kUnits>{});
     while (unit < whole) take(std::integral_constant<int, 1>{});
-    if (unit == whole && whole * kUnit<T> < a.k) {      // the wave whose turn it is has the rest, less than a unit
+    if (wave == 0 && whole * kUnit<T> < a.k) {      // the rest, less than a unit
         const uint32_t k = whole * kUnit<T>;
         const int64_t left = (int64_t)a.k - k - group * (2 * kPer<T>);
 #pragma unroll
@@ -775,7 +795,7 @@ Plan plan_of(const Product product, const uint64_t m, const uint64_t n, const ui
 }
 
 // Rows of x up to which the forward pass reads the weights straight to registers.
-constexpr uint64_t kTokens = 64;
+constexpr uint64_t kTokens = 32;
 
 // Rows from which on operands whose rows do not begin on 16-byte boundaries are copied to ones that do.  (A copy is read and written once, a weight's
 // two elements for each that a product of few rows reads anyway.)
@@ -897,7 +917,7 @@ bt_status bt_gated_forward(const void *d_x, const void *d_w_gate, const void *d_
         if (rows <= kTokens) {
             const dim3 grid((unsigned)ceil_div(f, 16));
             const auto go = [&](auto kernel) { return launch(kernel, grid, kTokenWaves * kWave, hs, a); };
-            return rows <= 16 ? go(gated_tokens_kernel<T, 1>) : rows <= 32 ? go(gated_tokens_kernel<T, 2>) : rows <= 48 ? go(gated_tokens_kernel<T, 3>) : go(gated_tokens_kernel<T, 4>);
+            return rows <= 16 ? go(gated_tokens_kernel<T, 1>) : go(gated_tokens_kernel<T, 2>);
         }
         return run_product<T, kForward>(a, plan_of(kForward, rows, f, pitch, sizeof(T), any_way(rows, d, sizeof(T))), (float *)ws, hs);
     });
