@@ -72,11 +72,22 @@ template <class T> __device__ inline raw16 pack(const float (&x)[kPer<T>]) {
     return v;
 }
 
-// Elements [0, left) of the vector at p, zeros behind them.
-template <class T> __device__ inline raw16 load_vec(const T *p, const int64_t left) {
+// Elements [0, left) of the vector at p, zeros behind them.  A vector that ends beyond its row is read from further in front, where the row has
+// `before` elements, and moved: one load instead of one an element.
+template <class T> __device__ inline raw16 load_vec(const T *p, const int left, const int before) {
     if (left >= kPer<T>) return reinterpret_cast<const Unaligned<T> *>(p)->v;
     raw16 v = {0, 0, 0, 0};
     if (left <= 0) return v;
+    if (left + before >= kPer<T>) {
+        typedef uint64_t two __attribute__((ext_vector_type(2)));
+        raw16 bits = reinterpret_cast<const Unaligned<T> *>(p + left - kPer<T>)->v;
+        // (Or the compiler makes one load of this and the one above, and waves without such a vector wait for theirs to be moved by nothing.)
+        asm volatile("" : "+v"(bits));
+        const two x = __builtin_bit_cast(two, bits);
+        const uint32_t shift = (uint32_t)(kPer<T> - left) * (8 * sizeof(T));      // 0 < shift < 128
+        const uint64_t low = x[0], high = x[1];
+        return __builtin_bit_cast(raw16, shift >= 64 ? two{high >> (shift - 64), 0} : two{low >> shift | high << (64 - shift), high >> shift});
+    }
 #pragma unroll
     for (int i = 0; i < kPer<T>; ++i)
         if (i < left) {
@@ -86,17 +97,28 @@ template <class T> __device__ inline raw16 load_vec(const T *p, const int64_t le
     return v;
 }
 
-template <class T> __device__ inline void store_vec(T *p, const int64_t left, const raw16 v) {
+// Elements [0, left) of v; of a part of a vector its halves, quarters and single elements.
+template <class T> __device__ inline void store_vec(T *p, const int left, const raw16 v) {
+    struct __attribute__((packed, aligned(sizeof(T)))) Eight { uint64_t v; };
+    struct __attribute__((packed, aligned(sizeof(T)))) Four { uint32_t v; };
     if (left >= kPer<T>) {
         reinterpret_cast<Unaligned<T> *>(p)->v = v;
         return;
     }
-#pragma unroll
-    for (int i = 0; i < kPer<T>; ++i)
-        if (i < left) {
-            if constexpr (sizeof(T) == 4) p[i] = __builtin_bit_cast(float, (uint32_t)v[i]);
-            else p[i] = __builtin_bit_cast(T, (uint16_t)(v[i / 2] >> (16 * (i & 1))));
-        }
+    if (left <= 0) return;
+    uint64_t x = (uint64_t)v[1] << 32 | v[0];
+    if (left & (8 / sizeof(T))) {
+        reinterpret_cast<Eight *>(p)->v = x;
+        p += 8 / sizeof(T);
+        x = (uint64_t)v[3] << 32 | v[2];
+    }
+    if (left & (4 / sizeof(T))) {
+        reinterpret_cast<Four *>(p)->v = (uint32_t)x;
+        p += 4 / sizeof(T);
+        x >>= 32;
+    }
+    if constexpr (sizeof(T) == 2)
+        if (left & 1) *p = __builtin_bit_cast(T, (uint16_t)x);
 }
 
 template <class T> static __global__ __launch_bounds__(256) void zero_kernel(T *p, const uint64_t n) {

@@ -56,14 +56,14 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_forward_kernel(const
     const uint32_t row = a.first_row + blockIdx.x * kRowsABlock<NT> + threadIdx.x / NT;
     if (row >= a.rows) return;
     const uint64_t at = (uint64_t)row * a.cols;
-    const int64_t cols = a.cols;
+    const int cols = (int)a.cols;
     const float inverse = 1.0f / (float)a.cols;
     raw16 x[V], b[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int64_t c = (int64_t)(i * NT + t) * E;
-        x[i] = load_vec((const T *)a.x + at + c, cols - c);
-        if (a.block) b[i] = load_vec((const T *)a.block + at + c, cols - c);
+        const int c = (i * NT + t) * E;
+        x[i] = load_vec((const T *)a.x + at + c, cols - c, c);
+        if (a.block) b[i] = load_vec((const T *)a.block + at + c, cols - c, c);
     }
     float rb = 1.0f;
     if (a.post_weight) {
@@ -81,18 +81,18 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_forward_kernel(const
     const uint64_t gate_at = a.gate ? (uint64_t)(row / a.rows_a_gate) * a.cols : 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int64_t c = (int64_t)(i * NT + t) * E;
+        const int c = (i * NT + t) * E;
         unpack<T>(x[i], out[i]);
         if (a.block) {
             float f[E], w[E];
             unpack<T>(b[i], f);
             if (a.post_weight) {
-                unpack<T>(load_vec((const T *)a.post_weight + c, cols - c), w);
+                unpack<T>(load_vec((const T *)a.post_weight + c, cols - c, c), w);
 #pragma unroll
                 for (int e = 0; e < E; ++e) f[e] = f[e] * rb * w[e];
             }
             if (a.gate) {
-                unpack<T>(load_vec((const T *)a.gate + gate_at + c, cols - c), w);
+                unpack<T>(load_vec((const T *)a.gate + gate_at + c, cols - c, c), w);
 #pragma unroll
                 for (int e = 0; e < E; ++e) f[e] *= w[e];
             }
@@ -108,10 +108,10 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_forward_kernel(const
         ro = 1.0f / sqrtf(row_sum<NT>(sum, room[1]) * inverse + a.eps);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int64_t c = (int64_t)(i * NT + t) * E;
+            const int c = (i * NT + t) * E;
             if (c >= cols) continue;
             float w[E];
-            unpack<T>(load_vec((const T *)a.pre_weight + c, cols - c), w);
+            unpack<T>(load_vec((const T *)a.pre_weight + c, cols - c, c), w);
 #pragma unroll
             for (int e = 0; e < E; ++e) w[e] *= out[i][e] * ro;
             store_vec((T *)a.y + at + c, cols - c, pack<T>(w));
@@ -138,6 +138,12 @@ struct NormBackward {
     float scale, residual_scale;
 };
 
+// `p`, which the compiler takes for another one each time: what is read there is read again, not held in registers.
+template <class T> __device__ inline const T *again(const T *p) {
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
 __device__ __host__ inline uint32_t run_start(const uint32_t run, const uint32_t rows, const uint32_t runs) {
     return (uint32_t)((uint64_t)run * rows / runs);
 }
@@ -148,10 +154,13 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormBackward a)
     // 16 columns a thread of a full workgroup: three sums of each are more than its registers hold beside the row, so two of them are kept in LDS
     // (128 of 160 KiB; 256 KiB of LDS traffic a row of 16384, a tenth of the time that the row takes from memory).
     constexpr bool kWide = V * E > 8;
+    // Workgroups of up to 512 threads have registers for two rows and for what all rows share; of 1024, half as many a thread, for one row's
+    // sums; where two of those are in LDS a row's vectors are read again (from the caches) rather than held.
+    constexpr bool kAhead = NT <= 512;
     __shared__ float room[2][NT / kWave];
     __shared__ float kept[kWide ? 2 : 1][kWide ? V * E : 1][kWide ? NT : 1];
     const int t = threadIdx.x;
-    const int64_t cols = a.cols;
+    const int cols = (int)a.cols;
     const float inverse = 1.0f / (float)a.cols;
     const uint32_t first = run_start(blockIdx.x, a.rows, a.runs), end = run_start(blockIdx.x + 1, a.rows, a.runs);
     float sum_post[kWide ? 1 : V][E], sum_pre[kWide ? 1 : V][E], sum_gate[V][E];
@@ -178,28 +187,70 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormBackward a)
         group_first = group * a.rows_a_gate;
         group_end = group_first + a.rows_a_gate;
     }
+    // Wide rows: what follows from the thread's number is worked out again each time, or it would take the registers that hold the row.
+    const auto number = [&] {
+        int n = t;
+        if (kWide) asm volatile("" : "+v"(n));
+        return n;
+    };
+    // A row's vectors: with kAhead the next row's are on their way while one is worked on.
+    struct Row {
+        raw16 gy[V], o[V], go[V], b[V];
+        float rb, ro;
+    };
+    const auto load = [&](Row &r, const uint32_t row) {
+        const uint64_t at = (uint64_t)row * a.cols;
+        r.rb = a.block ? a.stats[row] : 1.0f;
+        r.ro = a.grad_y ? a.stats[(uint64_t)a.rows + row] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int c = (i * NT + number()) * E;
+            if (a.grad_y) {
+                r.gy[i] = load_vec((const T *)a.grad_y + at + c, cols - c, c);
+                r.o[i] = load_vec((const T *)a.out + at + c, cols - c, c);
+            }
+            if (!kAhead) continue;
+            if (a.grad_out) r.go[i] = load_vec((const T *)a.grad_out + at + c, cols - c, c);
+            if (a.block) r.b[i] = load_vec((const T *)a.block + at + c, cols - c, c);
+        }
+    };
+    // What all rows share, or a group's do.
+    raw16 wn[V], wp[V], gate[V];
+    const auto load_gate = [&] {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int c = (i * NT + t) * E;
+            if (kAhead && a.gate) gate[i] = load_vec((const T *)a.gate + (uint64_t)group * a.cols + c, cols - c, c);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int c = (i * NT + t) * E;
+        if (kAhead && a.pre_weight) wn[i] = load_vec((const T *)a.pre_weight + c, cols - c, c);
+        if (kAhead && a.post_weight) wp[i] = load_vec((const T *)a.post_weight + c, cols - c, c);
+    }
+    load_gate();
+    Row next;
+    if (kAhead) load(next, first);
     for (uint32_t row = first; row < end; ++row) {
         const uint64_t at = (uint64_t)row * a.cols;
-        const float rb = a.block ? a.stats[row] : 1.0f, ro = a.grad_y ? a.stats[(uint64_t)a.rows + row] : 1.0f;
+        Row r;
+        if constexpr (kAhead) {
+            r = next;
+            if (row + 1 < end) load(next, row + 1);
+        } else load(r, row);
         float total[V][E], mean = 0.0f;
         if (a.grad_y) {
-            raw16 gy[V], o[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const int64_t c = (int64_t)(i * NT + t) * E;
-                gy[i] = load_vec((const T *)a.grad_y + at + c, cols - c);
-                o[i] = load_vec((const T *)a.out + at + c, cols - c);
-            }
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int64_t c = (int64_t)(i * NT + t) * E;
+                const int c = (i * NT + number()) * E;
                 float g[E], v[E], w[E];
-                unpack<T>(gy[i], g);
-                unpack<T>(o[i], v);
-                unpack<T>(load_vec((const T *)a.pre_weight + c, cols - c), w);
+                unpack<T>(r.gy[i], g);
+                unpack<T>(r.o[i], v);
+                unpack<T>(!kAhead ? load_vec(again((const T *)a.pre_weight) + c, cols - c, c) : wn[i], w);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    v[e] *= ro;
+                    v[e] *= r.ro;
                     add_pre(i, e, g[e], v[e]);
                     mean = fmaf(g[e] * w[e], v[e], mean);
                 }
@@ -207,13 +258,13 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormBackward a)
             mean = row_sum<NT>(mean, room[0]) * inverse;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const int64_t c = (int64_t)(i * NT + t) * E;
+                const int c = (i * NT + number()) * E;
                 float g[E], v[E], w[E];
-                unpack<T>(gy[i], g);
-                unpack<T>(o[i], v);
-                unpack<T>(load_vec((const T *)a.pre_weight + c, cols - c), w);
+                unpack<T>(kWide ? load_vec((const T *)a.grad_y + at + c, cols - c, c) : r.gy[i], g);
+                unpack<T>(kWide ? load_vec((const T *)a.out + at + c, cols - c, c) : r.o[i], v);
+                unpack<T>(!kAhead ? load_vec(again((const T *)a.pre_weight) + c, cols - c, c) : wn[i], w);
 #pragma unroll
-                for (int e = 0; e < E; ++e) total[i][e] = ro * (g[e] * w[e] - v[e] * ro * mean);
+                for (int e = 0; e < E; ++e) total[i][e] = r.ro * (g[e] * w[e] - v[e] * r.ro * mean);
             }
         } else {
 #pragma unroll
@@ -223,10 +274,10 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormBackward a)
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int64_t c = (int64_t)(i * NT + t) * E;
+            const int c = (i * NT + number()) * E;
             if (a.grad_out) {
                 float g[E];
-                unpack<T>(load_vec((const T *)a.grad_out + at + c, cols - c), g);
+                unpack<T>(!kAhead ? load_vec((const T *)a.grad_out + at + c, cols - c, c) : r.go[i], g);
 #pragma unroll
                 for (int e = 0; e < E; ++e) total[i][e] += g[e];
             }
@@ -245,27 +296,29 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormBackward a)
             ++group;
             group_first = group_end;
             group_end += a.rows_a_gate;
+            load_gate();
         }
         const bool last_of_group = row + 1 == group_end || row + 1 == end;
-        float z[V][E];
+        float kept_z[kWide ? 1 : V][E];
         mean = 0.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int64_t c = (int64_t)(i * NT + t) * E;
+            const int c = (i * NT + number()) * E;
             float w[E];
-            unpack<T>(load_vec((const T *)a.block + at + c, cols - c), z[i]);
+            float (&z)[E] = kept_z[kWide ? 0 : i];
+            unpack<T>(!kAhead ? load_vec((const T *)a.block + at + c, cols - c, c) : r.b[i], z);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                z[i][e] *= rb;
+                z[e] *= r.rb;
                 w[e] = 1.0f;
                 total[i][e] *= a.scale;
             }
-            if (a.post_weight) unpack<T>(load_vec((const T *)a.post_weight + c, cols - c), w);
+            if (a.post_weight) unpack<T>(!kAhead ? load_vec(again((const T *)a.post_weight) + c, cols - c, c) : wp[i], w);
             if (a.gate) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) sum_gate[i][e] = fmaf(total[i][e], z[i][e] * w[e], sum_gate[i][e]);
+                for (int e = 0; e < E; ++e) sum_gate[i][e] = fmaf(total[i][e], z[e] * w[e], sum_gate[i][e]);
                 float g[E];
-                unpack<T>(load_vec((const T *)a.gate + (uint64_t)group * a.cols + c, cols - c), g);
+                unpack<T>(!kAhead ? load_vec(again((const T *)a.gate) + (uint64_t)group * a.cols + c, cols - c, c) : gate[i], g);
 #pragma unroll
                 for (int e = 0; e < E; ++e) total[i][e] *= g[e];
                 if (last_of_group && a.grad_gate && c < cols) {
@@ -286,23 +339,31 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormBackward a)
             if (a.post_weight) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    add_post(i, e, total[i][e], z[i][e]);
+                    add_post(i, e, total[i][e], z[e]);
                     total[i][e] *= w[e];
-                    mean = fmaf(total[i][e], z[i][e], mean);
+                    mean = fmaf(total[i][e], z[e], mean);
                 }
             }
         }
         if (a.post_weight) {
             mean = row_sum<NT>(mean, room[1]) * inverse;
 #pragma unroll
-            for (int i = 0; i < V; ++i)
+            for (int i = 0; i < V; ++i) {
+                float (&z)[E] = kept_z[kWide ? 0 : i];
+                if (kWide) {
+                    const int c = (i * NT + number()) * E;
+                    unpack<T>(load_vec((const T *)a.block + at + c, cols - c, c), z);
 #pragma unroll
-                for (int e = 0; e < E; ++e) total[i][e] = rb * (total[i][e] - z[i][e] * mean);
+                    for (int e = 0; e < E; ++e) z[e] *= r.rb;
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) total[i][e] = r.rb * (total[i][e] - z[e] * mean);
+            }
         }
         if (a.grad_block)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const int64_t c = (int64_t)(i * NT + t) * E;
+                const int c = (i * NT + number()) * E;
                 if (c < cols) store_vec((T *)a.grad_block + at + c, cols - c, pack<T>(total[i]));
             }
         // (Where a row uses both rooms, each is read before its threads come to the barrier of the other.)
@@ -311,7 +372,7 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormBackward a)
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int64_t c = (int64_t)(i * NT + t) * E;
+        const int c = (i * NT + t) * E;
 #pragma unroll
         for (int e = 0; e < E; ++e)
             if (c + e < cols) {
@@ -334,35 +395,40 @@ template <class T> __global__ __launch_bounds__(kJoinWaves * kWave) void norm_jo
     T *result = (T *)(blockIdx.y == 0 ? a.grad_post_weight : a.grad_pre_weight);
     uint64_t pitch = a.cols;
     if (blockIdx.y >= 2) {
-        // The group, and the first run that has rows of it from the run before on.  Up to `runs` groups are looked at one by one, of more
-        // only those that a run begins inside of.
+        // The group, and the first run that begins behind its first row.  (A run begins at floor(run * rows / runs), at or behind row r from run
+        // ceil(r * runs / rows) on.)  Up to `runs` groups are looked at one by one, of more only those that a run begins inside of.
+        const auto run_from = [&](const uint32_t row) { return (uint32_t)(((uint64_t)row * a.runs + a.rows - 1) / a.rows); };
         uint32_t group = blockIdx.y - 2, run = blockIdx.y - 1;
-        if (a.gate_rows <= a.runs) {
-            const uint32_t first = group * a.rows_a_gate;
-            run = (uint32_t)((uint64_t)first * a.runs / a.rows) + 1;
-            while (run_start(run, a.rows, a.runs) <= first) ++run;
-            while (run > 1 && run_start(run - 1, a.rows, a.runs) > first) --run;
-        } else {
-            group = run_start(run, a.rows, a.runs) / a.rows_a_gate;
-        }
+        if (a.gate_rows <= a.runs) run = run_from(group * a.rows_a_gate + 1);
+        else group = run_start(run, a.rows, a.runs) / a.rows_a_gate;
         const uint32_t first = group * a.rows_a_gate, end = first + a.rows_a_gate;
         if (run >= a.runs || run_start(run, a.rows, a.runs) >= end) return;                  // within one run, which has written it
         if (run_start(run, a.rows, a.runs) == first || run_start(run - 1, a.rows, a.runs) > first) return;      // another workgroup's
         from = run - 1;
-        to = run + 1;
-        while (to < a.runs && run_start(to, a.rows, a.runs) < end) ++to;
+        to = run_from(end);
         parts = a.part_gate;
         pitch = 2 * (uint64_t)a.cols;
         result = a.grad_gate ? (T *)a.grad_gate + (uint64_t)group * a.cols : nullptr;
     }
     if (result == nullptr) return;
     float sum = 0.0f;
-    if (c < a.cols)
-        for (uint32_t run = from + wave; run < to; run += kJoinWaves) {
-            // a gate row's part lies in the second place of the run that it begins in, in the first of the others
-            const uint64_t place = blockIdx.y >= 2 && run == from ? a.cols : 0;
-            sum += parts[run * pitch + place + c];
+    if (c < a.cols) {
+        // (A gate row's part lies in the second place of the run that it begins in, in the first of the others.)
+        uint32_t run = from + wave;
+        if (blockIdx.y >= 2 && wave == 0) {
+            sum = parts[run * pitch + a.cols + c];
+            run += kJoinWaves;
         }
+        constexpr int kAtOnce = 8;
+        for (; run + (kAtOnce - 1) * kJoinWaves < to; run += kAtOnce * kJoinWaves) {
+            float x[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) x[i] = parts[(run + i * kJoinWaves) * pitch + c];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) sum += x[i];
+        }
+        for (; run < to; run += kJoinWaves) sum += parts[run * pitch + c];
+    }
     part[wave][lane] = sum;
     __syncthreads();
     if (wave == 0 && c < a.cols) {
@@ -377,7 +443,7 @@ template <class T> __global__ __launch_bounds__(kJoinWaves * kWave) void norm_jo
 // Up to kTable tensors a launch, laid end to end in chunks of 32 KiB.  The workgroups of a launch take the chunks in turn and leave one
 // partial sum each, in 64 bits: squares of any float fit them, so there is no range to mind.
 
-constexpr int kTable = 128;
+constexpr int kTable = 168;
 constexpr int kChunk = 32768;                  // bytes
 constexpr int kClipThreads = 256;
 constexpr int kClipVecs = kChunk / kVec / kClipThreads;
@@ -387,49 +453,57 @@ constexpr uint32_t kScalers = 2048;            // workgroups of a launch that sc
 struct ClipTable {
     const void *in[kTable];
     void *out[kTable];
-    uint64_t n[kTable];
-    uint32_t start[kTable];                    // first chunk; the chunks of all tensors from a tensor that is not there on
-    uint8_t dtype[kTable];
+    uint32_t start[kTable];                    // first chunk; of a tensor that is not there more than there are
+    uint32_t last[kTable];                     // elements of the last chunk, and the type in the two highest bits
     uint32_t chunks;
 };
-static_assert(sizeof(ClipTable) <= 3840, "kernel arguments");
+static_assert(sizeof(ClipTable) + 5 * 8 <= 4096, "kernel arguments");
 
 struct Piece {
     const void *in;
     void *out;
-    uint64_t left;                             // elements from the piece's first on
     uint64_t first;
+    uint32_t left;                             // elements of the piece
     int dtype;
 };
 
 __device__ inline Piece piece_of(const ClipTable &a, const uint32_t chunk) {
-    // the last tensor that starts at or before the chunk (empty ones start where the next one does)
-    static_assert(kTable == 2 * kWave);
+    // the last tensor that starts at or before the chunk
     const int lane = threadIdx.x % kWave;
-    const int i = __popcll(__ballot(a.start[lane] <= chunk)) + __popcll(__ballot(a.start[lane + kWave] <= chunk)) - 1;
+    int i = -1;
+#pragma unroll
+    for (int from = 0; from < kTable; from += kWave) i += __popcll(__ballot(from + lane < kTable && a.start[from + lane < kTable ? from + lane : 0] <= chunk));
     const int k = __builtin_amdgcn_readfirstlane(i);
     Piece p;
-    p.dtype = a.dtype[k];
-    const uint64_t per = p.dtype == BT_F32 ? kChunk / 4 : kChunk / 2;
+    p.dtype = a.last[k] >> 30;
+    const uint32_t per = p.dtype == BT_F32 ? kChunk / 4 : kChunk / 2, end = k + 1 < kTable && a.start[k + 1] < a.chunks ? a.start[k + 1] : a.chunks;
     p.first = (uint64_t)(chunk - a.start[k]) * per;
     p.in = a.in[k];
     p.out = a.out[k];
-    p.left = a.n[k] - p.first;
+    p.left = chunk + 1 == end ? a.last[k] & 0x3fffffffu : per;
     return p;
 }
 
 template <class T> __device__ inline void load_chunk(const Piece &p, raw16 (&v)[kClipVecs]) {
     const T *const in = (const T *)p.in + p.first;
+    if (p.left == kChunk / sizeof(T)) {
+#pragma unroll
+        for (int i = 0; i < kClipVecs; ++i) v[i] = reinterpret_cast<const Unaligned<T> *>(in + (i * kClipThreads + threadIdx.x) * kPer<T>)->v;
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < kClipVecs; ++i) {
-        const int64_t c = (int64_t)(i * kClipThreads + threadIdx.x) * kPer<T>;
-        v[i] = load_vec(in + c, (int64_t)p.left - c);
+        const int c = (int)((i * kClipThreads + threadIdx.x) * kPer<T>);
+        v[i] = load_vec(in + c, (int)p.left - c, p.first != 0 ? kPer<T> : c);
     }
 }
 
-template <class T> __device__ inline double sum_chunk(const Piece &p) {
-    raw16 v[kClipVecs];
-    load_chunk<T>(p, v);
+__device__ inline void load_chunk(const Piece &p, raw16 (&v)[kClipVecs]) {
+    if (p.dtype == BT_F32) load_chunk<float>(p, v);
+    else load_chunk<bf16>(p, v);      // (bits)
+}
+
+template <class T> __device__ inline double sum_chunk(const raw16 (&v)[kClipVecs]) {
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < kClipVecs; ++i) {
@@ -441,18 +515,16 @@ template <class T> __device__ inline double sum_chunk(const Piece &p) {
     return sum;
 }
 
-template <class T> __device__ inline void scale_chunk(const Piece &p, const float factor) {
-    raw16 v[kClipVecs];
-    load_chunk<T>(p, v);
+template <class T> __device__ inline void scale_chunk(const Piece &p, const raw16 (&v)[kClipVecs], const float factor) {
     T *const out = (T *)p.out + p.first;
 #pragma unroll
     for (int i = 0; i < kClipVecs; ++i) {
-        const int64_t c = (int64_t)(i * kClipThreads + threadIdx.x) * kPer<T>;
+        const int c = (int)((i * kClipThreads + threadIdx.x) * kPer<T>);
         float x[kPer<T>];
         unpack<T>(v[i], x);
 #pragma unroll
         for (int e = 0; e < kPer<T>; ++e) x[e] *= factor;
-        if (c < (int64_t)p.left) store_vec(out + c, (int64_t)p.left - c, pack<T>(x));
+        if (c < (int)p.left) store_vec(out + c, (int)p.left - c, pack<T>(x));
     }
 }
 
@@ -471,7 +543,9 @@ __global__ __launch_bounds__(kClipThreads) void square_sum_kernel(const ClipTabl
     double sum = 0.0;
     for (uint32_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
         const Piece p = piece_of(a, chunk);
-        sum += p.dtype == BT_F32 ? sum_chunk<float>(p) : p.dtype == BT_F16 ? sum_chunk<f16>(p) : sum_chunk<bf16>(p);
+        raw16 v[kClipVecs];
+        load_chunk(p, v);
+        sum += p.dtype == BT_F32 ? sum_chunk<float>(v) : p.dtype == BT_F16 ? sum_chunk<f16>(v) : sum_chunk<bf16>(v);
     }
     sum = block_sum(sum, room);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
@@ -498,18 +572,26 @@ __global__ __launch_bounds__(kClipThreads) void total_kernel(const double *sums,
 __global__ __launch_bounds__(kClipThreads) void scale_kernel(const ClipTable a, const double *sums, const uint32_t count, const double max_norm,
                                                              const double eps, float *norm) {
     __shared__ double room[kClipThreads / kWave];
+    // From the last chunk to the first: the last ones read are those that the caches still hold.  The first one comes while the sums do.
+    uint32_t i = blockIdx.x;
+    Piece p = piece_of(a, a.chunks - 1 - i);
+    raw16 v[kClipVecs];
+    load_chunk(p, v);
     const double x = sqrt(total_of(sums, count, room));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)x;
     double ratio = max_norm / (x + eps);
     if (ratio > 1.0) ratio = 1.0;              // (a NaN stays one)
     const float factor = (float)ratio;
-    // From the last chunk to the first: the last ones read are those that the caches still hold.
-    for (uint32_t i = blockIdx.x; i < a.chunks; i += gridDim.x) {
-        const Piece p = piece_of(a, a.chunks - 1 - i);
-        if (factor == 1.0f && p.in == p.out) continue;      // it is there
-        if (p.dtype == BT_F32) scale_chunk<float>(p, factor);
-        else if (p.dtype == BT_F16) scale_chunk<f16>(p, factor);
-        else scale_chunk<bf16>(p, factor);
+    for (;;) {
+        if (factor != 1.0f || p.in != p.out) {      // (else it is there)
+            if (p.dtype == BT_F32) scale_chunk<float>(p, v, factor);
+            else if (p.dtype == BT_F16) scale_chunk<f16>(p, v, factor);
+            else scale_chunk<bf16>(p, v, factor);
+        }
+        i += gridDim.x;
+        if (i >= a.chunks) break;
+        p = piece_of(a, a.chunks - 1 - i);
+        load_chunk(p, v);
     }
 }
 
@@ -535,7 +617,7 @@ int backward_threads(const uint64_t vectors) {
 
 uint32_t norm_runs(const uint64_t rows, const uint64_t cols, const int width) {
     const int nt = backward_threads((cols * width + kVec - 1) / kVec);
-    const uint64_t most = 256 * (nt <= 256 ? 4 : 1024 / nt);
+    const uint64_t most = 256 * (nt <= 256 ? 3 : nt <= 512 ? 2 : 1);
     return (uint32_t)(rows < most ? rows : most);
 }
 
@@ -574,9 +656,9 @@ struct ClipPlan {
             if (it.n == 0) continue;
             table.in[used] = it.d_in;
             table.out[used] = it.d_out;
-            table.n[used] = it.n;
+            const uint32_t per = kChunk / width_of(it.dtype);
             table.start[used] = (uint32_t)at;
-            table.dtype[used] = (uint8_t)it.dtype;
+            table.last[used] = (uint32_t)((it.n - 1) % per + 1) | (uint32_t)it.dtype << 30;
             at += chunks;
             ++used;
         }

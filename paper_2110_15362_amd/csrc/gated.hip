@@ -139,10 +139,10 @@ template <class T, Order O, int N, int F, int kThreads> struct Staged {
                 const Operand &from = two && (row / kHalf) % 2 ? other : a;
                 const uint32_t r = n + (two ? row / (2 * kHalf) * kHalf + weight_row<F>(row % kHalf) : row);
                 v[i] = raw16{0, 0, 0, 0};
-                if (r < from.rows) v[i] = load_vec((const T *)from.p + r * from.pitch + k + col, (int64_t)from.cols - k - col);
+                if (r < from.rows) v[i] = load_vec((const T *)from.p + r * from.pitch + k + col, (int)(from.cols - k) - col, (int)k + col);
             } else {
                 v[i] = raw16{0, 0, 0, 0};
-                if (k + row < a.rows) v[i] = load_vec((const T *)a.p + (k + row) * a.pitch + n + col, (int64_t)a.cols - n - col);
+                if (k + row < a.rows) v[i] = load_vec((const T *)a.p + (k + row) * a.pitch + n + col, (int)(a.cols - n) - col, (int)n + col);
             }
         }
     }
@@ -190,7 +190,7 @@ template <class T> __device__ inline float gated(const int activation, float &g,
     return h;
 }
 
-template <class T> __device__ inline void store4(T *p, const int64_t left, const float (&x)[4]) {
+template <class T> __device__ inline void store4(T *p, const int left, const float (&x)[4]) {
     if (left >= 4) {
         if constexpr (sizeof(T) == 4) store_vec(p, 4, pack<T>(x));
         else {
@@ -206,7 +206,7 @@ template <class T> __device__ inline void store4(T *p, const int64_t left, const
 }
 
 // N neighbours, whole vectors where there are any.
-template <class T, int N> __device__ inline void store_run(T *p, const int64_t left, const float (&x)[N]) {
+template <class T, int N> __device__ inline void store_run(T *p, const int left, const float (&x)[N]) {
     constexpr int E = kPer<T> < N ? kPer<T> : N;
 #pragma unroll
     for (int i = 0; i < N; i += E) {
@@ -271,7 +271,7 @@ template <class T, Product K, int FP, int FQ> __device__ inline void finish(cons
         if constexpr (K == kForward) {
             constexpr int N = 2 * FP;      // neighbours that the lane has
             const uint32_t col = n + lane / 16 * N;
-            const int64_t left = (int64_t)a.n - col;
+            const int left = (int)(a.n - col);
             const uint64_t at = row * a.pitch + col;
             if (left <= 0) continue;
             float g[N], u[N], h[N];
@@ -296,7 +296,7 @@ template <class T, Product K, int FP, int FQ> __device__ inline void finish(cons
 #pragma unroll
             for (int i = 0; i < FP; ++i) {
                 const uint32_t col = n + i * 16 + lane / 16 * 4;
-                const int64_t left = (int64_t)a.n - col;
+                const int left = (int)(a.n - col);
                 const float x[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
                 if (left <= 0) continue;
                 if (parts) store4(parts + (uint64_t)row * a.n + col, left, x);
@@ -626,14 +626,14 @@ template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) voi
     while (unit < whole) take(std::integral_constant<int, 1>{});
     if (wave == 0 && whole * kUnit<T> < a.k) {      // the rest, less than a unit
         const uint32_t k = whole * kUnit<T>;
-        const int64_t left = (int64_t)a.k - k - group * (2 * kPer<T>);
+        const int left = (int)(a.k - k) - group * (2 * kPer<T>);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             raw16 w[2], x[FQ];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) w[i] = load_vec(p[i] + k + h * kPer<T>, left - h * kPer<T>);
+            for (int i = 0; i < 2; ++i) w[i] = load_vec(p[i] + k + h * kPer<T>, left - h * kPer<T>, (int)a.k - left + h * kPer<T>);
 #pragma unroll
-            for (int j = 0; j < FQ; ++j) x[j] = load_vec(q[j] + k + h * kPer<T>, left - h * kPer<T>);
+            for (int j = 0; j < FQ; ++j) x[j] = load_vec(q[j] + k + h * kPer<T>, left - h * kPer<T>, (int)a.k - left + h * kPer<T>);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -668,7 +668,7 @@ template <class T, Product K> __global__ __launch_bounds__(256) void gated_join_
     constexpr int E = kPer<T>, kSums = K == kGradX ? 1 : 2;
     const uint64_t c = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * E;
     if (c >= cells) return;
-    const int64_t left = (int64_t)(cells - c);
+    const int left = cells - c < 64 ? (int)(cells - c) : 64;
     float x[kSums][E] = {};
     for (uint32_t split = 0; split < a.splits; ++split)
 #pragma unroll
@@ -676,7 +676,7 @@ template <class T, Product K> __global__ __launch_bounds__(256) void gated_join_
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
                 float y[4];
-                unpack<float>(load_vec(a.parts + (split * kSums + k) * cells + c + e, left - e), y);
+                unpack<float>(load_vec(a.parts + (split * kSums + k) * cells + c + e, left - e, (c != 0 ? 4 : 0) + e), y);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[k][e + i] += y[i];
             }
@@ -701,7 +701,7 @@ template <class T> __global__ __launch_bounds__(256) void pad_kernel(const T *fr
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < vectors; i += (uint64_t)gridDim.x * 256) {
         const uint64_t row = i / a_row;
         const uint32_t col = (uint32_t)(i - row * a_row) * kPer<T>;
-        store_vec(to + i * kPer<T>, kPer<T>, load_vec(from + row * cols + col, (int64_t)cols - col));
+        store_vec(to + i * kPer<T>, kPer<T>, load_vec(from + row * cols + col, (int)(cols - col), (int)col));
     }
 }
 
@@ -715,9 +715,9 @@ template <class T> __global__ __launch_bounds__(256) void gated_slopes_kernel(co
         const uint32_t col = (uint32_t)(i - row * a_row) * kPer<T>;
         const uint64_t at = row * f + col;
         float h[kPer<T>], g[kPer<T>], u[kPer<T>];
-        unpack<T>(load_vec(grad_h + at, (int64_t)f - col), h);
-        unpack<T>(load_vec(gate + at, (int64_t)f - col), g);
-        unpack<T>(load_vec(up + at, (int64_t)f - col), u);
+        unpack<T>(load_vec(grad_h + at, (int)(f - col), (int)col), h);
+        unpack<T>(load_vec(gate + at, (int)(f - col), (int)col), g);
+        unpack<T>(load_vec(up + at, (int)(f - col), (int)col), u);
 #pragma unroll
         for (int e = 0; e < kPer<T>; ++e) {
             if (activation == BT_ACT_RELU) {
