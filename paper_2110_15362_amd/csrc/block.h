@@ -73,12 +73,12 @@ template <class T> __device__ inline raw16 pack(const float (&x)[kPer<T>]) {
 }
 
 // Elements [0, left) of the vector at p, zeros behind them.  A vector that ends beyond its row is read from further in front, where the row has
-// `before` elements, and moved: one load instead of one an element.
+// `before` elements, and moved: one load instead of up to seven.
 template <class T> __device__ inline raw16 load_vec(const T *p, const int left, const int before) {
     if (left >= kPer<T>) return reinterpret_cast<const Unaligned<T> *>(p)->v;
     raw16 v = {0, 0, 0, 0};
     if (left <= 0) return v;
-    if (left + before >= kPer<T>) {
+    if (sizeof(T) == 2 && left + before >= kPer<T>) {
         typedef uint64_t two __attribute__((ext_vector_type(2)));
         raw16 bits = reinterpret_cast<const Unaligned<T> *>(p + left - kPer<T>)->v;
         // (Or the compiler makes one load of this and the one above, and waves without such a vector wait for theirs to be moved by nothing.)

@@ -149,7 +149,7 @@ __device__ __host__ inline uint32_t run_start(const uint32_t run, const uint32_t
 }
 
 template <class T, int NT, int V>
-__global__ __launch_bounds__(NT) void norm_backward_kernel(const NormBackward a) {
+__global__ __launch_bounds__(NT, 4) void norm_backward_kernel(const NormBackward a) {
     constexpr int E = kPer<T>;
     // 16 columns a thread of a full workgroup: three sums of each are more than its registers hold beside the row, so two of them are kept in LDS
     // (128 of 160 KiB; 256 KiB of LDS traffic a row of 16384, a tenth of the time that the row takes from memory).
@@ -187,10 +187,10 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormBackward a)
         group_first = group * a.rows_a_gate;
         group_end = group_first + a.rows_a_gate;
     }
-    // Wide rows: what follows from the thread's number is worked out again each time, or it would take the registers that hold the row.
+    // What follows from the thread's number is worked out again each time where it would take registers that hold the row.
     const auto number = [&] {
         int n = t;
-        if (kWide) asm volatile("" : "+v"(n));
+        if (kWide || sizeof(T) == 2) asm volatile("" : "+v"(n));
         return n;
     };
     // A row's vectors: with kAhead the next row's are on their way while one is worked on.
@@ -597,7 +597,12 @@ __global__ __launch_bounds__(kClipThreads) void scale_kernel(const ClipTable a, 
 
 // ---- host ------------------------------------------------------------------------------------------------------
 
-template <class T, class Go> bt_status with_forward_shape(const uint64_t vectors, Go go) {
+// (Few rows leave most compute units idle: what counts is how soon one row is through, and more threads are through sooner.)
+constexpr uint64_t kFewRows = 256;
+
+template <class T, class Go> bt_status with_forward_shape(const uint64_t rows, const uint64_t vectors, Go go) {
+    if (rows <= kFewRows && vectors > 256 && vectors <= 512) return go(norm_forward_kernel<T, 512, 1>, 512);
+    if (rows <= kFewRows && vectors > 512 && vectors <= 1024) return go(norm_forward_kernel<T, 1024, 1>, 1024);
     if (vectors <= 64) return go(norm_forward_kernel<T, 64, 1>, 64);
     if (vectors <= 128) return go(norm_forward_kernel<T, 64, 2>, 64);
     if (vectors <= 256) return go(norm_forward_kernel<T, 256, 1>, 256);
@@ -617,7 +622,7 @@ int backward_threads(const uint64_t vectors) {
 
 uint32_t norm_runs(const uint64_t rows, const uint64_t cols, const int width) {
     const int nt = backward_threads((cols * width + kVec - 1) / kVec);
-    const uint64_t most = 256 * (nt <= 256 ? 3 : nt <= 512 ? 2 : 1);
+    const uint64_t most = 256 * (nt <= 128 ? 8 : 1024 / nt);
     return (uint32_t)(rows < most ? rows : most);
 }
 
@@ -720,7 +725,7 @@ bt_status bt_residual_norm_forward(const void *d_x, const void *d_block, const v
                            (uint32_t)(d_gate ? rows / gate_rows : 1), 0, (float)eps, (float)scale, (float)residual_scale};
     return with_type(dtype, [&](auto type) {
         using T = decltype(type);
-        return with_forward_shape<T>((cols + kPer<T> - 1) / kPer<T>, [&](auto kernel, const int nt) {
+        return with_forward_shape<T>(rows, (cols + kPer<T> - 1) / kPer<T>, [&](auto kernel, const int nt) {
             // (A grid holds less than 2^32 threads.)
             const uint64_t a_block = nt < 256 ? 256 / nt : 1, most = (uint64_t)1 << 21;
             bt_status s = BT_OK;
