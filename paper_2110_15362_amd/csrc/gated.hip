@@ -18,6 +18,12 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 #define BT_LDS __attribute__((address_space(3)))
 
+// `x`, which the compiler takes for another one each time: what follows from it is worked out where it is needed, and holds no registers until then.
+__device__ inline int fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // ---- one step of a product -------------------------------------------------------------------------------------
 //
 // A fragment is 16 rows (or columns) by kKStep of the summed index, 16 bytes a lane: lane l holds row l % 16 and, of every kKStep, the
@@ -111,12 +117,12 @@ struct Operand {
 };
 
 // A workgroup: WP waves along P by two along Q, each of FP fragments of P by FQ of Q.
-template <int WP_, int FP_, int FQ_> struct Shape {
-    static constexpr int WP = WP_, FP = FP_, FQ = FQ_, WAVES = 2 * WP, THREADS = WAVES * kWave, NP = WP * FP * 16, NQ = 2 * FQ * 16;
+template <int WP_, int FP_, int FQ_, int PLACES_> struct Shape {
+    static constexpr int WP = WP_, FP = FP_, FQ = FQ_, PLACES = PLACES_, WAVES = 2 * WP, THREADS = WAVES * kWave, NP = WP * FP * 16, NQ = 2 * FQ * 16;
 };
-typedef Shape<4, 4, 8> Large;      // 256 by 256, 8 waves
-typedef Shape<2, 4, 4> Middle;     // 128 by 128, 4 waves
-typedef Shape<2, 2, 2> Small;      // 64 by 64, 4 waves
+typedef Shape<4, 4, 8, 4> Large;      // 256 by 256, 8 waves
+typedef Shape<2, 4, 4, 4> Middle;     // 128 by 128, 4 waves
+typedef Shape<2, 2, 2, 4> Small;      // 64 by 64, 4 waves
 
 // The forward pass: which row of a weight, of the 8 F that a wave has of it, lies in row r of them in LDS, the wave having F fragments, F / 2 of each
 // weight.  In this order a lane's results of all fragments are 2 F neighbours of h.
@@ -133,7 +139,7 @@ template <class T, Order O, int N, int F, int kThreads> struct Staged {
     __device__ void load(const Operand &a, const Operand &other, const bool two, const uint32_t n, const uint32_t k) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int q = i * kThreads + threadIdx.x, row = q / L::CHUNKS, col = (q % L::CHUNKS) * kPer<T>;
+            const int q = i * kThreads + fresh(threadIdx.x), row = q / L::CHUNKS, col = (q % L::CHUNKS) * kPer<T>;
             if constexpr (O == kAlong) {
                 constexpr int kHalf = F * 8;      // rows of a wave that belong to one weight
                 const Operand &from = two && (row / kHalf) % 2 ? other : a;
@@ -149,7 +155,7 @@ template <class T, Order O, int N, int F, int kThreads> struct Staged {
     __device__ void store(char *tile) const {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int q = i * kThreads + threadIdx.x;
+            const int q = i * kThreads + fresh(threadIdx.x);
             *(raw16 *)(tile + L::place(q / L::CHUNKS, q % L::CHUNKS)) = v[i];
         }
     }
@@ -229,6 +235,7 @@ struct GatedJob {
     uint32_t m, n, k;                // rows and columns of the output (of each), and the summed index (of each sum)
     uint32_t tiles_n, tiles_m;       // of each output
     uint32_t splits;                 // parts of the summed index, each of other workgroups
+    uint32_t groups;                 // tiles of all outputs and splits
     float *parts;                    // their sums, [splits, 2 of the forward pass and the weights' gradients, m, n]; with one split NULL
     int activation;
 };
@@ -236,16 +243,16 @@ struct GatedJob {
 template <class T, Product K> constexpr Order kOrderP = K == kForward ? kAlong : kAcross;
 template <class T, Product K> constexpr Order kOrderQ = K == kGradW ? kAcross : kAlong;
 
-// Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn, each of which has an L2 of its own: an XCD's are neighbours, in bands
+// The tile of a number, of a workgroup as a rule.  Workgroups go to the eight XCDs in turn, each of which has an L2 of its own: an XCD's are neighbours, in bands
 // of four rows of tiles, so that those that run at once share what they read.
 struct Place {
     uint32_t m, n, part, split;
 };
 
-template <Product K> __device__ inline Place place_of(const GatedJob &a, const uint32_t tile_m, const uint32_t tile_n) {
+template <Product K> __device__ inline Place place_of(const GatedJob &a, const uint32_t number, const uint32_t tile_m, const uint32_t tile_n) {
     constexpr uint32_t kXcds = 8, kBand = 4;
-    const uint32_t total = gridDim.x, xcd = blockIdx.x % kXcds, more = total % kXcds;
-    uint32_t tile = xcd * (total / kXcds) + (xcd < more ? xcd : more) + blockIdx.x / kXcds;
+    const uint32_t xcd = number % kXcds, more = a.groups % kXcds;
+    uint32_t tile = xcd * (a.groups / kXcds) + (xcd < more ? xcd : more) + number / kXcds;
     const uint32_t a_split = a.tiles_m * a.tiles_n * (K == kGradW ? 2 : 1);
     Place at;
     at.split = tile / a_split;
@@ -262,7 +269,7 @@ template <Product K> __device__ inline Place place_of(const GatedJob &a, const u
 // What becomes of a wave's sums: rows from m on, FQ fragments of 16; columns from n on, FP fragments, of the forward pass half of them columns
 // of the gate's product and half the same columns of the other.
 template <class T, Product K, int FP, int FQ> __device__ inline void finish(const GatedJob &a, const acc4 (&acc)[FP][FQ], const uint32_t m, const uint32_t n, const Place &of) {
-    const int lane = threadIdx.x % kWave;
+    const int lane = fresh(threadIdx.x) % kWave;
     float *const parts = a.parts ? a.parts + ((uint64_t)of.split * (K == kGradX ? 1 : 2) + of.part) * a.m * a.n : nullptr;
 #pragma unroll
     for (int j = 0; j < FQ; ++j) {
@@ -374,14 +381,16 @@ template <class T, Product K, class S> struct Work {
     }
 };
 
-// Of `count` tiles of the summed index, in order, the first of a split.
-__device__ inline uint32_t split_start(const GatedJob &a, const uint32_t split, const uint32_t count) { return (uint32_t)((uint64_t)count * split / a.splits); }
+// Of `count` tiles of the summed index, in order, the first of a split: one of an even number, since two share the memory's lines.
+__device__ inline uint32_t split_start(const GatedJob &a, const uint32_t split, const uint32_t count) {
+    return split == a.splits ? count : (uint32_t)((uint64_t)count * split / a.splits) & ~1u;
+}
 
 // Any alignment and any size: tiles go through registers, the next one on its way to them while one is multiplied.
 template <class T, Product K> __global__ __launch_bounds__(Small::THREADS) void gated_any_kernel(const GatedJob a) {
     typedef Work<T, K, Small> W;
     __shared__ __align__(16) char tiles[W::P::BYTES + W::Q::BYTES];
-    const Place at = place_of<K>(a, Small::NQ, W::COLS);
+    const Place at = place_of<K>(a, blockIdx.x, Small::NQ, W::COLS);
     typename W::Sums acc = {};
     W w;
     const uint32_t a_sum = (a.k + kK<T> - 1) / kK<T>, last = split_start(a, at.split + 1, a_sum * W::SUMS);
@@ -418,7 +427,7 @@ template <class T, Order O, int N, int WAVES, bool ROUND> struct Direct {
 
     // `n`: the product's row or column that the tile begins at.  F: of the forward pass, whose weights' rows are those of `n` on in another order.
     template <int F = 0> __device__ void start(const Operand &a, const uint32_t n) {
-        const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        const int lane = fresh(threadIdx.x) % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int q = (wave * PER + i) * kWave + lane, chunk = (L::place(q / L::CHUNKS, q % L::CHUNKS) / kVec) % L::CHUNKS;
@@ -439,13 +448,30 @@ template <class T, Order O, int N, int WAVES, bool ROUND> struct Direct {
         const Operand &a = wave % 2 ? up : gate;
         start<F>(a, first < a.rows ? first : 0);
     }
-    __device__ void fetch(char *tile) {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    // The next tile's descriptor.
+    __device__ __amdgpu_buffer_rsrc_t next() {
         const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00020000);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (BT_LDS void *)(tile + (wave * PER + i) * 1024), 16, (int)offset[i], 0, 0, 0);
         base += advance;
         if (ROUND && --ahead == 0) base -= round;
+        return r;
+    }
+    __device__ void piece(const __amdgpu_buffer_rsrc_t r, char *tile, const int i) const {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (BT_LDS void *)(tile + (wave * PER + i) * 1024), 16, (int)offset[i], 0, 0, 0);
+    }
+    __device__ void fetch(char *tile) {
+        const __amdgpu_buffer_rsrc_t r = next();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) piece(r, tile, i);
+    }
+    // The next tile and the one after it, piece by piece.
+    __device__ void fetch(char *tile, char *after) {
+        const __amdgpu_buffer_rsrc_t r = next(), s = next();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            piece(r, tile, i);
+            piece(s, after, i);
+        }
     }
     // Begin at tile `at` of the `count` from `first` on; with ROUND the tiles before it come last.
     __device__ void rotate(const uint32_t first, const uint32_t at, const uint32_t count) {
@@ -457,20 +483,24 @@ template <class T, Order O, int N, int WAVES, bool ROUND> struct Direct {
 
 // Until all but the last `LEFT` of this wave's fetches have landed, then for the other waves: their fetches have landed too, and they have read
 // what they need of the tiles before.
+constexpr int kFetchesNever = 64;      // (all are known to have)
+
 template <int LEFT> __device__ inline void wait_for_tiles() {
-    static_assert(LEFT < 64);
+    static_assert(LEFT <= kFetchesNever);
     asm volatile("" ::: "memory");           // (the barrier itself keeps the compiler's loads and stores from nothing)
-    __builtin_amdgcn_s_waitcnt(0x0f70 | (LEFT & 15) | (LEFT >> 4) << 14);      // vmcnt
+    if (LEFT < kFetchesNever) __builtin_amdgcn_s_waitcnt(0x0f70 | (LEFT & 15) | (LEFT >> 4 & 3) << 14);      // vmcnt
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
-// Four tiles of either operand in LDS: while one is multiplied, the next three are on their way.  A tile's products are made in two halves (of
-// Q's fragments).  While the first is made, the second's fragments are read and the tile three further on is asked for, while the second is made,
-// the next tile's; behind the barrier between them a tile's place has been read by all.  The instructions of either kind are spread among the
-// products: each waits for the unit that takes it, and a wave that waits for that multiplies nothing.
-constexpr int kPlaces = 4;
-
+// Tiles of either operand in LDS, the next ones on their way while one is multiplied.  A tile's products are made in two halves (of Q's
+// fragments).  While the first is made, the second's fragments are read and further tiles are asked for, while the second is made, the next
+// tile's first fragments are read; behind the barrier between them a tile's place has been read by all.  The instructions of either kind
+// are spread among the products: each waits for the unit that takes it, and a wave that waits for that multiplies nothing.
+//
+// With the summed index along the rows a tile has half of each 128-byte line that it touches, and a line asked for a tile later is fetched again from
+// the L2 (the forward pass: 132 M lines instead of 67 M).  So the forward pass and grad_x ask for two tiles at a time, in every second one, piece by
+// piece, and have five places; the weights' gradients, whose operands lie across, ask for one tile in each and have four.
 template <int KIND, int COUNT, int PRODUCTS, int GROUPS, int G = 0> __device__ inline void spread_kind() {
     if constexpr (G < GROUPS) {
         constexpr int c = COUNT * (G + 1) / GROUPS - COUNT * G / GROUPS, m = PRODUCTS * (G + 1) / GROUPS - PRODUCTS * G / GROUPS;
@@ -488,7 +518,14 @@ template <int READS, int FETCHES, int PRODUCTS> __device__ inline void spread() 
     if constexpr (FETCHES != 0) spread_kind<0x10, FETCHES, kSecond, (FETCHES < kSecond ? FETCHES : kSecond)>();
 }
 
-template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, S::THREADS >= 512 ? 2 : 1) void gated_kernel(const GatedJob a) {
+template <int N, int I = 0, class Go> __device__ inline void turn(Go go) {
+    if constexpr (I < N) {
+        go(std::integral_constant<int, I>{});
+        turn<N, I + 1>(go);
+    }
+}
+
+template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, S::FQ == 8 ? 2 : 1) void gated_kernel(const GatedJob a) {
     typedef Work<T, K, S> W;
     // Rows of a power of two of bytes all begin in the same channel of the memory, and workgroups in step would ask one after the other: each XCD
     // begins elsewhere in the summed index (us: forward [16384, 2048] x 8192 1045 -> 970, grad_x 915 -> 885), or with few rows each of 64
@@ -496,78 +533,116 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
     constexpr bool kRound = K != kGradW;
     typedef Direct<T, kOrderP<T, K>, S::NP, S::WAVES, kRound> FetchP;
     typedef Direct<T, kOrderQ<T, K>, S::NQ, S::WAVES, kRound> FetchQ;
-    constexpr int PB = W::P::BYTES, QB = W::Q::BYTES, kFetches = FetchP::PER + FetchQ::PER;
+    constexpr bool kTwo = K == kForward && S::FQ == 2;
+    constexpr int kPlaces = kTwo ? 5 : S::PLACES, kTurn = kPlaces % 2 == 0 ? kPlaces : 2 * kPlaces;
+    constexpr int kAhead = kPlaces - 1, kLeft = kTwo ? 2 : kAhead - 1;      // from a tile to the furthest that it asks for; tiles that may be on their way behind the next
+    constexpr int PB = W::P::BYTES, QB = W::Q::BYTES, kFetches = FetchP::PER + FetchQ::PER;      // kFetches: instructions of a tile
     constexpr int kReadsP = S::FP * Reader<T, kOrderP<T, K>, S::NP, S::FP>::READS, kReadsQ = S::FQ / 2 * Reader<T, kOrderQ<T, K>, S::NQ, S::FQ>::READS;
     constexpr int kProducts = S::FP * S::FQ / 2 * (sizeof(T) == 4 ? 4 : 1);
     __shared__ __align__(1024) char tiles[kPlaces * (PB + QB)];
-    const Place at = place_of<K>(a, S::NQ, W::COLS);
-    typename W::Sums acc = {};
     W w;
+    FetchP dp;
+    FetchQ dq;
     const uint32_t a_sum = a.k / kK<T>;      // whole tiles
     const uint32_t phases = a.tiles_m == 1 ? 64 : 8;
-    const uint32_t from = split_start(a, at.split, a_sum * W::SUMS), to = split_start(a, at.split + 1, a_sum * W::SUMS);
-    for (int sum = 0; sum < W::SUMS; ++sum) {
-        const Operand &op = a.p[sum], &oq = a.q[sum + at.part];
+    const auto tile_p = [&](const int t) { return tiles + t % kPlaces * PB; };
+    const auto tile_q = [&](const int t) { return tiles + kPlaces * PB + t % kPlaces * QB; };
+    // The first tiles of a sum are asked for; returns how many there are.
+    const auto begin = [&](const Place &at, const int sum) {
+        const uint32_t from = split_start(a, at.split, a_sum * W::SUMS), to = split_start(a, at.split + 1, a_sum * W::SUMS);
         const uint32_t before = sum * a_sum, behind = before + a_sum, first = from > before ? from : before, last = to < behind ? to : behind;
-        if (first < last) {
-            const uint32_t count = last - first;
-            FetchP dp;
-            FetchQ dq;
-            if constexpr (K == kForward) dp.template start_pair<S::FP>(a.p[0], a.p[1], at.n);
-            else dp.start(op, at.n);
-            dq.start(oq, at.m);
-            const uint32_t phase = kRound ? (uint32_t)((uint64_t)(blockIdx.x % phases) * count / phases) : 0;
-            dp.rotate(first - before, phase, count);
-            dq.rotate(first - before, phase, count);
-            const auto tile_p = [&](const int place) { return tiles + place * PB; };
-            const auto tile_q = [&](const int place) { return tiles + kPlaces * PB + place * QB; };
-            const auto fetch = [&](const int place) {
-                dp.fetch(tile_p(place));
-                dq.fetch(tile_q(place));
-            };
-            // The tile that lies in `place`; `more`: there is one three further on.
-            const auto tile = [&](const int place, const bool more) {
-                w.read_q(tile_q(place), 1);
-                if (more) fetch((place + 3) % kPlaces);
-                w.multiply(acc, place & 1, 0);
-                spread<kReadsQ, kFetches, kProducts>();
-                __builtin_amdgcn_sched_barrier(0);
-                __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the last fragments of this tile are here
-                if (more) wait_for_tiles<2 * kFetches>();
-                else wait_for_tiles<0>();
-                w.read_p(tile_p((place + 1) % kPlaces), (place + 1) & 1);      // (behind the last tile: what lies there, unused)
-                w.read_q(tile_q((place + 1) % kPlaces), 0);
-                w.multiply(acc, place & 1, 1);
-                spread<kReadsP + kReadsQ, 0, kProducts>();
-                __builtin_amdgcn_sched_barrier(0);
-            };
-            if (sum != 0) __syncthreads();
+        if (first >= last) return 0u;
+        const uint32_t count = last - first, phase = kRound ? (uint32_t)((uint64_t)(blockIdx.x % phases) * count / phases) & ~1u : 0;
+        if constexpr (K == kForward) dp.template start_pair<S::FP>(a.p[0], a.p[1], at.n);
+        else dp.start(a.p[sum], at.n);
+        dq.start(a.q[sum + at.part], at.m);
+        dp.rotate(first - before, phase, count);
+        dq.rotate(first - before, phase, count);
 #pragma unroll
-            for (int t = 0; t < 3; ++t)
-                if ((uint32_t)t < count) fetch(t);
-            if (count >= 3) wait_for_tiles<2 * kFetches>();
-            else wait_for_tiles<0>();
-            w.read_p(tile_p(0), 0);
-            w.read_q(tile_q(0), 0);
-            __builtin_amdgcn_sched_barrier(0);
-            uint32_t t = 0;
-            for (; t + 7 <= count; t += 4) {
-                tile(0, true);
-                tile(1, true);
-                tile(2, true);
-                tile(3, true);
+        for (int t = 0; t < kAhead; ++t)
+            if ((uint32_t)t < count) {
+                dp.fetch(tile_p(t));
+                dq.fetch(tile_q(t));
             }
-            for (; t < count; t += 4) {
-                tile(0, t + 3 < count);
-                if (t + 1 < count) tile(1, t + 4 < count);
-                if (t + 2 < count) tile(2, t + 5 < count);
-                if (t + 3 < count) tile(3, t + 6 < count);
+        return count;
+    };
+    // Workgroups of the largest tiles, one to a compute unit, take several: the next one's first tiles of the summed index are asked for before
+    // the results of this one are worked out and stored.
+    uint32_t number = blockIdx.x;
+    Place at = place_of<K>(a, number, S::NQ, W::COLS);
+    uint32_t count = begin(at, 0);
+    bool stored = false;      // since the first tiles were asked for: kStores results of each lane, exactly
+    constexpr int kStores = K == kForward ? S::FQ : S::FP * S::FQ;
+    for (;;) {
+        typename W::Sums acc = {};
+        // Tile i of a turn, which lies in place i % kPlaces, with `left` tiles from it to the end.
+        const auto tile = [&](auto turn_number, const uint32_t left) {
+            constexpr int i = decltype(turn_number)::value;
+            constexpr bool kAsks = !kTwo || i % 2 == 1;
+            w.read_q(tile_q(i), 1);
+            if (kTwo && kAsks && left > 4) {
+                dp.fetch(tile_p(i + 3), tile_p(i + 4));
+                dq.fetch(tile_q(i + 3), tile_q(i + 4));
+            } else if (kAsks && left > (kTwo ? 3 : kAhead)) {
+                dp.fetch(tile_p(i + (kTwo ? 3 : kAhead)));
+                dq.fetch(tile_q(i + (kTwo ? 3 : kAhead)));
+            }
+            w.multiply(acc, i & 1, 0);
+            spread<kReadsQ, kAsks ? (kTwo ? 2 : 1) * kFetches : 0, kProducts>();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the last fragments of this tile are here
+            // The next tile has come: what is asked for behind it may still be on its way.  (Of two that were asked for together the second came
+            // with the first.)
+            if (!kAsks) wait_for_tiles<kFetchesNever>();
+            else if (left > kAhead) wait_for_tiles<kLeft * kFetches>();
+            else wait_for_tiles<0>();
+            w.read_p(tile_p(i + 1), (i + 1) & 1);      // (behind the last tile: what lies there, unused)
+            w.read_q(tile_q(i + 1), 0);
+            w.multiply(acc, i & 1, 1);
+            spread<kReadsP + kReadsQ, 0, kProducts>();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        bool through = false;      // registers
+        for (int sum = 0; sum < W::SUMS; ++sum) {
+            if (sum != 0) {
+                __syncthreads();
+                count = begin(at, sum);
+            }
+            if (count != 0) {
+                // (Fetches and stores are counted together, in order.)
+                if (count < kAhead) wait_for_tiles<0>();
+                else if (!stored || sum != 0) wait_for_tiles<kLeft * kFetches>();
+                else if (K == kForward && a.gate) wait_for_tiles<kLeft * kFetches + (K == kForward ? 3 : 1) * kStores>();
+                else wait_for_tiles<kLeft * kFetches + kStores>();
+                w.read_p(tile_p(0), 0);
+                w.read_q(tile_q(0), 0);
+                __builtin_amdgcn_sched_barrier(0);
+                uint32_t t = 0;
+                for (; t + kTurn + kAhead <= count; t += kTurn) turn<kTurn>([&](auto i) { tile(i, kTurn + kAhead); });
+                for (; t < count; t += kTurn)
+                    turn<kTurn>([&](auto i) {
+                        if (t + decltype(i)::value < count) tile(i, count - t - decltype(i)::value);
+                    });
+            }
+            // The rest of the summed index, less than a tile, through registers: of the split that has the last whole tile, or the only one.
+            const uint32_t behind = (sum + 1) * a_sum;
+            if (a_sum * kK<T> < a.k && (a.splits == 1 || (split_start(a, at.split, a_sum * W::SUMS) < behind && behind <= split_start(a, at.split + 1, a_sum * W::SUMS)))) {
+                w.staged(a, a.p[sum], a.q[sum + at.part], at, a_sum * kK<T>, tiles, tiles + PB, acc);
+                through = true;
             }
         }
-        // The rest of the summed index, less than a tile, through registers: of the split that has the last whole tile, or the only one.
-        if (a_sum * kK<T> < a.k && (a.splits == 1 || (from < behind && behind <= to))) w.staged(a, op, oq, at, a_sum * kK<T>, tiles, tiles + kPlaces * PB, acc);
+        const Place here = at;
+        number += gridDim.x;
+        const bool more = number < a.groups;
+        if (more) {
+            if (through) __syncthreads();
+            at = place_of<K>(a, number, S::NQ, W::COLS);
+            count = begin(at, 0);
+        }
+        W::end(a, acc, here);
+        if (!more) break;
+        stored = sizeof(T) == 2 && here.m + S::NQ <= a.m && here.n + W::COLS <= a.n;
     }
-    W::end(a, acc, at);
 }
 
 // Few rows (tokens to answer with): the weights are read once and bound the time, so they go from memory to the registers that multiply them, as many
@@ -835,7 +910,8 @@ template <class T, Product K> bt_status run_product(GatedJob &a, const Plan &pla
         if (groups >= 1u << 23) return BT_ERR_SIZE;      // (a grid holds less than 2^32 threads)
         a.tiles_m = (uint32_t)tiles_m;
         a.tiles_n = (uint32_t)tiles_n;
-        return launch(kernel, dim3((unsigned)groups), S::THREADS, hs, a);
+        a.groups = (uint32_t)groups;
+        return launch(kernel, dim3((unsigned)(S::THREADS == Large::THREADS && groups > 256 ? 256 : groups)), S::THREADS, hs, a);
     };
     bt_status st = BT_OK;
     if (!straight || plan.kind == kAnyKind) st = go(gated_any_kernel<T, K>, Small{});
