@@ -839,10 +839,10 @@ Plan plan_of(const Product product, const uint64_t m, const uint64_t n, const ui
     struct Form {
         Kind kind;
         int rows, cols, together;      // rows and columns of a tile, workgroups that a compute unit holds
-        double rate;
+        double rate, alone;
     };
     const bool single = width == 4;
-    static const Form forms[] = {{kSmall, 64, 64, 4, 0.45}, {kMiddle, 128, 128, 2, 0.75}, {kLarge, 256, 256, 1, 1.0}};
+    static const Form forms[] = {{kSmall, 64, 64, 4, 0.33, 0.28}, {kMiddle, 128, 128, 2, 0.6, 0.38}, {kLarge, 256, 256, 1, 0.95, 0.75}};
     const double peak = single ? 0.6e6 : 5.9e6;                                  // operations a us of a compute unit
     const uint64_t steps = ceil_div(k * width, kKBytes) * (product == kGradX ? 2 : 1), outputs = product == kGradX ? 1 : 2;
     Plan best = {kSmall, 1};
@@ -856,7 +856,7 @@ Plan plan_of(const Product product, const uint64_t m, const uint64_t n, const ui
             const double a_unit = (double)ceil_div(tiles * splits, 256);
             const double rate = single ? 0.8 : f.rate;
             double time = a_unit * work / (peak * rate);
-            const double alone = (double)steps / splits * 0.25 * (double)ceil_div((uint64_t)a_unit, f.together);
+            const double alone = (double)steps / splits * f.alone * (double)ceil_div((uint64_t)a_unit, f.together);
             if (time < alone) time = alone;
             if (splits > 1) time += 4.0 + (double)splits * m * n * outputs * 8.0 / 4e6;
             if (time < least) {
