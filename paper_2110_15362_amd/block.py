@@ -156,9 +156,7 @@ class _GatedLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w_gate, w_up, activation):
         x, w_gate, w_up = _plain(x), _plain(w_gate), _plain(w_up)
-        rows, d, f = x.numel() // max(x.shape[-1], 1), x.shape[-1], w_gate.shape[0]
-        if x.shape[-1] == 0:
-            rows = x.shape[:-1].numel()
+        rows, d, f = x.shape[:-1].numel(), x.shape[-1], w_gate.shape[0]
         h = x.new_empty(x.shape[:-1] + (f,))
         keep = any(ctx.needs_input_grad[:3])
         gate, up = (torch.empty_like(h), torch.empty_like(h)) if keep else (None, None)
@@ -278,10 +276,10 @@ def rms_norm(x, weight, eps=1e-6):
 
 def clip_grad_norm_(parameters, max_norm, eps=1e-6):
     """Scales the gradients of the parameters in place so that their norm is at most max_norm; returns the norm that they had, on the device
-    (float32[1]; infinite or NaN where a gradient is).  Nothing waits for the device."""
+    (float32[1]; infinite or NaN where a gradient is).  A parameter that is given twice counts once.  Nothing waits for the device."""
     if isinstance(parameters, torch.Tensor):
         parameters = [parameters]
-    grads = [p.grad for p in parameters if p.grad is not None]
+    grads = list({id(p): p.grad for p in parameters if p.grad is not None}.values())
     if not grads:
         raise ValueError("no parameter has a gradient")
     _check_device(*grads)

@@ -151,6 +151,11 @@ def test_clip_grad_norm(block):
     assert torch.allclose(norm[0], want, rtol=1e-6) and params[3].grad is None
     for p, r in zip(params[:3], ref):
         assert torch.allclose(p.grad, r.grad, rtol=1e-5, atol=0)
+    before = [p.grad.clone() for p in params[:3]]
+    again = block.clip_grad_norm_([params[0], params[1], params[2], params[0]], 0.35)      # a parameter twice
+    assert torch.allclose(again, torch.full_like(again, 0.7), rtol=1e-5)
+    for p, b in zip(params[:3], before):
+        assert torch.allclose(p.grad, b * 0.5, rtol=1e-5, atol=0)
     with pytest.raises(ValueError, match="no parameter"):
         block.clip_grad_norm_([params[3]], 1.0)
 

@@ -167,7 +167,7 @@ def test_gradients_that_are_not_wanted(block, dtype):
 @pytest.mark.parametrize("dtype", sorted(DTYPES))
 def test_empty_sizes(block, dtype):
     t = DTYPES[dtype]
-    for rows, d, f in ((0, 16, 24), (5, 0, 24), (5, 16, 0), (0, 0, 0)):
+    for rows, d, f in ((0, 16, 24), (5, 0, 24), (5, 16, 0), (0, 0, 0), (70, 0, 24), (300, 0, 40), (300, 16, 0)):
         x, wg, wu, grad_h = _inputs(rows, d, f, t, 7)
         h, gate, up = _forward(block, x, wg, wu, "relu")
         assert h.shape == (rows, f) and not bool(h.any())
@@ -326,6 +326,19 @@ def test_a_stash_keeps_what_relu_gates_save_compressed(block):
         kept = step()
     assert all(torch.equal(a, b) for a, b in zip(plain, kept))
     assert stash.stats["compressed"] >= 3 and stash.stats["stored_bytes"] < 0.8 * stash.stats["dense_bytes"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [(4099, 264, 4104), (4100, 4104, 264), (300, 4104, 4100), (4097, 1000, 4100)], ids=str)
+def test_more_of_the_largest_tiles_than_compute_units(block, dtype, size):
+    """Workgroups that take several tiles, whole ones and ragged ones, in each product; a summed index with and without a rest."""
+    x, wg, wu, grad_h = _inputs(*size, DTYPES[dtype], 18)
+    kept = _forward(block, x, wg, wu, "silu")
+    _check_forward(x, wg, wu, "silu", *kept)
+    alone = _forward(block, x, wg, wu, "silu", keep=False)[0]
+    assert torch.equal(alone, kept[0])
+    gate, up = kept[1].cpu(), kept[2].cpu()
+    _check_backward(grad_h, x, wg, wu, gate, up, "silu", _backward(block, grad_h, x, wg, wu, gate, up, "silu"))
 
 
 def test_addresses_beyond_32_bits(block):

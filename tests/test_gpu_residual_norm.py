@@ -76,7 +76,7 @@ def _check_forward(s, out, y, stats, post=True):
 
 SHAPES = [(1, 1, 1), (1, 4096, 1), (2, 7, 2), (3, 64, 1), (5, 1000, 5), (7, 129, 1), (8, 256, 4), (9, 513, 3), (6, 1024, 0), (33, 1999, 33), (12, 2048, 2),
           (30, 4096, 5), (10, 5001, 1), (4, 8192, 4), (6, 8200, 3), (5, 16384, 1), (3, 16383, 0), (2100, 72, 700), (3000, 40, 8), (1500, 250, 1500),
-          (1100, 136, 1), (4097, 8, 0), (2049, 24, 683)]
+          (1100, 136, 1), (4097, 8, 0), (2049, 24, 683), (6000, 40, 3000), (5001, 24, 1667), (4200, 600, 2100)]
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
@@ -330,6 +330,21 @@ def test_results_do_not_change_and_graphs_replay(block):
         calls()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, [out, y] + grads)), i
+
+
+def test_more_rows_than_a_launch_takes(block):
+    """2^23 + 3 short rows: the last ones are another launch's, and take their own gate rows."""
+    rows, cols, t = (1 << 23) + 4, 8, torch.bfloat16
+    if torch.cuda.mem_get_info()[0] < 4 << 30:
+        pytest.skip("needs 4 GiB")
+    g = torch.Generator(device="cuda").manual_seed(14)
+    x, b = (torch.randn(rows, cols, generator=g, device="cuda").to(t) for _ in range(2))
+    w, gate = torch.ones(cols, dtype=t, device="cuda"), torch.tensor([[1.0], [-2.0]], device="cuda").repeat(1, cols).to(t)
+    out, y = torch.empty_like(x), torch.empty_like(x)
+    block.bt_residual_norm_forward(x, b, w, gate, w, out, y, None, EPS, SCALE, KEEP)
+    for at in (0, rows // 2 - 2, rows // 2, rows - 4):
+        s = {"x": x[at:at + 2].cpu(), "block": b[at:at + 2].cpu(), "post_weight": w.cpu(), "gate": gate[at * 2 // rows:at * 2 // rows + 1].cpu(), "pre_weight": w.cpu()}
+        _check_forward(s, out[at:at + 2], y[at:at + 2], None)
 
 
 def test_addresses_beyond_32_bits(block):
