@@ -383,13 +383,14 @@ __global__ __launch_bounds__(NT, 4) void norm_backward_kernel(const NormBackward
 }
 
 // The runs' partial sums, added up: blockIdx.y 0 for post_weight, 1 for pre_weight, from 2 on for the gate rows ("groups" of rows) that more
-// than one run has a part of.  A thread of each wave has one column, the waves take the runs in turn.
-constexpr int kJoinWaves = 16;
+// than one run has a part of.  A workgroup has 32 columns, half a wave a run, 16 runs of each on their way at once: there are few workgroups, and what
+// they have on its way bounds them.
+constexpr int kJoinCols = 32, kJoinTeams = 32, kJoinAtOnce = 16;
 
-template <class T> __global__ __launch_bounds__(kJoinWaves * kWave) void norm_join_kernel(const NormBackward a) {
-    __shared__ float part[kJoinWaves][kWave];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const uint32_t c = blockIdx.x * kWave + lane;
+template <class T> __global__ __launch_bounds__(kJoinCols * kJoinTeams) void norm_join_kernel(const NormBackward a) {
+    __shared__ float part[kJoinTeams][kJoinCols];
+    const int lane = threadIdx.x % kJoinCols, team = threadIdx.x / kJoinCols;
+    const uint32_t c = blockIdx.x * kJoinCols + lane;
     uint32_t from = 0, to = a.runs;       // runs
     const float *parts = blockIdx.y == 0 ? a.part_post : a.part_pre;
     T *result = (T *)(blockIdx.y == 0 ? a.grad_post_weight : a.grad_pre_weight);
@@ -414,26 +415,26 @@ template <class T> __global__ __launch_bounds__(kJoinWaves * kWave) void norm_jo
     float sum = 0.0f;
     if (c < a.cols) {
         // (A gate row's part lies in the second place of the run that it begins in, in the first of the others.)
-        uint32_t run = from + wave;
-        if (blockIdx.y >= 2 && wave == 0) {
+        uint32_t run = from + team;
+        if (blockIdx.y >= 2 && team == 0) {
             sum = parts[run * pitch + a.cols + c];
-            run += kJoinWaves;
+            run += kJoinTeams;
         }
-        constexpr int kAtOnce = 8;
-        for (; run + (kAtOnce - 1) * kJoinWaves < to; run += kAtOnce * kJoinWaves) {
-            float x[kAtOnce];
+        for (; run + (kJoinAtOnce - 1) * kJoinTeams < to; run += kJoinAtOnce * kJoinTeams) {
+            float x[kJoinAtOnce];
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) x[i] = parts[(run + i * kJoinWaves) * pitch + c];
+            for (int i = 0; i < kJoinAtOnce; ++i) x[i] = parts[(run + i * kJoinTeams) * pitch + c];
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) sum += x[i];
+            for (int i = 0; i < kJoinAtOnce; ++i) sum += x[i];
         }
-        for (; run < to; run += kJoinWaves) sum += parts[run * pitch + c];
+#pragma unroll 4
+        for (; run < to; run += kJoinTeams) sum += parts[run * pitch + c];
     }
-    part[wave][lane] = sum;
+    part[team][lane] = sum;
     __syncthreads();
-    if (wave == 0 && c < a.cols) {
+    if (team == 0 && c < a.cols) {
 #pragma unroll
-        for (int w = 1; w < kJoinWaves; ++w) sum += part[w][lane];
+        for (int w = 1; w < kJoinTeams; ++w) sum += part[w][lane];
         result[c] = narrow<T>(sum);
     }
 }
@@ -787,7 +788,7 @@ bt_status bt_residual_norm_backward(const void *d_grad_out, const void *d_grad_y
         using T = decltype(type);
         const bt_status s = with_backward_shape<T>((cols + kPer<T> - 1) / kPer<T>, [&](auto kernel, const int nt) { return launch(kernel, dim3(runs), nt, (hipStream_t)stream, a); });
         if (s != BT_OK || !(d_grad_post_weight || d_grad_pre_weight || (parts && d_grad_gate))) return s;
-        return launch(norm_join_kernel<T>, dim3((unsigned)((cols + kWave - 1) / kWave), 2 + (unsigned)(!parts || !d_grad_gate ? 0 : gate_rows <= runs ? gate_rows : runs - 1)), kJoinWaves * kWave,
+        return launch(norm_join_kernel<T>, dim3((unsigned)((cols + kJoinCols - 1) / kJoinCols), 2 + (unsigned)(!parts || !d_grad_gate ? 0 : gate_rows <= runs ? gate_rows : runs - 1)), kJoinCols * kJoinTeams,
                       (hipStream_t)stream, a);
     });
 }

@@ -770,13 +770,23 @@ template <class T, Product K> __global__ __launch_bounds__(256) void gated_join_
     }
 }
 
-// Rows of `cols` elements, one behind the other, to rows of `pitch`, zeros behind them: where rows are to begin on 16-byte boundaries.
-template <class T> __global__ __launch_bounds__(256) void pad_kernel(const T *from, T *to, const uint32_t cols, const uint32_t pitch, const uint64_t vectors) {
-    const uint32_t a_row = pitch / kPer<T>;
+// Rows of `cols` elements, one behind the other, to rows of `pitch`, zeros behind them: where rows are to begin on 16-byte boundaries.  Up to
+// three matrices a launch, blockIdx.y.
+struct PadJob {
+    const void *from[3];
+    void *to[3];
+    uint32_t rows[3], cols, pitch;
+};
+
+template <class T> __global__ __launch_bounds__(256) void pad_kernel(const PadJob a) {
+    const uint32_t a_row = a.pitch / kPer<T>;
+    const uint64_t vectors = (uint64_t)a.rows[blockIdx.y] * a_row;
+    const T *const from = (const T *)a.from[blockIdx.y];
+    T *const to = (T *)a.to[blockIdx.y];
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < vectors; i += (uint64_t)gridDim.x * 256) {
         const uint64_t row = i / a_row;
         const uint32_t col = (uint32_t)(i - row * a_row) * kPer<T>;
-        store_vec(to + i * kPer<T>, kPer<T>, load_vec(from + row * cols + col, (int)(cols - col), (int)col));
+        store_vec(to + i * kPer<T>, kPer<T>, load_vec(from + row * a.cols + col, (int)(a.cols - col), (int)col));
     }
 }
 
@@ -886,11 +896,30 @@ uint64_t parts_bytes(const Product product, const uint64_t m, const uint64_t n, 
     return splits == 1 ? 0 : whole(4 * m * n * splits * (product == kGradX ? 1 : 2));
 }
 
-template <class T> void pad(const void *from, T *to, const uint64_t rows, const uint64_t cols, const uint64_t pitch, bt_status *st, hipStream_t hs) {
-    const uint64_t vectors = rows * pitch / kPer<T>, blocks = ceil_div(vectors, 256);
-    if (*st == BT_OK)
-        *st = launch(pad_kernel<T>, dim3((unsigned)(blocks < 1u << 16 ? blocks : 1u << 16)), 256, hs, (const T *)from, to, (uint32_t)cols, (uint32_t)pitch, vectors);
-}
+// What is to be copied to rows of `pitch`, and where to.
+template <class T> struct Pads {
+    PadJob job = {};
+    int count = 0;
+
+    T *add(char **ws, const void *from, const uint64_t rows, const uint64_t pitch, const bool wanted = true) {
+        T *const to = (T *)*ws;
+        *ws += whole(rows * pitch * sizeof(T));
+        if (wanted) {
+            job.from[count] = from;
+            job.to[count] = to;
+            job.rows[count++] = (uint32_t)rows;
+        }
+        return to;
+    }
+    bt_status run(const uint64_t cols, const uint64_t pitch, hipStream_t hs) {
+        job.cols = (uint32_t)cols;
+        job.pitch = (uint32_t)pitch;
+        uint64_t most = 1;
+        for (int i = 0; i < count; ++i) most = job.rows[i] > most ? job.rows[i] : most;
+        const uint64_t blocks = ceil_div(most * (pitch / kPer<T>), 256);
+        return launch(pad_kernel<T>, dim3((unsigned)(blocks < 1u << 14 ? blocks : 1u << 14), (unsigned)count), 256, hs, job);
+    }
+};
 
 // Rows of whole vectors on 16-byte boundaries, and a tile within 32 bits of offsets.
 template <class T> bool direct(const Operand &a) {
@@ -967,15 +996,11 @@ bt_status bt_gated_forward(const void *d_x, const void *d_w_gate, const void *d_
         bt_status s = BT_OK;
         if (pads(rows, d, sizeof(T))) {
             pitch = padded(d, sizeof(T));
-            const auto copy = [&](const void *from, const uint64_t n) {
-                T *const to = (T *)ws;
-                ws += whole(n * pitch * sizeof(T));
-                pad(from, to, n, d, pitch, &s, hs);
-                return to;
-            };
-            x = copy(d_x, rows);
-            w_gate = copy(d_w_gate, f);
-            w_up = copy(d_w_up, f);
+            Pads<T> copies;
+            x = copies.add(&ws, d_x, rows, pitch);
+            w_gate = copies.add(&ws, d_w_gate, f, pitch);
+            w_up = copies.add(&ws, d_w_up, f, pitch);
+            s = copies.run(d, pitch, hs);
             if (s != BT_OK) return s;
         }
         GatedJob a = {};
@@ -1042,15 +1067,11 @@ bt_status bt_gated_backward(const void *d_grad_h, const void *d_x, const void *d
         const void *x = d_x, *w_gate = d_w_gate, *w_up = d_w_up;
         if (copies) {
             pitch = padded(d, sizeof(T));
-            T *const to_x = take(rows * pitch), *const to_gate = take(f * pitch), *const to_up = take(f * pitch);
-            if (d_grad_w_gate) pad(d_x, to_x, rows, d, pitch, &s, hs);
-            if (d_grad_x) {
-                pad(d_w_gate, to_gate, f, d, pitch, &s, hs);
-                pad(d_w_up, to_up, f, d, pitch, &s, hs);
-            }
-            x = to_x;
-            w_gate = to_gate;
-            w_up = to_up;
+            Pads<T> to;
+            x = to.add(&ws, d_x, rows, pitch, d_grad_w_gate != nullptr);
+            w_gate = to.add(&ws, d_w_gate, f, pitch, d_grad_x != nullptr);
+            w_up = to.add(&ws, d_w_up, f, pitch, d_grad_x != nullptr);
+            if (s == BT_OK) s = to.run(d, pitch, hs);
         }
         if (s == BT_OK && d_grad_x) {
             GatedJob a = {};
