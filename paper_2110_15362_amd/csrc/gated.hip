@@ -161,6 +161,87 @@ template <class T, Order O, int N, int F, int kThreads> struct Staged {
     }
 };
 
+// The elements of a vector from `shift` on, zeros behind them.
+template <class T> __device__ inline raw16 moved(const raw16 v, const int shift) {
+    typedef uint64_t two __attribute__((ext_vector_type(2)));
+    const two x = __builtin_bit_cast(two, v);
+    const uint32_t bits = (uint32_t)shift * (8 * sizeof(T)), rest = bits % 64;
+    const uint64_t low = bits < 64 ? x[0] : bits < 128 ? x[1] : 0, high = bits < 64 ? x[1] : 0;
+    return __builtin_bit_cast(raw16, two{low >> rest | high << 1 << (63 - rest), high >> rest});
+}
+
+// A tile's chunks on their way to LDS like those above, but each by one load that no condition skips, so that the compiler knows how many are on their way
+// behind it: what would end beyond its row is read from further in front and moved when it is stored, and rows beyond the last are the last again.
+// Needs rows of a vector or more.
+template <class T, Order O, int N, int F, int kThreads> struct Ring {
+    typedef Tile<T, O, N> L;
+    static constexpr int PER = L::ROWS * L::CHUNKS / kThreads, E = kPer<T>;
+    uint64_t offset[O == kAlong ? PER : 1];      // of the lane's row
+    int first;                                   // the lane's column, of N as it is read
+    int shift;
+
+    __device__ static int chunk(const int i) { return i * kThreads + fresh(threadIdx.x); }
+
+    __device__ void start(const Operand &a, const bool two, const uint32_t n) {
+        static_assert(kThreads % L::CHUNKS == 0, "a lane has the same column of all its rows");
+        const int col = (int)(threadIdx.x % L::CHUNKS) * E;
+        first = col;
+        shift = 0;
+        if constexpr (O == kAlong) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                constexpr int kHalf = F * 8;
+                const int row = (i * kThreads + (int)threadIdx.x) / L::CHUNKS;
+                const uint32_t r = n + (two ? row / (2 * kHalf) * kHalf + weight_row<F>(row % kHalf) : row);
+                offset[i] = (r < a.rows ? r : a.rows - 1) * a.pitch;
+            }
+        } else {
+            first = (int)n + col;
+            const int over = first + E - (int)a.cols;
+            if (over > 0) {
+                shift = over < E ? over : E;
+                first = (int)a.cols - E;
+            }
+        }
+    }
+    // Which weight a lane's chunk belongs to, of the forward pass.
+    __device__ static bool second(const int i) { return (i * kThreads + (int)threadIdx.x) / L::CHUNKS / (F * 8) % 2 != 0; }
+
+    __device__ void load(raw16 (&v)[PER], const Operand &a, const void *other, const bool two, const uint32_t k) const {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const T *p = (const T *)a.p;
+            if (two && second(i)) p = (const T *)other;
+            if constexpr (O == kAlong) {
+                const uint32_t col = k + first, end = a.cols - E;
+                p += offset[i] + (col < end ? col : end);
+            } else {
+                const uint32_t row = k + chunk(i) / L::CHUNKS;
+                p += (row < a.rows ? row : a.rows - 1) * a.pitch + first;
+            }
+            v[i] = reinterpret_cast<const Unaligned<T> *>(p)->v;
+        }
+    }
+    // (`k`: where the tile begins that is stored.)
+    __device__ void store(char *tile, const raw16 (&v)[PER], const Operand &a, const uint32_t k) const {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int q = chunk(i);
+            raw16 x = v[i];
+            if constexpr (O == kAlong) {
+                if (k + kK<T> > a.cols) {
+                    const int over = (int)(k + first) + E - (int)a.cols;
+                    x = moved<T>(x, over < 0 ? 0 : over < E ? over : E);
+                }
+            } else {
+                x = moved<T>(x, shift);
+                if (k + kK<T> > a.rows && k + q / L::CHUNKS >= a.rows) x = raw16{0, 0, 0, 0};
+            }
+            *(raw16 *)(tile + L::place(q / L::CHUNKS, q % L::CHUNKS)) = x;
+        }
+    }
+};
+
 // 1 / (1 + exp(-g)).  Where the result is rounded to 16 bits, with the instructions for 2^x and 1 / x, whose last places are lost anyway.
 template <class T> __device__ inline float sigmoid(const float g) {
     if constexpr (sizeof(T) == 4) return 1.0f / (1.0f + expf(-g));
@@ -386,30 +467,64 @@ __device__ inline uint32_t split_start(const GatedJob &a, const uint32_t split, 
     return split == a.splits ? count : (uint32_t)((uint64_t)count * split / a.splits) & ~1u;
 }
 
-// Any alignment and any size: tiles go through registers, the next one on its way to them while one is multiplied.
-template <class T, Product K> __global__ __launch_bounds__(Small::THREADS) void gated_any_kernel(const GatedJob a) {
+// Any alignment and any size: tiles go through registers, kDeep of them on their way while one is multiplied; a tile has one of two places in LDS,
+// so that one barrier a tile is enough.  Rows of less than a vector: one tile at a time.
+template <class T, Product K> __global__ __launch_bounds__(Small::THREADS, 2) void gated_any_kernel(const GatedJob a) {
     typedef Work<T, K, Small> W;
-    __shared__ __align__(16) char tiles[W::P::BYTES + W::Q::BYTES];
+    typedef Ring<T, kOrderP<T, K>, Small::NP, Small::FP, Small::THREADS> RingP;
+    typedef Ring<T, kOrderQ<T, K>, Small::NQ, Small::FQ, Small::THREADS> RingQ;
+    constexpr int kDeep = 4;
+    __shared__ __align__(16) char tiles[2][W::P::BYTES + W::Q::BYTES];
     const Place at = place_of<K>(a, blockIdx.x, Small::NQ, W::COLS);
     typename W::Sums acc = {};
     W w;
     const uint32_t a_sum = (a.k + kK<T> - 1) / kK<T>, last = split_start(a, at.split + 1, a_sum * W::SUMS);
-    typename W::ThroughP sp;
-    typename W::ThroughQ sq;
-    const auto load = [&](const uint32_t t) {
-        const uint32_t sum = W::SUMS == 2 && t >= a_sum ? 1 : 0, k = (t - sum * a_sum) * kK<T>;
-        sp.load(a.p[sum], a.p[1], K == kForward, at.n, k);
-        sq.load(a.q[sum + at.part], a.q[sum + at.part], false, at.m, k);
-    };
     uint32_t t = split_start(a, at.split, a_sum * W::SUMS);
-    if (t < last) load(t);
-    while (t < last) {
+    const auto sum_of = [&](const uint32_t i) { return W::SUMS == 2 && i >= a_sum ? 1u : 0u; };
+    const auto start_of = [&](const uint32_t i) { return (i - sum_of(i) * a_sum) * kK<T>; };
+    if (a.p[0].cols < kPer<T> || a.q[0].cols < kPer<T>) {
+        for (; t < last; ++t) w.staged(a, a.p[sum_of(t)], a.q[sum_of(t) + at.part], at, start_of(t), tiles[0], tiles[0] + W::P::BYTES, acc);
+        W::end(a, acc, at);
+        return;
+    }
+    RingP rp;
+    RingQ rq;
+    rp.start(a.p[0], K == kForward, at.n);
+    rq.start(a.q[0], false, at.m);
+    raw16 p[kDeep][RingP::PER], q[kDeep][RingQ::PER];
+    const auto load = [&](raw16 (&to_p)[RingP::PER], raw16 (&to_q)[RingQ::PER], const uint32_t i) {
+        rp.load(to_p, a.p[sum_of(i)], a.p[1].p, K == kForward, start_of(i));
+        rq.load(to_q, a.q[sum_of(i) + at.part], nullptr, false, start_of(i));
+    };
+    const auto step = [&](const raw16 (&from_p)[RingP::PER], const raw16 (&from_q)[RingQ::PER], const int place) {
+        rp.store(tiles[place], from_p, a.p[0], start_of(t));
+        rq.store(tiles[place] + W::P::BYTES, from_q, a.q[0], start_of(t));
         __syncthreads();
-        sp.store(tiles);
-        sq.store(tiles + W::P::BYTES);
-        __syncthreads();
-        if (++t < last) load(t);
-        w.multiply_all(acc, tiles, tiles + W::P::BYTES);
+        ++t;
+    };
+    if (t + kDeep < last) {
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) load(p[j], q[j], t + j);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j)
+            if (t + j < last) load(p[j], q[j], t + j);
+    }
+#pragma unroll 1
+    while (t + kDeep < last) {
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) {
+            step(p[j], q[j], j % 2);
+            const uint32_t next = t + kDeep - 1;
+            load(p[j], q[j], next < last ? next : last - 1);
+            w.multiply_all(acc, tiles[j % 2], tiles[j % 2] + W::P::BYTES);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kDeep; ++j) {
+        if (t >= last) break;
+        step(p[j], q[j], j % 2);
+        w.multiply_all(acc, tiles[j % 2], tiles[j % 2] + W::P::BYTES);
     }
     W::end(a, acc, at);
 }
@@ -655,6 +770,7 @@ template <class T> constexpr int kUnit = 128 / (int)sizeof(T);
 
 template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) void gated_tokens_kernel(const GatedJob a) {
     constexpr int kUnits = 4;      // on their way at once
+    constexpr int kLane = sizeof(T) == 4 ? kPer<T> : 2 * kPer<T>, kNext = sizeof(T) == 4 ? 4 * kPer<T> : kPer<T>;      // from one lane's first vector to the next one's, to its second
     __shared__ float sums[kTokenWaves][2][FQ][kWave][4];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / 16, t = lane % 16;
     const uint32_t n = blockIdx.x * 16;
@@ -662,10 +778,10 @@ template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) voi
     // (Rows that are not there are others again: their results are not stored.)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        p[i] = (const T *)a.p[i].p + (n + t < a.n ? n + t : a.n - 1) * a.p[i].pitch + group * (2 * kPer<T>);
+        p[i] = (const T *)a.p[i].p + (n + t < a.n ? n + t : a.n - 1) * a.p[i].pitch + group * kLane;
     }
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) q[j] = (const T *)a.q[0].p + (uint64_t)((uint32_t)(j * 16 + t) < a.m ? j * 16 + t : a.m - 1) * a.q[0].pitch + group * (2 * kPer<T>);
+    for (int j = 0; j < FQ; ++j) q[j] = (const T *)a.q[0].p + (uint64_t)((uint32_t)(j * 16 + t) < a.m ? j * 16 + t : a.m - 1) * a.q[0].pitch + group * kLane;
     acc4 acc[2][FQ] = {};
     // The workgroups begin in different places of the summed index, or all would ask the same channels of the memory at a time.
     const uint32_t whole = a.k / kUnit<T>, shift = whole == 0 ? 0 : blockIdx.x * kTokenWaves % whole;
@@ -681,9 +797,9 @@ template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) voi
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) w[s][i][h] = reinterpret_cast<const Unaligned<T> *>(p[i] + k + h * kPer<T>)->v;
+                for (int i = 0; i < 2; ++i) w[s][i][h] = reinterpret_cast<const Unaligned<T> *>(p[i] + k + h * kNext)->v;
 #pragma unroll
-                for (int j = 0; j < FQ; ++j) x[s][j][h] = reinterpret_cast<const Unaligned<T> *>(q[j] + k + h * kPer<T>)->v;
+                for (int j = 0; j < FQ; ++j) x[s][j][h] = reinterpret_cast<const Unaligned<T> *>(q[j] + k + h * kNext)->v;
             }
         }
         __builtin_amdgcn_sched_barrier(0);      // (all of them before the first product)
@@ -701,14 +817,14 @@ template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) voi
     while (unit < whole) take(std::integral_constant<int, 1>{});
     if (wave == 0 && whole * kUnit<T> < a.k) {      // the rest, less than a unit
         const uint32_t k = whole * kUnit<T>;
-        const int left = (int)(a.k - k) - group * (2 * kPer<T>);
+        const int left = (int)(a.k - k) - group * kLane;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             raw16 w[2], x[FQ];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) w[i] = load_vec(p[i] + k + h * kPer<T>, left - h * kPer<T>, (int)a.k - left + h * kPer<T>);
+            for (int i = 0; i < 2; ++i) w[i] = load_vec(p[i] + k + h * kNext, left - h * kNext, (int)a.k - left + h * kNext);
 #pragma unroll
-            for (int j = 0; j < FQ; ++j) x[j] = load_vec(q[j] + k + h * kPer<T>, left - h * kPer<T>, (int)a.k - left + h * kPer<T>);
+            for (int j = 0; j < FQ; ++j) x[j] = load_vec(q[j] + k + h * kNext, left - h * kNext, (int)a.k - left + h * kNext);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -866,7 +982,7 @@ Plan plan_of(const Product product, const uint64_t m, const uint64_t n, const ui
             const double a_unit = (double)ceil_div(tiles * splits, 256);
             const double rate = single ? 0.8 : f.rate;
             double time = a_unit * work / (peak * rate);
-            const double alone = (double)steps / splits * f.alone * (double)ceil_div((uint64_t)a_unit, f.together);
+            const double alone = (double)steps / splits * (any ? 0.37 : f.alone) * (double)ceil_div((uint64_t)a_unit, f.together);
             if (time < alone) time = alone;
             if (splits > 1) time += 4.0 + (double)splits * m * n * outputs * 8.0 / 4e6;
             if (time < least) {
@@ -886,8 +1002,9 @@ constexpr uint64_t kTokens = 32;
 // two elements for each that a product of few rows reads anyway.)
 constexpr uint64_t kPadRows = 128;
 
-bool pads(const uint64_t rows, const uint64_t d, const int width) { return d * width % kVec != 0 && rows >= kPadRows; }
-bool any_way(const uint64_t rows, const uint64_t d, const int width) { return d * width % kVec != 0 && rows < kPadRows; }
+bool ragged(const uint64_t d, const int width) { return d * width % kVec != 0; }
+bool pads(const uint64_t rows, const uint64_t d, const int width) { return ragged(d, width) && rows >= kPadRows; }
+bool any_way(const uint64_t rows, const uint64_t d, const int width) { return ragged(d, width) && rows < kPadRows; }
 
 uint64_t whole(const uint64_t bytes) { return (bytes + 127) / 128 * 128; }
 
@@ -964,11 +1081,12 @@ size_t bt_gated_workspace_bytes(uint64_t rows, uint64_t d, uint64_t f, bt_dtype 
     const int w = width_of(dtype);
     const bool copies = pads(rows, d, w), any = any_way(rows, d, w);
     const uint64_t pitch = padded(d, w);
-    uint64_t bytes = copies ? whole(rows * pitch * w) + 2 * whole(f * pitch * w) : 0;
+    uint64_t bytes = copies || (backward && ragged(d, w)) ? whole(rows * pitch * w) : 0;
+    if (copies) bytes += 2 * whole(f * pitch * w);
     if (!backward && rows <= kTokens) return 0;
     if (!backward) return (size_t)(bytes + parts_bytes(kForward, rows, f, copies ? pitch : d, w, any));
     bytes += 2 * whole(rows * padded(f, w) * w);
-    const uint64_t x = parts_bytes(kGradX, rows, d, f, w, any), weights = parts_bytes(kGradW, f, d, rows, w, any);
+    const uint64_t x = parts_bytes(kGradX, rows, d, f, w, any), weights = parts_bytes(kGradW, f, d, rows, w, false);
     return (size_t)(bytes + (x > weights ? x : weights));
 }
 
@@ -1063,20 +1181,19 @@ bt_status bt_gated_backward(const void *d_grad_h, const void *d_x, const void *d
         bt_status s = launch(gated_slopes_kernel<T>, dim3((unsigned)(blocks < 1u << 20 ? blocks : 1u << 20)), 256, hs, (const T *)d_grad_h, (const T *)d_gate,
                              (const T *)d_up, dg, du, (uint32_t)f, (uint32_t)pitch_f, vectors, (int)activation);
         const bool copies = pads(rows, d, sizeof(T)), any = any_way(rows, d, sizeof(T));
-        uint64_t pitch = d;
         const void *x = d_x, *w_gate = d_w_gate, *w_up = d_w_up;
+        const uint64_t pitch = ragged(d, sizeof(T)) ? padded(d, sizeof(T)) : d;
+        Pads<T> to;
+        if (pitch != d) x = to.add(&ws, d_x, rows, pitch, d_grad_w_gate != nullptr);
         if (copies) {
-            pitch = padded(d, sizeof(T));
-            Pads<T> to;
-            x = to.add(&ws, d_x, rows, pitch, d_grad_w_gate != nullptr);
             w_gate = to.add(&ws, d_w_gate, f, pitch, d_grad_x != nullptr);
             w_up = to.add(&ws, d_w_up, f, pitch, d_grad_x != nullptr);
-            if (s == BT_OK) s = to.run(d, pitch, hs);
         }
+        if (s == BT_OK && to.count != 0) s = to.run(d, pitch, hs);
         if (s == BT_OK && d_grad_x) {
             GatedJob a = {};
-            a.p[0] = {w_gate, pitch, (uint32_t)f, (uint32_t)d};
-            a.p[1] = {w_up, pitch, (uint32_t)f, (uint32_t)d};
+            a.p[0] = {w_gate, copies ? pitch : d, (uint32_t)f, (uint32_t)d};
+            a.p[1] = {w_up, copies ? pitch : d, (uint32_t)f, (uint32_t)d};
             a.q[0] = {dg, pitch_f, (uint32_t)rows, (uint32_t)f};
             a.q[1] = {du, pitch_f, (uint32_t)rows, (uint32_t)f};
             a.out[0] = d_grad_x;
@@ -1097,7 +1214,7 @@ bt_status bt_gated_backward(const void *d_grad_h, const void *d_x, const void *d
             a.m = (uint32_t)f;
             a.n = (uint32_t)d;
             a.k = (uint32_t)rows;
-            s = run_product<T, kGradW>(a, plan_of(kGradW, f, d, rows, sizeof(T), any), (float *)ws, hs);
+            s = run_product<T, kGradW>(a, plan_of(kGradW, f, d, rows, sizeof(T), false), (float *)ws, hs);
         }
         return s;
     });
