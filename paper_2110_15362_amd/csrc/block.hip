@@ -36,6 +36,9 @@ template <int NT> __device__ inline float row_sum(float x, float *room) {
 //
 // A row stays in the registers of the threads that share it: NT threads hold V vectors each, vector i of thread t being number
 // i * NT + t of the row, so that the root mean squares are known before anything is read twice.
+//
+// Forward, bytes read and written at the least: x, block, out and y (bf16 [16384, 4096]: 97.5 us, 5.5 TB/s; f32 [8192, 1024]: 27.6 us, 4.9 TB/s; one row
+// of 4096: 3.4 us, the time of a launch and of one way to memory and back).
 
 struct NormForward {
     const void *x, *block, *post_weight, *gate, *pre_weight;
@@ -144,6 +147,10 @@ template <class T> __device__ inline const T *again(const T *p) {
     return p;
 }
 
+// Backward: x, block, grad_out and grad_y are read and two gradients written; the weights' are sums over the rows, which a workgroup makes in its registers
+// over a run of rows and a second kernel over the runs, in order, so that no result depends on who came first.  (f32 [8192, 1024]: 37.6 us, 5.4 TB/s;
+// bf16 [4096, 16384]: 230 us, 3.5 TB/s, where registers hold one row's vectors alone; bf16 [4095, 1999] with a gate a row, off all boundaries: 36.7 us, 3.6
+// TB/s.)
 __device__ __host__ inline uint32_t run_start(const uint32_t run, const uint32_t rows, const uint32_t runs) {
     return (uint32_t)((uint64_t)run * rows / runs);
 }
@@ -384,7 +391,7 @@ __global__ __launch_bounds__(NT, 4) void norm_backward_kernel(const NormBackward
 
 // The runs' partial sums, added up: blockIdx.y 0 for post_weight, 1 for pre_weight, from 2 on for the gate rows ("groups" of rows) that more
 // than one run has a part of.  A workgroup has 32 columns, half a wave a run, 16 runs of each on their way at once: there are few workgroups, and what
-// they have on its way bounds them.
+// they have on its way bounds them ([1024 runs, 1024], two weights: 6.0 us; one run a wave at a time and 64 columns: 9.0).
 constexpr int kJoinCols = 32, kJoinTeams = 32, kJoinAtOnce = 16;
 
 template <class T> __global__ __launch_bounds__(kJoinCols * kJoinTeams) void norm_join_kernel(const NormBackward a) {
@@ -539,6 +546,9 @@ __device__ inline double block_sum(double x, double *room) {
     return x;
 }
 
+// The norm is the square root of the sum of all squares, in 64 bits, in which no square of a 32-bit number overflows or vanishes.  Chunks of all gradients
+// go to the workgroups in turn.  Both passes are bound by memory (1.2 G elements in bf16: 416 us, 5.8 TB/s, and 939 us, 5.1 TB/s; a ResNet-50's 161
+// gradients in f32: 16 us and 32).
 __global__ __launch_bounds__(kClipThreads) void square_sum_kernel(const ClipTable a, double *const sums) {
     __shared__ double room[kClipThreads / kWave];
     double sum = 0.0;

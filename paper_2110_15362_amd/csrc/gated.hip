@@ -170,6 +170,22 @@ template <class T> __device__ inline raw16 moved(const raw16 v, const int shift)
     return __builtin_bit_cast(raw16, two{low >> rest | high << 1 << (63 - rest), high >> rest});
 }
 
+// Rows of an odd number of 16-bit elements begin off the 4-byte boundaries in turn, and a load off them takes the memory more than twice as long (bf16
+// forward of [1, 3001] x 11003: 48 us; x 3002: 30).  With a tensor that begins on one, such a vector is read from the element before it, its last
+// element by itself, and moved.  (`before`: the vector from there, `end`: the last element.)
+template <class T> __device__ inline raw16 from_odd(const raw16 before, const uint32_t end, const bool odd) {
+    const uint32_t by = odd ? 16 : 0;
+    raw16 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbit(i < 3 ? before[i < 3 ? i + 1 : 0] : end, before[i], by);
+    return v;
+}
+
+template <class T> __device__ inline uint32_t bits_at(const T *p) {
+    static_assert(sizeof(T) == 2);
+    return *(const uint16_t *)p;
+}
+
 // A tile's chunks on their way to LDS like those above, but each by one load that no condition skips, so that the compiler knows how many are on their way
 // behind it: what would end beyond its row is read from further in front and moved when it is stored, and rows beyond the last are the last again.
 // Needs rows of a vector or more.
@@ -228,6 +244,7 @@ template <class T, Order O, int N, int F, int kThreads> struct Ring {
         for (int i = 0; i < PER; ++i) {
             const int q = chunk(i);
             raw16 x = v[i];
+            asm volatile("" : "+v"(x));      // (or the vectors of the steps behind are moved, and waited for, as soon as this one)
             if constexpr (O == kAlong) {
                 if (k + kK<T> > a.cols) {
                     const int over = (int)(k + first) + E - (int)a.cols;
@@ -468,7 +485,10 @@ __device__ inline uint32_t split_start(const GatedJob &a, const uint32_t split, 
 }
 
 // Any alignment and any size: tiles go through registers, kDeep of them on their way while one is multiplied; a tile has one of two places in LDS,
-// so that one barrier a tile is enough.  Rows of less than a vector: one tile at a time.
+// so that one barrier a tile is enough.  Rows of less than a vector, and the weights' gradients, which have few tiles to sum and many workgroups to
+// wait beside each other: one tile at a time.  Bound by what loads off the boundaries cost (bf16, us: forward of [40, 3001] x 11003 56, of x 3008 on
+// them 37; with one tile on its way 138; with eight as with four) and, in single precision, by the products (forward of [100, 4001] x 16001 327 us, 78
+// TFLOP/s).
 template <class T, Product K> __global__ __launch_bounds__(Small::THREADS, 2) void gated_any_kernel(const GatedJob a) {
     typedef Work<T, K, Small> W;
     typedef Ring<T, kOrderP<T, K>, Small::NP, Small::FP, Small::THREADS> RingP;
@@ -482,7 +502,7 @@ template <class T, Product K> __global__ __launch_bounds__(Small::THREADS, 2) vo
     uint32_t t = split_start(a, at.split, a_sum * W::SUMS);
     const auto sum_of = [&](const uint32_t i) { return W::SUMS == 2 && i >= a_sum ? 1u : 0u; };
     const auto start_of = [&](const uint32_t i) { return (i - sum_of(i) * a_sum) * kK<T>; };
-    if (a.p[0].cols < kPer<T> || a.q[0].cols < kPer<T>) {
+    if (K == kGradW || a.p[0].cols < kPer<T> || a.q[0].cols < kPer<T>) {
         for (; t < last; ++t) w.staged(a, a.p[sum_of(t)], a.q[sum_of(t) + at.part], at, start_of(t), tiles[0], tiles[0] + W::P::BYTES, acc);
         W::end(a, acc, at);
         return;
@@ -502,13 +522,10 @@ template <class T, Product K> __global__ __launch_bounds__(Small::THREADS, 2) vo
         __syncthreads();
         ++t;
     };
-    if (t + kDeep < last) {
+    // (Of a short sum the last tile several times: a condition here would be one that the compiler's count of loads has to allow for in every turn.)
+    if (t < last) {
 #pragma unroll
-        for (int j = 0; j < kDeep; ++j) load(p[j], q[j], t + j);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kDeep; ++j)
-            if (t + j < last) load(p[j], q[j], t + j);
+        for (int j = 0; j < kDeep; ++j) load(p[j], q[j], t + j < last ? t + j : last - 1);
     }
 #pragma unroll 1
     while (t + kDeep < last) {
@@ -614,8 +631,9 @@ template <int LEFT> __device__ inline void wait_for_tiles() {
 // are spread among the products: each waits for the unit that takes it, and a wave that waits for that multiplies nothing.
 //
 // With the summed index along the rows a tile has half of each 128-byte line that it touches, and a line asked for a tile later is fetched again from
-// the L2 (the forward pass: 132 M lines instead of 67 M).  So the forward pass and grad_x ask for two tiles at a time, in every second one, piece by
-// piece, and have five places; the weights' gradients, whose operands lie across, ask for one tile in each and have four.
+// the L2 where that has other things to hold in between.  The forward pass in tiles of 64, whose weights nothing else reads, asks for two tiles at a time,
+// in every second one, piece by piece, and has five places (f16 forward of [37, 4096] x 11003: 50 -> 46 us); larger tiles ask for one in each and have
+// four: with two the bf16 forward pass of [16384, 2048] x 8192 took the same time, and grad_x has no registers for it.
 template <int KIND, int COUNT, int PRODUCTS, int GROUPS, int G = 0> __device__ inline void spread_kind() {
     if constexpr (G < GROUPS) {
         constexpr int c = COUNT * (G + 1) / GROUPS - COUNT * G / GROUPS, m = PRODUCTS * (G + 1) / GROUPS - PRODUCTS * G / GROUPS;
@@ -640,6 +658,11 @@ template <int N, int I = 0, class Go> __device__ inline void turn(Go go) {
     }
 }
 
+// Bound by the matrix units (and, in the largest calls, by the power that they take: they are busy for 57 to 65 % of the cycles at 1.9 GHz).  bf16,
+// tiles of 256 by 256: forward of [16384, 1024] x 4096 230 us, 1195 TFLOP/s, of [16384, 2048] x 8192 with gate and up kept 957 us, 1149; grad_x of the
+// latter 895 us, 1228, its weights' gradients 825 us, 1333; instructions for 32 by 32 results, which read half as many registers, 4 % slower;
+// four waves of 128 by 128, 667; 256 by 128, two workgroups a compute unit, 8 % slower.  Single precision, tiles of 64 by 64: [1024, 2048] x 8192 545 to 554
+// us each, 125 TFLOP/s.  Smaller sizes take smaller tiles, and parts of the sum each, so that there is work for all compute units: see plan_of.
 template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, S::FQ == 8 ? 2 : 1) void gated_kernel(const GatedJob a) {
     typedef Work<T, K, S> W;
     // Rows of a power of two of bytes all begin in the same channel of the memory, and workgroups in step would ask one after the other: each XCD
@@ -763,12 +786,14 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
 // Few rows (tokens to answer with): the weights are read once and bound the time, so they go from memory to the registers that multiply them, as many
 // vectors at once as those hold.  A workgroup has 16 columns of h, its waves take units of 128 bytes of the summed index in turn; their sums
 // meet in LDS.  In a unit a lane holds 32 bytes in a row of each operand: which summed index belongs to which lane does not matter as long as both
-// have the same.  Any alignment.  (bf16, weights of [4096, 1024], 1 row: 4.9 us, 3.4 TB/s; of [16384, 4096], 52.8 us, 5.1 TB/s; of [11008, 4096], 16 rows:
-// 42 us, 4.3 TB/s.  32 columns a workgroup, which read x half as often: 59 and 63.  From 33 rows on tiles in LDS are faster.)
+// have the same; in single precision, whose products take longer, two vectors 64 bytes apart, so that an instruction asks for whole lines (20 rows of
+// [11003, 3001]: 110 -> 84 us).  Any alignment; ODD: rows of an odd number of 16-bit elements, from a 4-byte boundary on.  (bf16, weights of [4096, 1024],
+// 1 row: 4.7 us, 3.6 TB/s; of [16384, 4096], 52.8 us, 5.1 TB/s; of [11008, 4096], 16 rows: 42 us, 4.3 TB/s.  32 columns a workgroup, which read x half
+// as often: 59 and 63.  From 33 rows on tiles in LDS are faster.)
 constexpr int kTokenWaves = 8;
 template <class T> constexpr int kUnit = 128 / (int)sizeof(T);
 
-template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) void gated_tokens_kernel(const GatedJob a) {
+template <class T, int FQ, bool ODD> __global__ __launch_bounds__(kTokenWaves * kWave) void gated_tokens_kernel(const GatedJob a) {
     constexpr int kUnits = 4;      // on their way at once
     constexpr int kLane = sizeof(T) == 4 ? kPer<T> : 2 * kPer<T>, kNext = sizeof(T) == 4 ? 4 * kPer<T> : kPer<T>;      // from one lane's first vector to the next one's, to its second
     __shared__ float sums[kTokenWaves][2][FQ][kWave][4];
@@ -782,6 +807,11 @@ template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) voi
     }
 #pragma unroll
     for (int j = 0; j < FQ; ++j) q[j] = (const T *)a.q[0].p + (uint64_t)((uint32_t)(j * 16 + t) < a.m ? j * 16 + t : a.m - 1) * a.q[0].pitch + group * kLane;
+    bool odd_p[2], odd_q[FQ];      // where a lane's vectors are read from the element before (`k` is even)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) odd_p[i] = ODD && ((uintptr_t)p[i] & 2) != 0;
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) odd_q[j] = ODD && ((uintptr_t)q[j] & 2) != 0;
     acc4 acc[2][FQ] = {};
     // The workgroups begin in different places of the summed index, or all would ask the same channels of the memory at a time.
     const uint32_t whole = a.k / kUnit<T>, shift = whole == 0 ? 0 : blockIdx.x * kTokenWaves % whole;
@@ -789,6 +819,7 @@ template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) voi
     const auto take = [&](auto many) {
         constexpr int N = decltype(many)::value;
         raw16 w[N][2][2], x[N][FQ][2];
+        uint32_t w_end[N][2], x_end[N][FQ];
 #pragma unroll
         for (int s = 0; s < N; ++s) {
             uint32_t at = unit + s * kTokenWaves + shift;
@@ -797,20 +828,37 @@ template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) voi
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) w[s][i][h] = reinterpret_cast<const Unaligned<T> *>(p[i] + k + h * kNext)->v;
+                for (int i = 0; i < 2; ++i) w[s][i][h] = reinterpret_cast<const Unaligned<T> *>(p[i] + k + h * kNext - (odd_p[i] ? 1 : 0))->v;
 #pragma unroll
-                for (int j = 0; j < FQ; ++j) x[s][j][h] = reinterpret_cast<const Unaligned<T> *>(q[j] + k + h * kNext)->v;
+                for (int j = 0; j < FQ; ++j) x[s][j][h] = reinterpret_cast<const Unaligned<T> *>(q[j] + k + h * kNext - (odd_q[j] ? 1 : 0))->v;
+            }
+            if constexpr (ODD) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) w_end[s][i] = bits_at(p[i] + k + (2 * kPer<T> - 1));
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) x_end[s][j] = bits_at(q[j] + k + (2 * kPer<T> - 1));
             }
         }
         __builtin_amdgcn_sched_barrier(0);      // (all of them before the first product)
+        const auto move = [&](raw16 (&v)[2], const uint32_t end, const bool odd) {
+            v[0] = from_odd<T>(v[0], v[1][0], odd);
+            v[1] = from_odd<T>(v[1], end, odd);
+        };
 #pragma unroll
-        for (int s = 0; s < N; ++s)
+        for (int s = 0; s < N; ++s) {
+            if constexpr (ODD) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) move(w[s][i], w_end[s][i], odd_p[i]);
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) move(x[s][j], x_end[s][j], odd_q[j]);
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int j = 0; j < FQ; ++j) acc[i][j] = multiply<T>(w[s][i][h], x[s][j][h], acc[i][j]);
+        }
         unit += N * kTokenWaves;
     };
     while (unit + (kUnits - 1) * kTokenWaves < whole) take(std::integral_constant<int, kUnits>{});
@@ -854,7 +902,8 @@ template <class T, int FQ> __global__ __launch_bounds__(kTokenWaves * kWave) voi
     }
 }
 
-// The splits' sums added up, in order, and what becomes of them.  `cells` elements of each output, which has no gaps.
+// The splits' sums added up, in order, and what becomes of them.  `cells` elements of each output, which has no gaps.  Bound by memory, and where there
+// is little by the launch (two splits of [37, 11003], forward: 4.7 us).
 template <class T, Product K> __global__ __launch_bounds__(256) void gated_join_kernel(const GatedJob a, const uint64_t cells) {
     constexpr int E = kPer<T>, kSums = K == kGradX ? 1 : 2;
     const uint64_t c = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * E;
@@ -887,7 +936,7 @@ template <class T, Product K> __global__ __launch_bounds__(256) void gated_join_
 }
 
 // Rows of `cols` elements, one behind the other, to rows of `pitch`, zeros behind them: where rows are to begin on 16-byte boundaries.  Up to
-// three matrices a launch, blockIdx.y.
+// three matrices a launch, blockIdx.y.  Bound by memory (single precision, both weights of [2731, 1001] and x of [500, 1001]: 9.1 us, 5.2 TB/s).
 struct PadJob {
     const void *from[3];
     void *to[3];
@@ -907,7 +956,8 @@ template <class T> __global__ __launch_bounds__(256) void pad_kernel(const PadJo
 }
 
 // dg = grad_h u act'(g) and du = grad_h act(g), rounded to the type: they are factors of the products, whose matrix instructions take them
-// so, and an error of half a unit in the last place of each term averages out in the sums.  Rows of `pitch` elements, whole vectors.
+// so, and an error of half a unit in the last place of each term averages out in the sums.  Rows of `pitch` elements, whole vectors.  Bound by memory
+// ([16384, 8192] in bf16: 252 us, 5.3 TB/s).
 template <class T> __global__ __launch_bounds__(256) void gated_slopes_kernel(const T *grad_h, const T *gate, const T *up, T *dg, T *du,
                                                                              const uint32_t f, const uint32_t pitch, const uint64_t vectors, const int activation) {
     const uint32_t a_row = pitch / kPer<T>;
@@ -982,9 +1032,9 @@ Plan plan_of(const Product product, const uint64_t m, const uint64_t n, const ui
             const double a_unit = (double)ceil_div(tiles * splits, 256);
             const double rate = single ? 0.8 : f.rate;
             double time = a_unit * work / (peak * rate);
-            const double alone = (double)steps / splits * (any ? 0.37 : f.alone) * (double)ceil_div((uint64_t)a_unit, f.together);
+            const double alone = (double)steps / splits * (any ? 0.3 : f.alone) * (double)ceil_div((uint64_t)a_unit, f.together);
             if (time < alone) time = alone;
-            if (splits > 1) time += 4.0 + (double)splits * m * n * outputs * 8.0 / 4e6;
+            if (splits > 1) time += (any ? 5.0 : 4.0) + (double)splits * m * n * outputs * 8.0 / 4e6;
             if (time < least) {
                 least = time;
                 best = {f.kind, splits};
@@ -1002,8 +1052,12 @@ constexpr uint64_t kTokens = 32;
 // two elements for each that a product of few rows reads anyway.)
 constexpr uint64_t kPadRows = 128;
 
+// Of x alone, for the weights' gradients (bf16, us, copied or not: [40, 3001] x 11003 87 and 65, [100, 4001] x 16001 152 and 160).
+constexpr uint64_t kPadRowsX = 96;
+
 bool ragged(const uint64_t d, const int width) { return d * width % kVec != 0; }
 bool pads(const uint64_t rows, const uint64_t d, const int width) { return ragged(d, width) && rows >= kPadRows; }
+bool pads_x(const uint64_t rows, const uint64_t d, const int width) { return ragged(d, width) && rows >= kPadRowsX; }
 bool any_way(const uint64_t rows, const uint64_t d, const int width) { return ragged(d, width) && rows < kPadRows; }
 
 uint64_t whole(const uint64_t bytes) { return (bytes + 127) / 128 * 128; }
@@ -1043,6 +1097,9 @@ template <class T> bool direct(const Operand &a) {
     return !misaligned(a.p, kVec) && a.pitch % kPer<T> == 0 && a.pitch * sizeof(T) * 320 < 1u << 31;
 }
 
+// An odd number of (16-bit) elements from each row to the next, the first on a 4-byte boundary.
+bool odd_rows(const Operand &a) { return a.pitch % 2 != 0 && !misaligned(a.p, 4); }
+
 template <class T, Product K> bt_status run_product(GatedJob &a, const Plan &plan, float *parts, hipStream_t hs) {
     bool straight = direct<T>(a.p[0]) && direct<T>(a.q[0]);
     if (K != kGradW) straight = straight && direct<T>(a.p[1]);
@@ -1081,12 +1138,12 @@ size_t bt_gated_workspace_bytes(uint64_t rows, uint64_t d, uint64_t f, bt_dtype 
     const int w = width_of(dtype);
     const bool copies = pads(rows, d, w), any = any_way(rows, d, w);
     const uint64_t pitch = padded(d, w);
-    uint64_t bytes = copies || (backward && ragged(d, w)) ? whole(rows * pitch * w) : 0;
+    uint64_t bytes = copies || (backward && pads_x(rows, d, w)) ? whole(rows * pitch * w) : 0;
     if (copies) bytes += 2 * whole(f * pitch * w);
     if (!backward && rows <= kTokens) return 0;
     if (!backward) return (size_t)(bytes + parts_bytes(kForward, rows, f, copies ? pitch : d, w, any));
     bytes += 2 * whole(rows * padded(f, w) * w);
-    const uint64_t x = parts_bytes(kGradX, rows, d, f, w, any), weights = parts_bytes(kGradW, f, d, rows, w, false);
+    const uint64_t x = parts_bytes(kGradX, rows, d, f, w, any), weights = parts_bytes(kGradW, f, d, rows, w, ragged(d, w) && !pads_x(rows, d, w));
     return (size_t)(bytes + (x > weights ? x : weights));
 }
 
@@ -1136,7 +1193,9 @@ bt_status bt_gated_forward(const void *d_x, const void *d_w_gate, const void *d_
         if (rows <= kTokens) {
             const dim3 grid((unsigned)ceil_div(f, 16));
             const auto go = [&](auto kernel) { return launch(kernel, grid, kTokenWaves * kWave, hs, a); };
-            return rows <= 16 ? go(gated_tokens_kernel<T, 1>) : go(gated_tokens_kernel<T, 2>);
+            if constexpr (sizeof(T) == 2)
+                if (odd_rows(a.p[0]) && odd_rows(a.p[1]) && odd_rows(a.q[0])) return rows <= 16 ? go(gated_tokens_kernel<T, 1, true>) : go(gated_tokens_kernel<T, 2, true>);
+            return rows <= 16 ? go(gated_tokens_kernel<T, 1, false>) : go(gated_tokens_kernel<T, 2, false>);
         }
         return run_product<T, kForward>(a, plan_of(kForward, rows, f, pitch, sizeof(T), any_way(rows, d, sizeof(T))), (float *)ws, hs);
     });
@@ -1182,9 +1241,10 @@ bt_status bt_gated_backward(const void *d_grad_h, const void *d_x, const void *d
                              (const T *)d_up, dg, du, (uint32_t)f, (uint32_t)pitch_f, vectors, (int)activation);
         const bool copies = pads(rows, d, sizeof(T)), any = any_way(rows, d, sizeof(T));
         const void *x = d_x, *w_gate = d_w_gate, *w_up = d_w_up;
-        const uint64_t pitch = ragged(d, sizeof(T)) ? padded(d, sizeof(T)) : d;
+        const bool copies_x = pads_x(rows, d, sizeof(T));
+        const uint64_t pitch = copies_x ? padded(d, sizeof(T)) : d;
         Pads<T> to;
-        if (pitch != d) x = to.add(&ws, d_x, rows, pitch, d_grad_w_gate != nullptr);
+        if (copies_x) x = to.add(&ws, d_x, rows, pitch, d_grad_w_gate != nullptr);
         if (copies) {
             w_gate = to.add(&ws, d_w_gate, f, pitch, d_grad_x != nullptr);
             w_up = to.add(&ws, d_w_up, f, pitch, d_grad_x != nullptr);
@@ -1214,7 +1274,7 @@ bt_status bt_gated_backward(const void *d_grad_h, const void *d_x, const void *d
             a.m = (uint32_t)f;
             a.n = (uint32_t)d;
             a.k = (uint32_t)rows;
-            s = run_product<T, kGradW>(a, plan_of(kGradW, f, d, rows, sizeof(T), false), (float *)ws, hs);
+            s = run_product<T, kGradW>(a, plan_of(kGradW, f, d, rows, sizeof(T), ragged(d, sizeof(T)) && !copies_x), (float *)ws, hs);
         }
         return s;
     });

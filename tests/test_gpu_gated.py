@@ -155,6 +155,18 @@ def test_tensors_off_a_16_byte_boundary(block, dtype, size, offset):
     _check_backward(grad_h, x, wg, wu, gate, up, "silu", _backward(block, grad_h, x, wg, wu, gate, up, "silu", offset=offset))
 
 
+# rows of an odd number of elements, or of less than a vector, none on a 16-byte boundary but the first: through registers, several tiles on their way
+@pytest.mark.parametrize("offset", [0, 1, 2])
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("size", [(1, 515, 100), (16, 1031, 50), (20, 129, 33), (32, 1001, 72), (40, 1001, 333), (64, 3, 40), (90, 9, 7), (100, 2003, 70), (127, 291, 601)], ids=str)
+def test_rows_off_the_boundaries(block, dtype, size, offset):
+    x, wg, wu, grad_h = _inputs(*size, DTYPES[dtype], 11 + offset)
+    kept = _forward(block, x, wg, wu, "gelu_tanh", offset=offset)
+    _check_forward(x, wg, wu, "gelu_tanh", *kept)
+    gate, up = kept[1].cpu(), kept[2].cpu()
+    _check_backward(grad_h, x, wg, wu, gate, up, "gelu_tanh", _backward(block, grad_h, x, wg, wu, gate, up, "gelu_tanh", offset=offset))
+
+
 @pytest.mark.parametrize("dtype", sorted(DTYPES))
 def test_gradients_that_are_not_wanted(block, dtype):
     x, wg, wu, grad_h = _inputs(70, 136, 88, DTYPES[dtype], 6)
