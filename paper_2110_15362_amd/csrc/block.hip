@@ -631,10 +631,18 @@ int backward_threads(const uint64_t vectors) {
     return nt;
 }
 
+// As many runs as the card holds workgroups, but of some rows each, up to four, where a run for each row would have its partial sums written and read for
+// little else; and no fewer than there are compute units.  Two sums of each column go to memory for each run: their time grows with rows * cols / (rows a
+// run), that of a run with its rows, so the rows that are best grow with the root of rows * cols.  (us, bf16, a run a row or as below: [1024, 2048] 31.0 and
+// 19.8, [2048, 2048] 35.2 and 28.5, [4096, 1024] 36.0 and 29.2; with four rows each throughout [1000, 300] 15.4 and 19.7, [64, 8192] 22.0 and 30.7.)
 uint32_t norm_runs(const uint64_t rows, const uint64_t cols, const int width) {
+    constexpr uint64_t kUnits = 256;
     const int nt = backward_threads((cols * width + kVec - 1) / kVec);
-    const uint64_t most = 256 * (nt <= 128 ? 8 : 1024 / nt);
-    return (uint32_t)(rows < most ? rows : most);
+    const uint64_t most = kUnits * (nt <= 128 ? 8 : 1024 / nt), cells = rows * cols;
+    const uint64_t a_run = cells < 360000 ? 1 : cells < 1000000 ? 2 : cells < 1960000 ? 3 : 4;
+    uint64_t runs = (rows + a_run - 1) / a_run;
+    if (runs < kUnits) runs = rows < kUnits ? rows : kUnits;
+    return (uint32_t)(runs < most ? runs : most);
 }
 
 template <class T, class Go> bt_status with_backward_shape(const uint64_t vectors, Go go) {
