@@ -364,6 +364,19 @@ template <Product K> __device__ inline Place place_of(const GatedJob &a, const u
     return at;
 }
 
+// Results of two fragments, 32 columns of 16 rows: lane l has columns 4 (l / 16) to 4 (l / 16) + 3 of each, and gets columns 8 (l / 16) to 8 (l / 16) + 7 of
+// both, so that four lanes write 64 bytes in a row.  `low`, `high`: of either fragment two results in a word.
+__device__ inline raw16 eight_neighbours(uint32_t (&low)[2], uint32_t (&high)[2]) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const auto halves = __builtin_amdgcn_permlane32_swap(low[w], high[w], false, false);
+        const auto quarters = __builtin_amdgcn_permlane16_swap(halves[0], halves[1], false, false);
+        low[w] = quarters[0];
+        high[w] = quarters[1];
+    }
+    return raw16{low[0], low[1], high[0], high[1]};
+}
+
 // What becomes of a wave's sums: rows from m on, FQ fragments of 16; columns from n on, FP fragments, of the forward pass half of them columns
 // of the gate's product and half the same columns of the other.
 template <class T, Product K, int FP, int FQ> __device__ inline void finish(const GatedJob &a, const acc4 (&acc)[FP][FQ], const uint32_t m, const uint32_t n, const Place &of) {
@@ -372,6 +385,21 @@ template <class T, Product K, int FP, int FQ> __device__ inline void finish(cons
 #pragma unroll
     for (int j = 0; j < FQ; ++j) {
         const uint32_t row = m + j * 16 + lane % 16;
+        if constexpr (K != kForward && sizeof(T) == 2) {
+            // Where rows begin on 64-byte boundaries (us, weights' gradients with 8 or 64 bytes in a row: [40, 3008] x 11008 66 and 49, [96, 4096] x 16384 98 and 76;
+            // but of [1, 4008] x 16008, whose rows do not, 71 and 84).  All lanes take part, those beyond the last row too.
+            if (!parts && a.pitch % 32 == 0) {
+#pragma unroll
+                for (int i = 0; i < FP; i += 2) {
+                    uint32_t low[2] = {pack2<T>(acc[i][j][0], acc[i][j][1]), pack2<T>(acc[i][j][2], acc[i][j][3])};
+                    uint32_t high[2] = {pack2<T>(acc[i + 1][j][0], acc[i + 1][j][1]), pack2<T>(acc[i + 1][j][2], acc[i + 1][j][3])};
+                    const raw16 v = eight_neighbours(low, high);
+                    const uint32_t col = n + i * 16 + lane / 16 * 8;
+                    if (row < a.m) store_vec((T *)a.out[of.part] + row * a.pitch + col, (int)(a.n - col), v);
+                }
+                continue;
+            }
+        }
         if (row >= a.m) continue;
         if constexpr (K == kForward) {
             constexpr int N = 2 * FP;      // neighbours that the lane has
