@@ -689,8 +689,8 @@ template <int N, int I = 0, class Go> __device__ inline void turn(Go go) {
 // Bound by the matrix units (and, in the largest calls, by the power that they take: they are busy for 57 to 65 % of the cycles at 1.9 GHz).  bf16,
 // tiles of 256 by 256: forward of [16384, 1024] x 4096 230 us, 1195 TFLOP/s, of [16384, 2048] x 8192 with gate and up kept 957 us, 1149; grad_x of the
 // latter 895 us, 1228, its weights' gradients 825 us, 1333; instructions for 32 by 32 results, which read half as many registers, 4 % slower;
-// four waves of 128 by 128, 667; 256 by 128, two workgroups a compute unit, 8 % slower.  Single precision, tiles of 64 by 64: [1024, 2048] x 8192 545 to 554
-// us each, 125 TFLOP/s.  Smaller sizes take smaller tiles, and parts of the sum each, so that there is work for all compute units: see plan_of.
+// four waves of 128 by 128, 667; 256 by 128, two workgroups a compute unit, 8 % slower.  Single precision, tiles of 64 by 64: [1024, 2048] x 8192 537 to 554
+// us each, 126 TFLOP/s.  Smaller sizes take smaller tiles, and parts of the sum each, so that there is work for all compute units: see plan_of.
 template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, S::FQ == 8 ? 2 : 1) void gated_kernel(const GatedJob a) {
     typedef Work<T, K, S> W;
     // Rows of a power of two of bytes all begin in the same channel of the memory, and workgroups in step would ask one after the other: each XCD
@@ -933,7 +933,8 @@ template <class T, int FQ, bool ODD> __global__ __launch_bounds__(kTokenWaves * 
 // The splits' sums added up, in order, and what becomes of them.  `cells` elements of each output, which has no gaps.  Bound by memory, and where there
 // is little by the launch (two splits of [37, 11003], forward: 4.7 us).
 // Several splits are on their way at once (a power of two, as their number is); small sums go to workgroups of one wave, for there to be some on all compute
-// units (16 splits of [64, 1001], grad_x: 7.6 us one split at a time with 256 threads, 4.6 now; 8 of [1024, 2048], bound by memory: 12.0 with 256 threads, 13.0 with 64).
+// units (16 splits of [64, 1001], grad_x: 7.6 us one split at a time with 256 threads, 4.0 now; 8 of [1024, 2048], bound by memory: 12.0 to 12.6 with 256 threads, 13.0 with
+// 64).
 template <class T, Product K> __global__ __launch_bounds__(256) void gated_join_kernel(const GatedJob a, const uint64_t cells) {
     constexpr int E = kPer<T>, kSums = K == kGradX ? 1 : 2;
     const uint64_t c = ((uint64_t)blockIdx.x * blockDim.x + threadIdx.x) * E;
