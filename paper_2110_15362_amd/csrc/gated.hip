@@ -377,6 +377,13 @@ __device__ inline raw16 eight_neighbours(uint32_t (&low)[2], uint32_t (&high)[2]
     return raw16{low[0], low[1], high[0], high[1]};
 }
 
+// Fragments of which a lane writes its results together, where that is done.
+constexpr int kTogether = 2;
+
+// Stores that a lane makes of each output (h, gate, up; a gradient; a split's sums), in the function below, of a tile that lies inside the output: at the least, since
+// it also stores smaller pieces.  What a wait that counts them may rely on: one that counts on more than there are waits for nothing.
+template <class T, Product K, int FP, int FQ> constexpr int kStoresAtLeast = K == kForward ? FQ : sizeof(T) == 2 ? FQ * (FP / kTogether) : FQ * FP;
+
 // What becomes of a wave's sums: rows from m on, FQ fragments of 16; columns from n on, FP fragments, of the forward pass half of them columns
 // of the gate's product and half the same columns of the other.
 template <class T, Product K, int FP, int FQ> __device__ inline void finish(const GatedJob &a, const acc4 (&acc)[FP][FQ], const uint32_t m, const uint32_t n, const Place &of) {
@@ -389,8 +396,9 @@ template <class T, Product K, int FP, int FQ> __device__ inline void finish(cons
             // Where rows begin on 64-byte boundaries (us, weights' gradients with 8 or 64 bytes in a row: [40, 3008] x 11008 66 and 49, [96, 4096] x 16384 98 and 76;
             // but of [1, 4008] x 16008, whose rows do not, 71 and 84).  All lanes take part, those beyond the last row too.
             if (!parts && a.pitch % 32 == 0) {
+                static_assert(kStoresAtLeast<T, K, FP, FQ> <= FQ * (FP / kTogether));
 #pragma unroll
-                for (int i = 0; i < FP; i += 2) {
+                for (int i = 0; i < FP; i += kTogether) {
                     uint32_t low[2] = {pack2<T>(acc[i][j][0], acc[i][j][1]), pack2<T>(acc[i][j][2], acc[i][j][3])};
                     uint32_t high[2] = {pack2<T>(acc[i + 1][j][0], acc[i + 1][j][1]), pack2<T>(acc[i + 1][j][2], acc[i + 1][j][3])};
                     const raw16 v = eight_neighbours(low, high);
@@ -403,6 +411,7 @@ template <class T, Product K, int FP, int FQ> __device__ inline void finish(cons
         if (row >= a.m) continue;
         if constexpr (K == kForward) {
             constexpr int N = 2 * FP;      // neighbours that the lane has
+            static_assert(kStoresAtLeast<T, K, FP, FQ> <= FQ * ((N + kPer<T> - 1) / kPer<T>));
             const uint32_t col = n + lane / 16 * N;
             const int left = (int)(a.n - col);
             const uint64_t at = row * a.pitch + col;
@@ -426,6 +435,7 @@ template <class T, Product K, int FP, int FQ> __device__ inline void finish(cons
                 store_run<T, N>((T *)a.up + at, left, u);
             }
         } else {
+            static_assert(kStoresAtLeast<T, K, FP, FQ> <= FQ * FP);
 #pragma unroll
             for (int i = 0; i < FP; ++i) {
                 const uint32_t col = n + i * 16 + lane / 16 * 4;
@@ -737,8 +747,8 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
     uint32_t number = blockIdx.x;
     Place at = place_of<K>(a, number, S::NQ, W::COLS);
     uint32_t count = begin(at, 0);
-    bool stored = false;      // since the first tiles were asked for: kStores results of each lane, exactly
-    constexpr int kStores = K == kForward ? S::FQ : S::FP * S::FQ;
+    bool stored = false;      // since the first tiles were asked for: by each lane, kStores of each output or more
+    constexpr int kStores = kStoresAtLeast<T, K, S::FP, S::FQ>;
     for (;;) {
         typename W::Sums acc = {};
         // Tile i of a turn, which lies in place i % kPlaces, with `left` tiles from it to the end.
@@ -775,10 +785,11 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
                 count = begin(at, sum);
             }
             if (count != 0) {
-                // (Fetches and stores are counted together, in order.)
+                // The first tile of every wave has to be in LDS.  Fetches and stores are counted together, in order: of those that may still be on their way,
+                // the first tile's fetches are followed by those of kLeft tiles and by the stores.
                 if (count < kAhead) wait_for_tiles<0>();
                 else if (!stored || sum != 0) wait_for_tiles<kLeft * kFetches>();
-                else if (K == kForward && a.gate) wait_for_tiles<kLeft * kFetches + (K == kForward ? 3 : 1) * kStores>();
+                else if (K == kForward && a.gate && !a.parts) wait_for_tiles<kLeft * kFetches + (K == kForward ? 3 : 1) * kStores>();
                 else wait_for_tiles<kLeft * kFetches + kStores>();
                 w.read_p(tile_p(0), 0);
                 w.read_q(tile_q(0), 0);
@@ -804,6 +815,7 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
             if (through) __syncthreads();
             at = place_of<K>(a, number, S::NQ, W::COLS);
             count = begin(at, 0);
+            asm volatile("" ::: "memory");      // (the stores stay behind the fetches: see the wait that counts both)
         }
         W::end(a, acc, here);
         if (!more) break;

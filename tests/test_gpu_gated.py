@@ -353,6 +353,22 @@ def test_more_of_the_largest_tiles_than_compute_units(block, dtype, size):
     _check_backward(grad_h, x, wg, wu, gate, up, "silu", _backward(block, grad_h, x, wg, wu, gate, up, "silu"))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [(6144, 4096, 160), (6200, 4128, 296), (288, 4096, 4352), (300, 4096, 4100), (512, 4128, 4112)], ids=str)
+def test_several_of_the_largest_tiles_with_results_written_together(block, dtype, size):
+    """Rows that begin on 64-byte boundaries, where a lane writes the results of two fragments at once: grad_x (the first two sizes) and the weights' gradients
+    (the others) in more than 256 of the largest tiles, whole ones and ragged ones, each with several steps of the summed index.  Equal bits
+    the second time."""
+    x, wg, wu, grad_h = _inputs(*size, DTYPES[dtype], 19)
+    kept = _forward(block, x, wg, wu, "silu")
+    _check_forward(x, wg, wu, "silu", *kept)
+    gate, up = kept[1].cpu(), kept[2].cpu()
+    grads = _backward(block, grad_h, x, wg, wu, gate, up, "silu")
+    _check_backward(grad_h, x, wg, wu, gate, up, "silu", grads)
+    again = _backward(block, grad_h, x, wg, wu, gate, up, "silu")
+    assert all(torch.equal(a, b) for a, b in zip(grads, again))
+
+
 def test_addresses_beyond_32_bits(block):
     """h of more than 2^32 bytes and of more than 2^31 elements: the last rows are where they belong."""
     t, rows, d, f = torch.bfloat16, 70000, 8, 32768
