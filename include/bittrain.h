@@ -397,7 +397,7 @@ bt_status bt_workspace_status(const void *d_workspace, uint32_t *d_status, bt_st
 typedef enum {
     BT_ACT_RELU = 0,     /* act(g) = g where g > 0 (or g is a NaN), else 0 */
     BT_ACT_SILU = 1,     /* act(g) = g / (1 + exp(-g)) */
-    BT_ACT_GELU_TANH = 2 /* act(g) = g / 2 * (1 + tanh(sqrt(2 / pi) * (g + 0.044715 g^3))) */
+    BT_ACT_GELU_TANH = 2 /* act(g) = g / 2 * (1 + tanh(sqrt(2 / pi) * (g + 0.044715 g^3))); both are 0 at -infinity, with a slope of 0 */
 } bt_activation;
 
 /* Largest numbers of rows and of features that these calls accept. */

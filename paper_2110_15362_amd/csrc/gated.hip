@@ -265,12 +265,13 @@ template <class T> __device__ inline float sigmoid(const float g) {
     else return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g));
 }
 
-// act(g) and its derivative, of SiLU and of the GELU, whose (1 + tanh(y)) / 2 is sigmoid(2 y).
+// act(g) and its derivative, of SiLU and of the GELU, whose (1 + tanh(y)) / 2 is sigmoid(2 y).  Where the sigmoid is 0 or 1 it is the derivative, and 0 is act(g): the
+// other factors, g^2 and g^3 among them, may be infinite there (and g, where it was rounded to 16 bits), and 0 times them is a NaN.
 constexpr float kGelu = 1.5957691216057308f, kGeluCube = 0.044715f;      // 2 sqrt(2 / pi)
 
 template <class T> __device__ inline float activate(const int activation, const float g) {
-    if (activation == BT_ACT_SILU) return g * sigmoid<T>(g);
-    return g * sigmoid<T>(kGelu * (g + kGeluCube * g * g * g));
+    const float s = sigmoid<T>(activation == BT_ACT_SILU ? g : kGelu * (g + kGeluCube * g * g * g));
+    return s == 0.0f ? -0.0f : g * s;
 }
 
 template <class T> __device__ inline void activate(const int activation, const float g, float *value, float *slope) {
@@ -280,8 +281,8 @@ template <class T> __device__ inline void activate(const int activation, const f
         s = sigmoid<T>(kGelu * (g + kGeluCube * g * g * g));
         inner = kGelu * (1.0f + 3.0f * kGeluCube * g * g);
     }
-    *value = g * s;
-    *slope = s * (1.0f + g * (1.0f - s) * inner);
+    *value = s == 0.0f ? -0.0f : g * s;
+    *slope = s == 0.0f || s == 1.0f ? s : s * (1.0f + g * (1.0f - s) * inner);
 }
 
 // h of both products; with ReLU what is kept of them where the gate is closed is 0 too.

@@ -226,6 +226,30 @@ def test_values_at_the_ends_of_the_range(block):
             within(grads[1][:, 0], slope, torch.full_like(slope, 1e-6), "slope")
 
 
+@pytest.mark.parametrize("activation", ["silu", "gelu_tanh"])
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+def test_slopes_where_an_activation_is_done(block, dtype, activation):
+    """Gates from where the activation is 0 or the gate itself to the ends of the type's range, and those that its rounding takes to an infinity: slopes of 0 and 1,
+    not products with infinities.  (2 |g| is finite in 32 bits; the gate is kept in the type.)"""
+    t = DTYPES[dtype]
+    size = torch.tensor([200.0, 3e4, 65504.0] if dtype == "f16" else [200.0, 1e7, 1e13, 1e16, 1.8e19, 6e19, 1e25, 1e30, 1.6e38]).to(t)
+    for sign in (-1.0, 1.0):
+        wg = (sign * size)[:, None].repeat(1, 2).contiguous()
+        x, wu = torch.ones(1, 2, dtype=t), torch.full((len(size), 2), 0.5, dtype=t)
+        for terms in (1, 2):                                 # g = +-size and twice that: an infinity in f16
+            x[0, 1] = terms - 1
+            h, gate, up = _forward(block, x, wg, wu, activation)
+            value = terms * size.double() * (sign > 0)
+            want = value * terms / 2
+            want[want > torch.finfo(t).max] = float("inf")
+            within(h[0], want, rounded(want, t, 2.0 ** -17 * value), "h")
+            grads = _backward(block, torch.ones(1, len(size), dtype=t), x, wg, wu, gate.cpu(), up.cpu(), activation)
+            slope = torch.full((len(size), 1), float(sign > 0), dtype=torch.float64) * terms / 2
+            within(grads[1][:, :1], slope, rounded(slope, t, 2.0 ** -17 * slope), "grad_w_gate")
+            kept = torch.where(gate[0].cpu().double() > 0, gate[0].cpu().double(), 0.0)[:, None]
+            within(grads[2][:, :1], kept, rounded(kept, t, 2.0 ** -17 * kept), "grad_w_up")
+
+
 @pytest.mark.parametrize("activation", ["relu", "silu", "gelu_tanh"])
 def test_autograd_against_differences(block, activation):
     """The directional derivative of a weighted sum of the definition, in 64 bits by central differences, and by the gradients.  (A difference over
