@@ -416,7 +416,8 @@ size_t bt_gated_workspace_bytes(uint64_t rows, uint64_t d, uint64_t f, bt_dtype 
  *   d_gate, d_up      [rows, f] each, or NULL both: what bt_gated_backward needs of this pass, rounded to the
  *                     tensors' type: the pre-activations x w_gate^T and x w_up^T.  With BT_ACT_RELU act(x w_gate^T) and, where
  *                     that is not 0, x w_up^T, else +0: then h, gate and up are all +0 wherever a gate is closed and
- *                     compress as one.
+ *                     compress as one.  (A gate that is open is kept as a number above 0, the smallest at the least, where
+ *                     rounding would give 0.)
  * With BT_ACT_RELU h is +0 where the gate is closed, whatever the other factor is there (a select, never a multiply).
  * rows == 0 or f == 0 does nothing; with d == 0 the products are 0.  No output may overlap an input or another output.
  * Errors: BT_ERR_NULL, BT_ERR_DTYPE (BT_F64 too), BT_ERR_ALIGN, BT_ERR_SIZE, BT_ERR_WORKSPACE, BT_ERR_HIP, BT_ERR_ARGUMENT

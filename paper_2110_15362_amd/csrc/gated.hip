@@ -285,12 +285,18 @@ template <class T> __device__ inline void activate(const int activation, const f
     *slope = s == 0.0f || s == 1.0f ? s : s * (1.0f + g * (1.0f - s) * inner);
 }
 
-// h of both products; with ReLU what is kept of them where the gate is closed is 0 too.
+// The smallest number above 0 that T holds.
+template <class T> constexpr float kLeast = 0x1p-149f;
+template <> constexpr float kLeast<f16> = 0x1p-24f;
+template <> constexpr float kLeast<bf16> = 0x1p-133f;
+
+// h of both products; with ReLU what is kept of them where the gate is closed is 0 too.  An open gate that T would round to 0 is kept as the smallest number
+// instead: the backward pass, which has the rounded one, is to find it open.
 template <class T> __device__ inline float gated(const int activation, float &g, float &u) {
     if (activation != BT_ACT_RELU) return activate<T>(activation, g) * u;
     const bool closed = g <= 0.0f;
     const float h = closed ? 0.0f : g * u;
-    g = closed ? 0.0f : g;
+    g = closed ? 0.0f : g < kLeast<T> ? kLeast<T> : g;
     u = closed ? 0.0f : u;
     return h;
 }

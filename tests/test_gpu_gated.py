@@ -210,6 +210,23 @@ def test_a_closed_relu_gate_selects(block, dtype):
             assert not any(bool(v.any()) for v in grads)
 
 
+@pytest.mark.parametrize("size", [(1, 8, 16), (20, 9, 40), (40, 11, 7), (64, 4096, 72), (200, 40, 136)], ids=str)
+def test_a_relu_gate_that_f16_does_not_hold_stays_open(block, size):
+    """A pre-activation of 2^-26, which f16 rounds to 0: the gate is open, and its gradient is grad_h * u."""
+    rows, d, f = size
+    x, wg, wu = (torch.zeros(s, dtype=torch.float16) for s in ((rows, d), (f, d), (f, d)))
+    x[:, 0], wg[:, 0], wu[:, 0] = 2.0 ** -13, 2.0 ** -13, 2.0 ** 13
+    wg[1::2, 0] = -(2.0 ** -13)                              # (every other one is closed)
+    h, gate, up = _forward(block, x, wg, wu, "relu")
+    open_ = (torch.arange(f) % 2 == 0).expand(rows, f)
+    assert not bool(h.any()) and torch.equal(gate.cpu() > 0, open_) and torch.equal(up.cpu(), open_.half())
+    assert bool((gate.cpu().double() <= 2.0 ** -24).all())   # the smallest number that is not 0
+    grads = _backward(block, torch.ones(rows, f, dtype=torch.float16), x, wg, wu, gate.cpu(), up.cpu(), "relu")
+    want = torch.zeros(f, d, dtype=torch.float64)
+    want[::2, 0] = rows * 2.0 ** -13
+    within(grads[1], want, rounded(want, torch.float16, (rows + 1) * SUM * want), "grad_w_gate")
+
+
 def test_values_at_the_ends_of_the_range(block):
     """Pre-activations that exp takes to infinity or 0: the activations are 0 or the argument itself there."""
     for dtype in (torch.float32, torch.bfloat16):
