@@ -341,6 +341,7 @@ struct GatedJob {
     uint32_t tiles_n, tiles_m;       // of each output
     uint32_t splits;                 // parts of the summed index, each of other workgroups
     uint32_t groups;                 // tiles of all outputs and splits
+    uint32_t first, end;             // those of them that the launch has
     float *parts;                    // their sums, [splits, 2 of the forward pass and the weights' gradients, m, n]; with one split NULL
     int activation;
 };
@@ -540,7 +541,7 @@ template <class T, Product K> __global__ __launch_bounds__(Small::THREADS, 2) vo
     typedef Ring<T, kOrderQ<T, K>, Small::NQ, Small::FQ, Small::THREADS> RingQ;
     constexpr int kDeep = 4;
     __shared__ __align__(16) char tiles[2][W::P::BYTES + W::Q::BYTES];
-    const Place at = place_of<K>(a, blockIdx.x, Small::NQ, W::COLS);
+    const Place at = place_of<K>(a, a.first + blockIdx.x, Small::NQ, W::COLS);
     typename W::Sums acc = {};
     W w;
     const uint32_t a_sum = (a.k + kK<T> - 1) / kK<T>, last = split_start(a, at.split + 1, a_sum * W::SUMS);
@@ -751,7 +752,7 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
     };
     // Workgroups of the largest tiles, one to a compute unit, take several: the next one's first tiles of the summed index are asked for before
     // the results of this one are worked out and stored.
-    uint32_t number = blockIdx.x;
+    uint32_t number = a.first + blockIdx.x;
     Place at = place_of<K>(a, number, S::NQ, W::COLS);
     uint32_t count = begin(at, 0);
     bool stored = false;      // since the first tiles were asked for: by each lane, kStores of each output or more
@@ -817,7 +818,7 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
         }
         const Place here = at;
         number += gridDim.x;
-        const bool more = number < a.groups;
+        const bool more = number < a.end;
         if (more) {
             if (through) __syncthreads();
             at = place_of<K>(a, number, S::NQ, W::COLS);
@@ -1183,11 +1184,19 @@ template <class T, Product K> bt_status run_product(GatedJob &a, const Plan &pla
         typedef decltype(shape) S;
         const uint64_t tiles_m = ceil_div(a.m, S::NQ), tiles_n = ceil_div(a.n, K == kForward ? S::NP / 2 : S::NP);
         const uint64_t groups = tiles_m * tiles_n * (K == kGradW ? 2 : 1) * a.splits;
-        if (groups >= 1u << 23) return BT_ERR_SIZE;      // (a grid holds less than 2^32 threads)
+        if (groups >= 1u << 31) return BT_ERR_SIZE;      // (outputs of terabytes)
         a.tiles_m = (uint32_t)tiles_m;
         a.tiles_n = (uint32_t)tiles_n;
         a.groups = (uint32_t)groups;
-        return launch(kernel, dim3((unsigned)(S::THREADS == Large::THREADS && groups > 256 ? 256 : groups)), S::THREADS, hs, a);
+        constexpr bool kSeveral = S::THREADS == Large::THREADS;      // tiles to a workgroup, 256 of those at the most
+        constexpr uint32_t kMost = kSeveral ? 1u << 31 : 1u << 22;   // of a launch: a grid holds less than 2^32 threads
+        bt_status s = BT_OK;
+        for (a.first = 0; a.first < a.groups && s == BT_OK; a.first = a.end) {
+            a.end = a.groups - a.first < kMost ? a.groups : a.first + kMost;
+            const uint32_t here = a.end - a.first;
+            s = launch(kernel, dim3(kSeveral && here > 256 ? 256 : here), S::THREADS, hs, a);
+        }
+        return s;
     };
     bt_status st = BT_OK;
     if (!straight || plan.kind == kAnyKind) st = go(gated_any_kernel<T, K>, Small{});

@@ -410,6 +410,21 @@ def test_several_of_the_largest_tiles_with_results_written_together(block, dtype
     assert all(torch.equal(a, b) for a, b in zip(grads, again))
 
 
+@pytest.mark.parametrize("dtype,offset", [("f32", 0), ("bf16", 1)])
+def test_outputs_of_more_tiles_than_a_launch_takes(block, dtype, offset):
+    """2^23 tiles of 64 by 32 and more, of aligned tensors and, through the kernel for any alignment, of others: the last rows are another launch's."""
+    t, rows, d, f = DTYPES[dtype], (1 << 20) + 70, 24, 1 << 14
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GiB")
+    g = torch.Generator(device="cuda").manual_seed(20)
+    x = torch.randn(rows * d + offset, generator=g, device="cuda").to(t)[offset:].view(rows, d)
+    wg, wu = (torch.randn(f, d, generator=g, device="cuda").to(t) for _ in range(2))
+    h = torch.empty(rows, f, dtype=t, device="cuda")
+    block.bt_gated_forward(x, wg, wu, "relu", h, None, None, block.new_gated_workspace(rows, d, f, t))
+    for at in (0, (1 << 19) - 2, (1 << 19) + 62, 1 << 20, rows - 3):
+        _check_forward(x[at:at + 3].cpu(), wg.cpu(), wu.cpu(), "relu", h[at:at + 3])
+
+
 def test_addresses_beyond_32_bits(block):
     """h of more than 2^32 bytes and of more than 2^31 elements: the last rows are where they belong."""
     t, rows, d, f = torch.bfloat16, 70000, 8, 32768
