@@ -152,13 +152,18 @@ def _plain(t):
     return None if t is None else t.contiguous().resolve_neg()
 
 
+def _keep(*tensors):
+    """Whether a backward pass will want something of a call on `tensors`.  (Inside of a Function gradients are always off, and its needs_input_grad
+    does not know of no_grad.)"""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
 class _GatedLinear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w_gate, w_up, activation):
+    def forward(ctx, x, w_gate, w_up, activation, keep):
         x, w_gate, w_up = _plain(x), _plain(w_gate), _plain(w_up)
         rows, d, f = x.shape[:-1].numel(), x.shape[-1], w_gate.shape[0]
         h = x.new_empty(x.shape[:-1] + (f,))
-        keep = any(ctx.needs_input_grad[:3])
         gate, up = (torch.empty_like(h), torch.empty_like(h)) if keep else (None, None)
         workspace = new_gated_workspace(rows, d, f, x.dtype, device=x.device)
         bt_gated_forward(x, w_gate, w_up, activation, h, gate, up, workspace)
@@ -184,33 +189,32 @@ class _GatedLinear(torch.autograd.Function):
         rows = x.shape[:-1].numel()
         workspace = new_gated_workspace(rows, x.shape[-1], w_gate.shape[0], x.dtype, backward=True, device=x.device)
         bt_gated_backward(grad_h, x, w_gate, w_up, gate, up, ctx.activation, grad_x, grad_w_gate, grad_w_up, workspace)
-        return grad_x, grad_w_gate if ctx.needs_input_grad[1] else None, grad_w_up if ctx.needs_input_grad[2] else None, None
+        return grad_x, grad_w_gate if ctx.needs_input_grad[1] else None, grad_w_up if ctx.needs_input_grad[2] else None, None, None
 
 
 def gated_linear(x, w_gate, w_up, activation="relu"):
     """act(x w_gate^T) * (x w_up^T): the gated half of a feed-forward block, with its gradient.  x [..., d], weights [f, d], all of one type."""
     _activation(activation)
     _check_device(x, w_gate, w_up)
+    args = x, w_gate, w_up, activation, _keep(x, w_gate, w_up)
     if _elsewhere(x):
         with torch.cuda.device(x.device):
-            return _GatedLinear.apply(x, w_gate, w_up, activation)
-    return _GatedLinear.apply(x, w_gate, w_up, activation)
+            return _GatedLinear.apply(*args)
+    return _GatedLinear.apply(*args)
 
 
 class _ResidualNorm(torch.autograd.Function):
     """(x, block, post_weight, gate, pre_weight) -> (out, y), either None where there is none."""
 
     @staticmethod
-    def forward(ctx, x, block, post_weight, gate, pre_weight, eps, scale, residual_scale):
+    def forward(ctx, x, block, post_weight, gate, pre_weight, eps, scale, residual_scale, keep):
         x, block, post_weight, gate, pre_weight = (_plain(t) for t in (x, block, post_weight, gate, pre_weight))
         rows = x.shape[:-1].numel()
         out = None if block is None else torch.empty_like(x)
         y = None if pre_weight is None else torch.empty_like(x)
-        stats = None
-        if any(ctx.needs_input_grad[:5]):
-            stats = torch.empty(2, rows, dtype=torch.float32, device=x.device)
+        stats = torch.empty(2, rows, dtype=torch.float32, device=x.device) if keep else None
         bt_residual_norm_forward(x, block, post_weight, gate, pre_weight, out, y, stats, eps, scale, residual_scale)
-        if stats is not None:
+        if keep:
             ctx.scales = scale, residual_scale
             ctx.set_materialize_grads(False)
             ctx.save_for_backward(x if block is None else out, block, post_weight, gate, pre_weight, stats)
@@ -228,7 +232,7 @@ class _ResidualNorm(torch.autograd.Function):
     @staticmethod
     def _gradients(ctx, grad_out, grad_y, out, block, post_weight, gate, pre_weight, stats):
         if grad_out is None and grad_y is None:
-            return (None,) * 8
+            return (None,) * 9
         needs, scale, residual_scale = ctx.needs_input_grad, *ctx.scales
         like = lambda t, i: torch.empty_like(t) if t is not None and needs[i] else None  # noqa: E731
         grads = like(out, 0), like(block, 1), like(post_weight, 2), like(gate, 3), like(pre_weight, 4)
@@ -240,7 +244,7 @@ class _ResidualNorm(torch.autograd.Function):
         workspace = new_residual_norm_workspace(rows, cols, 0 if gate is None else gate.numel() // max(cols, 1), out.dtype, device=out.device)
         bt_residual_norm_backward(grad_out, grad_y, out, block, post_weight, gate, pre_weight, stats, grads[0], grads[1], grads[2], grads[3],
                                   grads[4] if grad_y is not None else None, workspace, scale, residual_scale)
-        return grads + (None, None, None)
+        return grads + (None, None, None, None)
 
 
 def _gate_matrix(gate, cols):
@@ -258,7 +262,7 @@ def residual_norm(x, block, post_weight=None, gate=None, pre_weight=None, eps=1e
         raise ValueError("block must have the shape of x")
     if gate is not None and (gate.dim() == 0 or gate.shape[-1] != x.shape[-1]):
         raise ValueError("gate must have the last dimension of x")
-    args = x, block, post_weight, _gate_matrix(gate, x.shape[-1]), pre_weight, eps, scale, residual_scale
+    args = x, block, post_weight, _gate_matrix(gate, x.shape[-1]), pre_weight, eps, scale, residual_scale, _keep(x, block, post_weight, gate, pre_weight)
     if _elsewhere(x):
         with torch.cuda.device(x.device):
             return _ResidualNorm.apply(*args)
@@ -268,10 +272,11 @@ def residual_norm(x, block, post_weight=None, gate=None, pre_weight=None, eps=1e
 def rms_norm(x, weight, eps=1e-6):
     """x / sqrt(mean(x^2) + eps) * weight over the last dimension: the norm before the first block."""
     _check_device(x, weight)
+    args = x, None, None, None, weight, eps, 1.0, 1.0, _keep(x, weight)
     if _elsewhere(x):
         with torch.cuda.device(x.device):
-            return _ResidualNorm.apply(x, None, None, None, weight, eps, 1.0, 1.0)[1]
-    return _ResidualNorm.apply(x, None, None, None, weight, eps, 1.0, 1.0)[1]
+            return _ResidualNorm.apply(*args)[1]
+    return _ResidualNorm.apply(*args)[1]
 
 
 def clip_grad_norm_(parameters, max_norm, eps=1e-6):

@@ -66,6 +66,36 @@ def test_the_stash_changes_nothing_but_the_memory(example, deferred):
     assert stash.stats["compressed"] >= 6 and stash.stats["stored_bytes"] < 0.9 * stash.stats["dense_bytes"]
 
 
+def test_nothing_is_kept_where_no_gradient_can_be_asked_for(monkeypatch):
+    """Weights that are parameters, under no_grad and inference_mode: the calls get no place for what backward would need; with gradients they do.  Equal results."""
+    from paper_2110_15362_amd import block
+    kept = []
+
+    def watch(name, places):
+        call = getattr(block, name)
+
+        def watched(*args):
+            kept.append([args[i] is not None for i in places])
+            return call(*args)
+        monkeypatch.setattr(block, name, watched)
+    watch("bt_gated_forward", (5, 6))                        # gate, up
+    watch("bt_residual_norm_forward", (7,))                  # stats
+    g = torch.Generator().manual_seed(5)
+    x, w_gate, w_up, w_down, one, two = (torch.nn.Parameter(torch.randn(*s, generator=g).cuda()) for s in ((9, 16), (24, 16), (24, 16), (16, 24), (16,), (16,)))
+
+    def sublayer():
+        y = block.rms_norm(x, one)
+        return block.residual_norm(x, block.gated_linear(y, w_gate, w_up) @ w_down.t(), one, two, two)
+    want = sublayer()
+    assert kept == [[True], [True, True], [True]] and want[0].requires_grad and want[1].requires_grad
+    for mode in (torch.no_grad, torch.inference_mode):
+        del kept[:]
+        with mode():
+            got = sublayer()
+        assert kept == [[False], [False, False], [False]]
+        assert all(torch.equal(a, b) and not a.requires_grad for a, b in zip(got, want))
+
+
 def test_the_command_trains(example, capsys):
     losses = example.main(["--layers", "2", "--features", "256", "--hidden", "512", "--rows", "512", "--steps", "6", "--stash"])
     assert len(losses) == 6 and losses[-1] < losses[0]
