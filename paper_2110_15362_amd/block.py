@@ -247,22 +247,32 @@ class _ResidualNorm(torch.autograd.Function):
         return grads + (None, None, None, None)
 
 
-def _gate_matrix(gate, cols):
-    """A gate of shape [cols], [..., 1, cols] (one for each sequence) or [..., cols] as [gate_rows, cols]."""
-    return None if gate is None else gate.reshape(-1, cols) if cols else gate.reshape(gate.shape[:-1].numel(), cols)
+def _gate_matrix(gate, shape):
+    """A gate of shape [cols], [..., 1, cols] (one for each sequence) or [..., cols] as [gate_rows, cols], for x of `shape`.  Refused is one that broadcasting
+    would spread over x in another order than its rows are taken in."""
+    if gate is None:
+        return None
+    cols, lead, over = shape[-1], list(gate.shape[:-1]), list(shape[:-1])
+    while lead and lead[-1] == 1:
+        lead.pop()
+    if lead != over[:len(lead)] and gate.shape[:-1].numel() != shape[:-1].numel():      # (with a row for each row of x there is one order)
+        if gate.dim() <= len(shape) and all(a in (1, b) for a, b in zip(reversed(gate.shape), reversed(shape))):
+            raise ValueError("gate %s lacks leading dimensions of x %s: expand it to the shape of x" % (tuple(gate.shape), tuple(shape)))
+    return gate.reshape(gate.shape[:-1].numel(), cols)
 
 
 def residual_norm(x, block, post_weight=None, gate=None, pre_weight=None, eps=1e-6, scale=1.0, residual_scale=1.0):
     """What stands between two blocks: (out, y) with out = residual_scale * x + scale * gate * norm(block) * post_weight, the residual stream, and
     y = norm(out) * pre_weight, the input of the next block (None without pre_weight), with their gradients.  gate: [cols], or [..., cols] with a
     number of rows that divides that of x, row r of x taking gate row r * gate_rows // rows: a row for each of B sequences of x [B, T, cols] is
-    gate [B, cols] or [B, 1, cols]."""
+    gate [B, cols] or [B, 1, cols].  A gate that lacks leading dimensions of x, such as [1, T, cols] or (with T other than B) [T, cols], is refused:
+    gate.expand(x.shape) has a row for each row."""
     _check_device(x, block, post_weight, gate, pre_weight)
     if block.shape != x.shape:
         raise ValueError("block must have the shape of x")
     if gate is not None and (gate.dim() == 0 or gate.shape[-1] != x.shape[-1]):
         raise ValueError("gate must have the last dimension of x")
-    args = x, block, post_weight, _gate_matrix(gate, x.shape[-1]), pre_weight, eps, scale, residual_scale, _keep(x, block, post_weight, gate, pre_weight)
+    args = x, block, post_weight, _gate_matrix(gate, x.shape), pre_weight, eps, scale, residual_scale, _keep(x, block, post_weight, gate, pre_weight)
     if _elsewhere(x):
         with torch.cuda.device(x.device):
             return _ResidualNorm.apply(*args)

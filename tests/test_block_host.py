@@ -204,6 +204,28 @@ def test_functions_refuse_on_the_host(block):
         block.new_gated_workspace(1, 8, 8, torch.float64)
 
 
+def test_a_gate_that_broadcasting_reads_in_another_way_is_refused(block):
+    """A gate is taken by rows of x in their order: one that lacks leading dimensions of x, which broadcasting repeats, is not that."""
+    def matrix(gate, shape):
+        return block._gate_matrix(gate, torch.Size(shape))
+    x = (4, 6, 8)
+    for shape, rows in (((8,), 1), ((1, 8), 1), ((1, 1, 8), 1), ((4, 8), 4), ((4, 1, 8), 4), ((4, 6, 8), 24), ((24, 8), 24), ((12, 8), 12), ((3, 8), 3), ((2, 2, 8), 4)):
+        gate = torch.arange(float(torch.Size(shape).numel())).view(shape)
+        assert torch.equal(matrix(gate, x), gate.view(rows, 8)), shape
+        if gate.dim() == 3 and shape != (2, 2, 8):           # as broadcasting has it
+            assert torch.equal(gate.expand(x).reshape(24, 8), gate.view(rows, 8).repeat_interleave(24 // rows, 0))
+    for shape in ((6, 8), (1, 6, 8)):
+        with pytest.raises(ValueError, match="expand it to the shape of x"):
+            matrix(torch.zeros(shape), x)
+        assert matrix(torch.zeros(shape).expand(x), x).shape == (24, 8)
+    with pytest.raises(ValueError, match="expand it to the shape of x"):
+        matrix(torch.zeros(2, 1, 5, 8), (2, 3, 5, 8))
+    assert matrix(torch.zeros(2, 3, 1, 8), (2, 3, 5, 8)).shape == (6, 8)
+    for shape, of in (((6, 8), (1, 6, 8)), ((1, 6, 8), (1, 6, 8)), ((5, 8), (15, 8)), ((15, 8), (15, 8)), ((4, 8), (4, 4, 8))):
+        assert matrix(torch.zeros(shape), of).shape[0] == shape[-2]
+    assert matrix(torch.zeros(3, 0), (3, 5, 0)).shape == (3, 0) and matrix(None, x) is None
+
+
 def test_constants_are_the_headers(block):
     import re
     text = open(os.path.join(os.path.dirname(__file__), "..", "include", "bittrain.h")).read()

@@ -286,6 +286,21 @@ def test_autograd(block, gate_shape):
     assert all(torch.allclose(p.cpu().double(), q, rtol=2e-5, atol=2e-5) for p, q in zip(got, want))
 
 
+def test_a_gate_for_each_position(block):
+    """[T, cols] and [1, T, cols] for several sequences: refused as they are, right when expanded to the shape of x, their gradients sums over the sequences."""
+    g = torch.Generator().manual_seed(15)
+    x, b, gate, v = (torch.randn(*s, generator=g) for s in ((4, 6, 48), (4, 6, 48), (1, 6, 48), (4, 6, 48)))
+    dev, ref = [[t.to(d, k).requires_grad_() for t in (x, b, gate)] for d, k in (("cuda", torch.float32), ("cpu", torch.float64))]
+    for bad in (dev[2], dev[2][0]):
+        with pytest.raises(ValueError, match="expand it to the shape of x"):
+            block.residual_norm(dev[0], dev[1], None, bad)
+    out, _ = block.residual_norm(dev[0], dev[1], None, dev[2].expand(x.shape))
+    want = ref[0] + ref[2] * ref[1]
+    assert torch.allclose(out.cpu().double(), want, rtol=1e-6, atol=1e-6)
+    for p, q in zip(torch.autograd.grad(out, dev, v.cuda()), torch.autograd.grad(want, ref, v.double())):
+        assert p.shape == q.shape and torch.allclose(p.cpu().double(), q, rtol=1e-5, atol=1e-5)
+
+
 def test_gradients_against_differences(block):
     """The slope of a weighted sum of both outputs along a direction: central differences of the definition in 64 bits."""
     s = _inputs(24, 100, 4, torch.float32, 10)
