@@ -291,10 +291,12 @@ def rms_norm(x, weight, eps=1e-6):
 
 def clip_grad_norm_(parameters, max_norm, eps=1e-6):
     """Scales the gradients of the parameters in place so that their norm is at most max_norm; returns the norm that they had, on the device
-    (float32[1]; infinite or NaN where a gradient is).  A parameter that is given twice counts once.  Nothing waits for the device."""
+    (float32[1]; infinite or NaN where a gradient is).  A parameter that is given twice counts once, and so does a gradient that several parameters share;
+    gradients must not overlap otherwise.  Nothing waits for the device."""
     if isinstance(parameters, torch.Tensor):
         parameters = [parameters]
-    grads = list({id(p): p.grad for p in parameters if p.grad is not None}.values())
+    # (One tensor twice would be scaled twice, or once, by workgroups that do not know of each other.)
+    grads = list({id(g): g for g in (p.grad for p in parameters) if g is not None}.values())
     if not grads:
         raise ValueError("no parameter has a gradient")
     _check_device(*grads)

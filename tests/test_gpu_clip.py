@@ -160,6 +160,21 @@ def test_clip_grad_norm(block):
         block.clip_grad_norm_([params[3]], 1.0)
 
 
+def test_a_gradient_that_two_parameters_share(block):
+    """One tensor as the gradient of two parameters: counted once and scaled once."""
+    g = torch.Generator().manual_seed(43)
+    params = [torch.nn.Parameter(torch.zeros(300000, device="cuda")) for _ in range(3)]
+    shared, alone = (torch.randn(300000, generator=g) for _ in range(2))
+    params[0].grad = params[2].grad = shared.cuda()
+    params[1].grad = alone.cuda()
+    want = _norm([shared, alone])
+    norm = block.clip_grad_norm_(params, 1.0)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    for p, t in ((params[0], shared), (params[1], alone)):
+        exact = t.double() / (want + EPS)
+        within(p.grad, exact, rounded(exact, t.dtype, 3 * SUM * exact.abs()), "gradient")
+
+
 def test_a_tensor_of_more_than_32_bits(block):
     n = (1 << 32) + 5
     if torch.cuda.mem_get_info()[0] < 24 << 30:
