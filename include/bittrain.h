@@ -500,7 +500,8 @@ bt_status bt_grad_norm(const bt_clip_item *items, size_t count, float *d_norm,
 
 /* The same, and every gradient scaled so that their norm is at most max_norm: d_out = d_in * min(1, max_norm / (norm + eps)), the
  * product in 32 bits.  Nothing waits for the host: the factor stays on the device.  A norm of infinity makes the factor 0 and a NaN makes
- * it a NaN, as the formula has it; the caller sees either in *d_norm.  max_norm >= 0 (infinity: no clipping), eps >= 0.
+ * it a NaN, as the formula has it; the caller sees either in *d_norm.  max_norm >= 0 (infinity: no clipping, whatever the norm), eps >= 0 (with both
+ * 0 a norm of 0 leaves the zeros).
  * Errors: as bt_grad_norm, and BT_ERR_ARGUMENT. */
 bt_status bt_clip_grads(const bt_clip_item *items, size_t count, double max_norm, double eps, float *d_norm,
                         void *d_workspace, size_t workspace_bytes, bt_stream stream);

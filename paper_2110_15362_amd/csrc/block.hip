@@ -591,7 +591,7 @@ __global__ __launch_bounds__(kClipThreads) void scale_kernel(const ClipTable a, 
     const double x = sqrt(total_of(sums, count, room));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)x;
     double ratio = max_norm / (x + eps);
-    if (ratio > 1.0) ratio = 1.0;              // (a NaN stays one)
+    if (ratio > 1.0 || max_norm == INFINITY || x + eps == 0.0) ratio = 1.0;      // (a NaN stays one, but for infinity / infinity and 0 / 0: nothing is clipped)
     const float factor = (float)ratio;
     for (;;) {
         if (factor != 1.0f || p.in != p.out) {      // (else it is there)

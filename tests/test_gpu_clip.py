@@ -115,6 +115,20 @@ def test_infinities_and_nans_are_told(block, dtype):
             assert float(norm) == float("inf") and bool(torch.isnan(outs[0][49999])) and not bool(outs[0][:49999].any()) and not bool(outs[1].any())
 
 
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+def test_no_clipping_whatever_the_norm(block, dtype):
+    """An infinite max_norm leaves gradients as they are, also where one of them is an infinity or a NaN; one of 0 leaves zeros zeros without an eps."""
+    t = DTYPES[dtype]
+    for bad in (float("inf"), float("-inf"), float("nan"), 0.0):
+        grads = [torch.full((50000,), 0.5 if bad else 0.0, dtype=t, device="cuda"), torch.full((11,), bad, dtype=t, device="cuda")]
+        norm, ws = torch.empty(1, device="cuda"), block.new_clip_workspace(grads)
+        for eps in (0.0, EPS):
+            outs = [torch.full_like(g, 3.0) for g in grads]
+            block.bt_clip_grads(grads, outs, float("inf") if bad else 0.0, norm, ws, eps)
+            assert all(torch.equal(o, g) or (math.isnan(bad) and i == 1 and bool(torch.isnan(o).all())) for i, (o, g) in enumerate(zip(outs, grads)))
+            assert float(norm) == abs(bad) or (math.isnan(bad) and math.isnan(float(norm)))
+
+
 def test_results_do_not_change_and_graphs_replay(block):
     grads = [g.cuda() for g in _grads([70000 + 13 * i for i in range(150)], list(DTYPES.values()), 41)]
     outs = [torch.empty_like(g) for g in grads]
