@@ -267,6 +267,8 @@ def residual_norm(x, block, post_weight=None, gate=None, pre_weight=None, eps=1e
     number of rows that divides that of x, row r of x taking gate row r * gate_rows // rows: a row for each of B sequences of x [B, T, cols] is
     gate [B, cols] or [B, 1, cols].  A gate that lacks leading dimensions of x, such as [1, T, cols] or (with T other than B) [T, cols], is refused:
     gate.expand(x.shape) has a row for each row."""
+    if block is None:
+        raise TypeError("residual_norm needs a block: rms_norm is the norm alone")
     _check_device(x, block, post_weight, gate, pre_weight)
     if block.shape != x.shape:
         raise ValueError("block must have the shape of x")
@@ -281,6 +283,8 @@ def residual_norm(x, block, post_weight=None, gate=None, pre_weight=None, eps=1e
 
 def rms_norm(x, weight, eps=1e-6):
     """x / sqrt(mean(x^2) + eps) * weight over the last dimension: the norm before the first block."""
+    if weight is None:
+        raise TypeError("rms_norm needs a weight")
     _check_device(x, weight)
     args = x, None, None, None, weight, eps, 1.0, 1.0, _keep(x, weight)
     if _elsewhere(x):

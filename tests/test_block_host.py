@@ -204,6 +204,13 @@ def test_functions_refuse_on_the_host(block):
         block.new_gated_workspace(1, 8, 8, torch.float64)
 
 
+def test_what_the_norms_cannot_do_without(block):
+    with pytest.raises(TypeError, match="needs a weight"):
+        block.rms_norm(torch.zeros(4, 8), None)
+    with pytest.raises(TypeError, match="needs a block"):
+        block.residual_norm(torch.zeros(4, 8), None)
+
+
 def test_a_gate_that_broadcasting_reads_in_another_way_is_refused(block):
     """A gate is taken by rows of x in their order: one that lacks leading dimensions of x, which broadcasting repeats, is not that."""
     def matrix(gate, shape):
