@@ -1084,7 +1084,8 @@ struct Plan {
 };
 
 // By a model of the time, us, whose constants are measured: what a compute unit multiplies in tiles of either size (of 5.9 TFLOP/s in 16 bits, 0.6 in
-// single precision), a tile's step when nothing else runs beside it, and for the splits a launch and their sums' way to memory and back.
+// single precision), a tile's step when nothing else runs beside it, and for the splits a launch and their sums' way to memory and back.  Single precision has the
+// smallest tiles alone: they reach 0.8 of that rate, and larger ones would only leave more of the last turn idle.
 Plan plan_of(const Product product, const uint64_t m, const uint64_t n, const uint64_t k, const int width, const bool any) {
     struct Form {
         Kind kind;
@@ -1098,8 +1099,7 @@ Plan plan_of(const Product product, const uint64_t m, const uint64_t n, const ui
     Plan best = {kSmall, 1};
     double least = 1e300;
     for (const Form &f : forms) {
-        if (f.kind != kSmall && any) break;
-        if (f.kind == kLarge && single) break;
+        if (f.kind != kSmall && (any || single)) break;
         const uint64_t tiles = ceil_div(m, f.rows) * ceil_div(n, product == kForward ? f.cols / 2 : f.cols) * (product == kGradW ? 2 : 1);
         for (uint32_t splits = 1; splits <= 32 && (splits == 1 || (steps / splits >= 8 && tiles * splits <= 4096)); splits *= 2) {
             const double work = 2.0 * f.rows * f.cols * (kKBytes / width) * (double)steps / splits;      // of a workgroup
@@ -1200,9 +1200,8 @@ template <class T, Product K> bt_status run_product(GatedJob &a, const Plan &pla
     };
     bt_status st = BT_OK;
     if (!straight || plan.kind == kAnyKind) st = go(gated_any_kernel<T, K>, Small{});
-    else if (plan.kind == kSmall) st = go(gated_kernel<T, K, Small>, Small{});
-    else if (plan.kind == kMiddle) st = go(gated_kernel<T, K, Middle>, Middle{});
-    else if constexpr (sizeof(T) == 2) st = go(gated_kernel<T, K, Large>, Large{});
+    else if (sizeof(T) == 4 || plan.kind == kSmall) st = go(gated_kernel<T, K, Small>, Small{});
+    else if constexpr (sizeof(T) == 2) st = plan.kind == kMiddle ? go(gated_kernel<T, K, Middle>, Middle{}) : go(gated_kernel<T, K, Large>, Large{});
     if (st != BT_OK || a.splits == 1) return st;
     const uint64_t cells = (uint64_t)a.m * a.n;
     const int threads = cells / kPer<T> < 256 * 512 ? kWave : 256;      // (two workgroups of 256 a compute unit or more)
