@@ -386,7 +386,8 @@ bt_status bt_workspace_status(const void *d_workspace, uint32_t *d_status, bt_st
  * What stands around the activations that the codec keeps, in a step that trains such a sublayer or in a call that
  * answers with it: the gated projections whose output is the activation, the norms, gate and residual sum between two
  * sublayers, and the clipping of the step's gradients.  BT_F32, BT_F16 and BT_BF16.  All sums, statistics and
- * activations are computed in 32 bits or more and rounded once, to the tensors' type, where they are stored.
+ * activations are computed in 32 bits or more and rounded once, to the tensors' type, where they are stored.  What a backward
+ * pass takes from its forward pass is so rounded too (d_gate and d_up, d_out), and so are the factors that bt_gated_backward multiplies.
  *
  * Tensors are row-major and contiguous, and are aligned to their elements; those that are aligned to 16 bytes and whose
  * rows are whole 16-byte vectors go faster.  A workspace is scratch memory of the call: 128-byte aligned, of the size that the
@@ -409,7 +410,8 @@ typedef enum {
 /* Bytes of workspace for bt_gated_forward (backward == 0) or bt_gated_backward (else).  0 for an unknown dtype or sizes the calls refuse. */
 size_t bt_gated_workspace_bytes(uint64_t rows, uint64_t d, uint64_t f, bt_dtype dtype, int backward);
 
-/* The gated projections: h = act(x w_gate^T) * (x w_up^T), in one kernel.
+/* The gated projections: h = act(x w_gate^T) * (x w_up^T), in one kernel but where the sum over d is split (few rows) or rows that do not begin on 16-byte boundaries are
+ * copied to some (128 rows and more).
  *   d_x               [rows, d]
  *   d_w_gate, d_w_up  [f, d] each
  *   d_h               [rows, f]
@@ -428,7 +430,7 @@ bt_status bt_gated_forward(const void *d_x, const void *d_w_gate, const void *d_
                            void *d_workspace, size_t workspace_bytes, bt_stream stream);
 
 /* Its backward pass.  With g and u the two products, dg = grad_h * u * act'(g) and du = grad_h * act(g) (selects where a ReLU's gate
- * is closed), rounded to the tensors' type as the factors of the products
+ * is closed), rounded to the tensors' type as the factors of the products (BT_F16: to an infinity beyond 65504, to fewer bits below 2^-14)
  *   grad_x = dg w_gate + du w_up      grad_w_gate = dg^T x      grad_w_up = du^T x
  *   d_gate, d_up                  as bt_gated_forward left them, for the same activation
  *   d_grad_x                      [rows, d], or NULL: not wanted (d_w_gate and d_w_up are not read then and may be NULL)
@@ -467,7 +469,7 @@ size_t bt_residual_norm_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t g
 /* The backward pass: the gradients of x, block, post_weight, gate and pre_weight from those of out and y.
  *   d_grad_out          [rows, cols], or NULL: 0
  *   d_grad_y            [rows, cols], or NULL: 0 (d_pre_weight and d_grad_pre_weight must be NULL then)
- *   d_out               out as the forward pass left it (x, if there was no block)
+ *   d_out               out as the forward pass left it, rounded (x, if there was no block)
  *   d_block ... d_pre_weight, gate_rows, scale, residual_scale, d_stats    as in the forward pass
  *   d_grad_x            [rows, cols], or NULL: not wanted
  *   d_grad_block        [rows, cols]; d_grad_post_weight, d_grad_pre_weight [cols]; d_grad_gate [gate_rows, cols]: each NULL if not
@@ -492,7 +494,7 @@ typedef struct {
 /* Bytes of workspace for bt_grad_norm and bt_clip_grads on `count` items, whatever their sizes. */
 size_t bt_clip_workspace_bytes(size_t count);
 
-/* *d_norm = sqrt(sum of the squares of all elements of all items), the sum in 64 bits: it neither overflows nor depends on the order.
+/* *d_norm = sqrt(sum of the squares of all elements of all items), the sum in 64 bits, where no square overflows, in an order that the sizes alone decide.
  * (An infinity or a NaN among them makes it one.)  count == 0 writes 0.
  * Errors: BT_ERR_NULL, BT_ERR_DTYPE, BT_ERR_ALIGN, BT_ERR_SIZE (n beyond BT_MAX_ELEMENTS), BT_ERR_WORKSPACE, BT_ERR_HIP. */
 bt_status bt_grad_norm(const bt_clip_item *items, size_t count, float *d_norm,

@@ -402,7 +402,7 @@ template <class T, Product K, int FP, int FQ> __device__ inline void finish(cons
         const uint32_t row = m + j * 16 + lane % 16;
         if constexpr (K != kForward && sizeof(T) == 2) {
             // Where rows begin on 64-byte boundaries (us, weights' gradients with 8 or 64 bytes in a row: [40, 3008] x 11008 66 and 49, [96, 4096] x 16384 98 and 76;
-            // but of [1, 4008] x 16008, whose rows do not, 71 and 84).  All lanes take part, those beyond the last row too.
+            // but, where rows do not, [1, 4008] x 16008 71 and 84, [100, 4008] x 16008 109 and 103).  All lanes take part, those beyond the last row too.
             if (!parts && a.pitch % 32 == 0) {
                 static_assert(kStoresAtLeast<T, K, FP, FQ> <= FQ * (FP / kTogether));
 #pragma unroll
@@ -680,6 +680,11 @@ template <int LEFT> __device__ inline void wait_for_tiles() {
 // the L2 where that has other things to hold in between.  The forward pass in tiles of 64, whose weights nothing else reads, asks for two tiles at a time,
 // in every second one, piece by piece, and has five places (f16 forward of [37, 4096] x 11003: 50 -> 46 us); larger tiles ask for one in each and have
 // four: with two the bf16 forward pass of [16384, 2048] x 8192 took the same time, and grad_x has no registers for it.
+//
+// That holds for the forward pass and for single precision.  In 16 bits grad_x and the weights' gradients read fragments of the operands that lie across by the
+// transposing reads, which the compiler takes for reads of what any fetch may write: it waits for all of a wave's fetches behind the barrier of each step, those that
+// were asked for half a step ago too, and at a tile's start for the stores of the one before.  The waits below have to be right without that one: it says nothing of other
+// waves' fetches.
 template <int KIND, int COUNT, int PRODUCTS, int GROUPS, int G = 0> __device__ inline void spread_kind() {
     if constexpr (G < GROUPS) {
         constexpr int c = COUNT * (G + 1) / GROUPS - COUNT * G / GROUPS, m = PRODUCTS * (G + 1) / GROUPS - PRODUCTS * G / GROUPS;
@@ -704,11 +709,12 @@ template <int N, int I = 0, class Go> __device__ inline void turn(Go go) {
     }
 }
 
-// Bound by the matrix units (and, in the largest calls, by the power that they take: they are busy for 57 to 65 % of the cycles at 1.9 GHz).  bf16,
-// tiles of 256 by 256: forward of [16384, 1024] x 4096 230 us, 1195 TFLOP/s, of [16384, 2048] x 8192 with gate and up kept 957 us, 1149; grad_x of the
-// latter 895 us, 1228, its weights' gradients 825 us, 1333; instructions for 32 by 32 results, which read half as many registers, 4 % slower;
+// Bound by the matrix units (and, in the largest forward passes, by the power that they take: they are busy for 59 to 62 % of the cycles at 1.9 GHz), in 16 bits grad_x and
+// the weights' gradients by them and the full wait in every step (61 and 66 %).  bf16, tiles of 256 by 256: forward of [16384, 1024] x 4096 232 us, 1185 TFLOP/s, of
+// [16384, 2048] x 8192 with gate and up kept 977 us, 1125; grad_x of the latter 892 us, 1233, its weights' gradients 825 us, 1333 (on a
+// slower card 241, 1061, 948 and 886); instructions for 32 by 32 results, which read half as many registers, 4 % slower;
 // four waves of 128 by 128, 667; 256 by 128, two workgroups a compute unit, 8 % slower.  Single precision, tiles of 64 by 64: [1024, 2048] x 8192 537 to 554
-// us each, 126 TFLOP/s.  Smaller sizes take smaller tiles, and parts of the sum each, so that there is work for all compute units: see plan_of.
+// us each, 124 to 128 TFLOP/s.  Smaller sizes take smaller tiles, and parts of the sum each, so that there is work for all compute units: see plan_of.
 template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, S::FQ == 8 ? 2 : 1) void gated_kernel(const GatedJob a) {
     typedef Work<T, K, S> W;
     // Rows of a power of two of bytes all begin in the same channel of the memory, and workgroups in step would ask one after the other: each XCD
@@ -1029,9 +1035,11 @@ template <class T> __global__ __launch_bounds__(256) void pad_kernel(const PadJo
     }
 }
 
-// dg = grad_h u act'(g) and du = grad_h act(g), rounded to the type: they are factors of the products, whose matrix instructions take them
-// so, and an error of half a unit in the last place of each term averages out in the sums.  Rows of `pitch` elements, whole vectors.  Bound by memory
-// ([16384, 8192] in bf16: 252 us, 5.3 TB/s).
+// dg = grad_h u act'(g) and du = grad_h act(g), rounded to the type: they are factors of the products, whose matrix instructions take them so (in two
+// parts each they would be twice the work).  With gate and up, rounded between the passes, that makes the gradients of bf16 [16384, 2048] x 8192 off by 0.0031 of them, in the mean of
+// squares, and a form in 32 bits that is rounded at its end by 0.0017.  In f16 they also have its range: beyond 65504 an infinity, below 6e-5 fewer bits, as if they
+// were the tensors that a step made of single operators has there.  Rows of `pitch` elements, whole vectors.  Bound by memory
+// ([16384, 8192] in bf16: 258 us, 5.2 TB/s).
 template <class T> __global__ __launch_bounds__(256) void gated_slopes_kernel(const T *grad_h, const T *gate, const T *up, T *dg, T *du,
                                                                              const uint32_t f, const uint32_t pitch, const uint64_t vectors, const int activation) {
     const uint32_t a_row = pitch / kPer<T>;
