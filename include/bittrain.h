@@ -508,6 +508,116 @@ bt_status bt_grad_norm(const bt_clip_item *items, size_t count, float *d_norm,
 bt_status bt_clip_grads(const bt_clip_item *items, size_t count, double max_norm, double eps, float *d_norm,
                         void *d_workspace, size_t workspace_bytes, bt_stream stream);
 
+/* ---- a feed-forward sublayer of several experts ------------------------------------
+ *
+ * The sublayer's weights in `experts` parts, of which each token uses `chosen`: which ones, and in which order all tokens' rows then lie (bt_route_...), the
+ * gated projections and the product back with each row's own expert (bt_expert_...), and the rows of a token added up again (bt_combine_...).
+ * BT_F32, BT_F16 and BT_BF16; rounding, layouts, alignment, workspaces and equal bits as above.
+ *
+ * A row stands for one token at one of its experts: tokens * chosen rows, in the order of the experts, within an expert in that of the tokens.  A
+ * token may have fewer experts than `chosen`, or none (padding): the rows that are left over come behind the last expert's.  What is
+ * computed of those is zero, whatever the inputs hold there. */
+
+/* Largest numbers of experts, and of experts that a token uses. */
+#define BT_MAX_EXPERTS 1024
+#define BT_MAX_CHOSEN 32
+
+/* Who goes where (host memory, read before the call returns; the tables are device memory, 4-byte aligned).  1 <= chosen <= experts, tokens * chosen <= BT_MAX_ROWS.
+ * bt_route_forward and bt_route_order write the tables; the other calls read of them what they name, and take what a table holds beyond its range for
+ * no row, no token or the end of the rows, so that no table makes them leave their tensors. */
+typedef struct {
+    uint64_t tokens, experts, chosen;
+    int32_t *d_index;      /* [tokens, chosen]: a token's experts, the largest logit first; -1: none */
+    int32_t *d_slots;      /* [tokens, chosen]: the row of each of them; -1: none */
+    int32_t *d_source;     /* [tokens * chosen]: the token of each row; -1: a row of no expert */
+    int32_t *d_offsets;    /* [experts + 1]: expert e has the rows from offsets[e] on, up to offsets[e + 1]; ascending, the first 0 */
+} bt_expert_plan;
+
+/* Bytes of workspace for bt_route_forward and bt_route_order.  0 for sizes that the calls refuse. */
+size_t bt_route_workspace_bytes(uint64_t tokens, uint64_t experts, uint64_t chosen);
+
+/* A token's experts and weights, and the order of the rows.
+ *   d_logits     [tokens, experts]
+ *   plan         all four tables are written
+ *   d_weights    [tokens, chosen], single precision whatever the logits' type: the softmax of a token's logits at its experts, over all experts, or with
+ *                normalise != 0 over those chosen; 0 where index is -1
+ * Chosen are the `chosen` largest logits, of equal ones (+0 and -0 are) the expert of the lowest number; an expert with a logit of -infinity never.  A NaN counts as larger
+ * than any number, and it, as +infinity, makes the token's weights NaN, as the formula does.
+ * tokens == 0 writes offsets alone.  Errors: BT_ERR_NULL, BT_ERR_DTYPE, BT_ERR_ALIGN, BT_ERR_SIZE, BT_ERR_WORKSPACE, BT_ERR_HIP. */
+bt_status bt_route_forward(const void *d_logits, bt_dtype dtype, int normalise, const bt_expert_plan *plan, float *d_weights,
+                           void *d_workspace, size_t workspace_bytes, bt_stream stream);
+
+/* The order alone, for experts that were chosen otherwise: reads d_index, a number that is no expert's counting as none, and writes d_slots, d_source and d_offsets.  A
+ * token's experts must differ for bt_expert_... and bt_combine_... to mean what they say, not for this. */
+bt_status bt_route_order(const bt_expert_plan *plan, void *d_workspace, size_t workspace_bytes, bt_stream stream);
+
+/* The gradient of the logits from that of the weights.  With normalise w_j (g_j - sum_i w_i g_i) at a token's experts and 0 elsewhere; without it
+ * p_e (g_e - sum_i w_i g_i) for every expert e, p the softmax, g_e 0 where e is not chosen.
+ *   d_grad_weights   [tokens, chosen]; not looked at where index is -1
+ *   d_logits         as in the forward pass (not read with normalise, and may be NULL then)
+ *   plan             d_index is read
+ *   d_weights        as bt_route_forward left them
+ *   d_grad_logits    [tokens, experts], of the logits' type
+ * Errors as for bt_route_forward, without BT_ERR_WORKSPACE. */
+bt_status bt_route_backward(const float *d_grad_weights, const void *d_logits, bt_dtype dtype, int normalise, const bt_expert_plan *plan,
+                            const float *d_weights, void *d_grad_logits, bt_stream stream);
+
+/* Bytes of workspace for bt_expert_gated_forward (backward == 0) or bt_expert_gated_backward (else); of plan the three numbers are read.  0 for an unknown dtype or sizes the
+ * calls refuse. */
+size_t bt_expert_gated_workspace_bytes(const bt_expert_plan *plan, uint64_t d, uint64_t f, bt_dtype dtype, int ordered, int backward);
+
+/* The gated projections, as bt_gated_forward makes them, with the weights of each row's expert.
+ *   d_x               ordered == 0: [tokens, d], row r taking that of its token (d_source is read); else [rows, d], the rows' own
+ *   d_w_gate, d_w_up  [experts, f, d] each
+ *   plan              d_offsets is read, and d_source
+ *   d_h, d_gate, d_up [rows, f], rows = tokens * chosen; d_gate and d_up may be NULL both
+ * Errors as for bt_gated_forward. */
+bt_status bt_expert_gated_forward(const void *d_x, const void *d_w_gate, const void *d_w_up, const bt_expert_plan *plan,
+                                  uint64_t d, uint64_t f, bt_dtype dtype, bt_activation activation, int ordered,
+                                  void *d_h, void *d_gate, void *d_up, void *d_workspace, size_t workspace_bytes, bt_stream stream);
+
+/* Its backward pass, as bt_gated_backward.
+ *   plan                          d_offsets is read, and without `ordered` d_source and d_slots
+ *   d_grad_x                      of the shape of d_x, or NULL: not wanted.  Without `ordered` a token's rows are added up in 32 bits, in the order of its experts
+ *   d_grad_w_gate, d_grad_w_up    [experts, f, d] each, zeros for an expert without rows, or NULL both: not wanted
+ * Errors as for bt_gated_backward. */
+bt_status bt_expert_gated_backward(const void *d_grad_h, const void *d_x, const void *d_w_gate, const void *d_w_up,
+                                   const void *d_gate, const void *d_up, const bt_expert_plan *plan,
+                                   uint64_t d, uint64_t f, bt_dtype dtype, bt_activation activation, int ordered,
+                                   void *d_grad_x, void *d_grad_w_gate, void *d_grad_w_up,
+                                   void *d_workspace, size_t workspace_bytes, bt_stream stream);
+
+/* Bytes of workspace for bt_expert_linear_forward (backward == 0) or bt_expert_linear_backward (else), as above. */
+size_t bt_expert_linear_workspace_bytes(const bt_expert_plan *plan, uint64_t d_in, uint64_t d_out, bt_dtype dtype, int ordered, int backward);
+
+/* y = x w^T with the weight of each row's expert: x [rows, d_in] if `ordered`, else [tokens, d_in] as above; w [experts, d_out, d_in]; y [rows, d_out].
+ * rows == 0 or d_out == 0 does nothing; with d_in == 0 the products are 0.  Errors: BT_ERR_NULL, BT_ERR_DTYPE, BT_ERR_ALIGN, BT_ERR_SIZE, BT_ERR_WORKSPACE, BT_ERR_HIP. */
+bt_status bt_expert_linear_forward(const void *d_x, const void *d_w, const bt_expert_plan *plan, uint64_t d_in, uint64_t d_out, bt_dtype dtype, int ordered,
+                                   void *d_y, void *d_workspace, size_t workspace_bytes, bt_stream stream);
+
+/* Its backward pass: grad_x = grad_y w, of the shape of x (NULL: not wanted; d_w is not read then), and grad_w = grad_y^T x of each expert's rows (NULL: not
+ * wanted; d_x is not read then).  The plan as for bt_expert_gated_backward. */
+bt_status bt_expert_linear_backward(const void *d_grad_y, const void *d_x, const void *d_w, const bt_expert_plan *plan,
+                                    uint64_t d_in, uint64_t d_out, bt_dtype dtype, int ordered, void *d_grad_x, void *d_grad_w,
+                                    void *d_workspace, size_t workspace_bytes, bt_stream stream);
+
+/* out[t] = sum over j of weights[t, j] * y[slots[t, j]], in that order: 0 for a token without experts.
+ *   d_y          [rows, cols]
+ *   plan         d_slots is read
+ *   d_weights    [tokens, chosen], single precision, or NULL: 1; not looked at where slots is -1
+ *   d_out        [tokens, cols]
+ * tokens == 0 or cols == 0 does nothing.  Errors: BT_ERR_NULL, BT_ERR_DTYPE, BT_ERR_ALIGN, BT_ERR_SIZE, BT_ERR_HIP. */
+bt_status bt_combine_forward(const void *d_y, const bt_expert_plan *plan, const float *d_weights, uint64_t cols, bt_dtype dtype, void *d_out, bt_stream stream);
+
+/* Its backward pass: grad_y[slots[t, j]] = weights[t, j] * grad_out[t], zeros in the rows of no expert, and grad_weights[t, j] = sum over the columns of
+ * grad_out[t] * y[slots[t, j]], 0 where slots is -1.
+ *   plan              d_slots and d_offsets are read
+ *   d_grad_y          [rows, cols], or NULL: not wanted
+ *   d_grad_weights    [tokens, chosen], single precision, or NULL: not wanted (d_y is not read then and may be NULL)
+ * cols == 0 writes zeros to grad_weights.  Errors as for the forward pass. */
+bt_status bt_combine_backward(const void *d_grad_out, const void *d_y, const bt_expert_plan *plan, const float *d_weights, uint64_t cols, bt_dtype dtype,
+                              void *d_grad_y, float *d_grad_weights, bt_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

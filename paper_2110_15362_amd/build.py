@@ -9,8 +9,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "bittrain.hip")
-# the operators of a feed-forward sublayer, which both libraries hold beside their own source
-BLOCK_SRCS = [os.path.join(HERE, "csrc", name) for name in ("block.hip", "gated.hip")]
+# the operators of a feed-forward sublayer, of one expert or several, which both libraries hold beside their own source
+BLOCK_SRCS = [os.path.join(HERE, "csrc", name) for name in ("block.hip", "gated.hip", "route.hip", "experts.hip")]
 LIB = os.path.join(HERE, "libbittrain.so")
 # measurement aids for bench.py: the same kernels with per-tile time stamps compiled in, plus a plain stream
 BENCH_SRC = os.path.join(HERE, "csrc", "bench_aids.hip")

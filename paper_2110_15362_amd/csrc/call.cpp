@@ -1,5 +1,5 @@
 /*
- * paper_2110_15362_amd/_call.so: the calls of libbittrain on torch tensors, for bittrain.py and block.py.
+ * paper_2110_15362_amd/_call.so: the calls of libbittrain on torch tensors, for bittrain.py, block.py and experts.py.
  *
  * What a small call costs is the host's work, not the GPU's: the three calls of a training step on one image's
  * layer (fp32, 200,704 elements) keep the GPU busy for 10 us, and checking the tensors and marshalling the arguments with
@@ -819,6 +819,294 @@ static PyObject *py_clip_grads(PyObject *self, PyObject *const *args, Py_ssize_t
     END_HANDLE_TH_ERRORS
 }
 
+/* ---- the operators of a sublayer of several experts, for experts.py ------------------------------------- */
+
+static struct {
+    size_t (*route_workspace_bytes)(uint64_t, uint64_t, uint64_t);
+    bt_status (*route_forward)(const void *, bt_dtype, int, const bt_expert_plan *, float *, void *, size_t, bt_stream);
+    bt_status (*route_order)(const bt_expert_plan *, void *, size_t, bt_stream);
+    bt_status (*route_backward)(const float *, const void *, bt_dtype, int, const bt_expert_plan *, const float *, void *, bt_stream);
+    size_t (*gated_workspace_bytes)(const bt_expert_plan *, uint64_t, uint64_t, bt_dtype, int, int);
+    bt_status (*gated_forward)(const void *, const void *, const void *, const bt_expert_plan *, uint64_t, uint64_t, bt_dtype, bt_activation, int, void *, void *,
+                               void *, void *, size_t, bt_stream);
+    bt_status (*gated_backward)(const void *, const void *, const void *, const void *, const void *, const void *, const bt_expert_plan *, uint64_t, uint64_t,
+                                bt_dtype, bt_activation, int, void *, void *, void *, void *, size_t, bt_stream);
+    size_t (*linear_workspace_bytes)(const bt_expert_plan *, uint64_t, uint64_t, bt_dtype, int, int);
+    bt_status (*linear_forward)(const void *, const void *, const bt_expert_plan *, uint64_t, uint64_t, bt_dtype, int, void *, void *, size_t, bt_stream);
+    bt_status (*linear_backward)(const void *, const void *, const void *, const bt_expert_plan *, uint64_t, uint64_t, bt_dtype, int, void *, void *, void *, size_t,
+                                 bt_stream);
+    bt_status (*combine_forward)(const void *, const bt_expert_plan *, const float *, uint64_t, bt_dtype, void *, bt_stream);
+    bt_status (*combine_backward)(const void *, const void *, const bt_expert_plan *, const float *, uint64_t, bt_dtype, void *, float *, bt_stream);
+} experts;
+
+static int expect_experts(const Py_ssize_t got, const Py_ssize_t want) {
+    if (experts.combine_backward == NULL) return fail(PyExc_RuntimeError, "the library is not loaded");
+    return got == want ? 0 : fail(PyExc_TypeError, "wrong number of arguments");
+}
+
+/* The four tables of a plan, which come behind the call's other tensors: (index, slots, source, offsets). */
+static int plan_of(const tensor *a, bt_expert_plan *plan, uint64_t *rows) {
+    static const char *const names[] = {"index", "slots", "source", "offsets"};
+    uint64_t tokens, chosen = 0;
+    for (int i = 0; i < 4; ++i)
+        if (a[i].code >= 0 || a[i].width != 4) return refuse(names[i], "must hold 32-bit integers");
+    if (matrix_of(&a[0], "index", &tokens, &chosen) != 0) return -1;
+    if (a[1].numel != a[0].numel || a[2].numel != a[0].numel) return refuse(a[1].numel != a[0].numel ? "slots" : "source", "must have as many elements as index");
+    if (a[3].numel < 2) return refuse("offsets", "must hold a number for each expert and one more");
+    *plan = {tokens, a[3].numel - 1, chosen, a[0].ptr, a[1].ptr, a[2].ptr, a[3].ptr};
+    *rows = a[0].numel;
+    return 0;
+}
+
+static int floats(const tensor *a, const char *name, const uint64_t elements) {
+    if (a->t == NULL) return 0;
+    if (a->code != BT_F32) return refuse(name, "must be in single precision");
+    return a->numel == elements ? 0 : refuse(name, "does not have the shape that goes with the others");
+}
+
+static int flag(PyObject *o, int *v) {
+    *v = PyObject_IsTrue(o);
+    return *v < 0 ? -1 : 0;
+}
+
+static int needed(PyObject *const *args, const char *const *names, const int count) {
+    for (int i = 0; i < count; ++i)
+        if (args[i] == Py_None) {
+            PyErr_Format(PyExc_TypeError, "%s is needed", names[i]);
+            return -1;
+        }
+    return 0;
+}
+
+/* (gated, tokens, experts, chosen, d, f, code, ordered, backward): bytes of workspace */
+static PyObject *py_experts_workspace(PyObject *self, PyObject *args) {
+    (void)self;
+    int gated, code, ordered, backward;
+    unsigned long long tokens, n, chosen, d, f;
+    if (experts.combine_backward == NULL) return fail(PyExc_RuntimeError, "the library is not loaded"), nullptr;
+    if (!PyArg_ParseTuple(args, "iKKKKKiii", &gated, &tokens, &n, &chosen, &d, &f, &code, &ordered, &backward)) return NULL;
+    const bt_expert_plan plan = {tokens, n, chosen, NULL, NULL, NULL, NULL};
+    return PyLong_FromSize_t((gated ? experts.gated_workspace_bytes : experts.linear_workspace_bytes)(&plan, d, f, (bt_dtype)code, ordered, backward));
+}
+
+/* (logits, weights, index, slots, source, offsets, workspace, normalise, stream) */
+static PyObject *py_route_forward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"logits", "weights", "index", "slots", "source", "offsets", "workspace"};
+    tensor a[7];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    bt_expert_plan plan;
+    uint64_t rows, tokens;
+    int normalise;
+    if (expect_experts(nargs, 9) != 0 || needed(args, names, 6) != 0 || take_some(a, args, names, 7) != 0 || plan_of(a + 2, &plan, &rows) != 0 ||
+        rows_of(&a[0], "logits", plan.experts, &tokens) != 0)
+        return NULL;
+    if (tokens != plan.tokens) return refuse("logits", "must have a row for each token of the plan"), nullptr;
+    if (floats(&a[1], "weights", rows) != 0 || code_of(&a[0], &code) != 0 || flag(args[7], &normalise) != 0 || stream_of(args[8], &stream) != 0) return NULL;
+    CALL("bt_route_forward", experts.route_forward(a[0].ptr, code, normalise, &plan, a[1].ptr, a[6].ptr, a[6].numel * a[6].width, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* (index, slots, source, offsets, workspace, stream) */
+static PyObject *py_route_order(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"index", "slots", "source", "offsets", "workspace"};
+    tensor a[5];
+    bt_stream stream = NULL;
+    bt_expert_plan plan;
+    uint64_t rows;
+    if (expect_experts(nargs, 6) != 0 || needed(args, names, 4) != 0 || take_some(a, args, names, 5) != 0 || plan_of(a, &plan, &rows) != 0 ||
+        stream_of(args[5], &stream) != 0)
+        return NULL;
+    CALL("bt_route_order", experts.route_order(&plan, a[4].ptr, a[4].numel * a[4].width, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* (grad_weights, weights, grad_logits, index, slots, source, offsets, logits, normalise, stream) */
+static PyObject *py_route_backward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"grad_weights", "weights", "grad_logits", "index", "slots", "source", "offsets", "logits"};
+    tensor a[8];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    bt_expert_plan plan;
+    uint64_t rows, tokens;
+    int normalise;
+    if (expect_experts(nargs, 10) != 0 || needed(args, names, 7) != 0 || take_some(a, args, names, 8) != 0 || plan_of(a + 3, &plan, &rows) != 0 ||
+        rows_of(&a[2], "grad_logits", plan.experts, &tokens) != 0)
+        return NULL;
+    if (tokens != plan.tokens) return refuse("grad_logits", "must have a row for each token of the plan"), nullptr;
+    const uint64_t elements[] = {tokens * plan.experts};
+    if (check_all(a + 7, names + 7, 1, &a[2], elements) != 0 || floats(&a[0], "grad_weights", rows) != 0 || floats(&a[1], "weights", rows) != 0 ||
+        code_of(&a[2], &code) != 0 || flag(args[8], &normalise) != 0 || stream_of(args[9], &stream) != 0)
+        return NULL;
+    CALL("bt_route_backward", experts.route_backward(a[0].ptr, a[7].ptr, code, normalise, &plan, a[1].ptr, a[2].ptr, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* Of a weight [experts, f, d] f and d; the experts have to be the plan's. */
+static int expert_weight(const tensor *w, const char *name, const uint64_t n, uint64_t *f, uint64_t *d) {
+    uint64_t size[3];
+    PyObject *const shape = PyObject_GetAttrString(w->t, "shape"), *const items = shape != NULL ? PySequence_Tuple(shape) : NULL;
+    Py_XDECREF(shape);
+    if (items == NULL) return -1;
+    bool fits = PyTuple_GET_SIZE(items) == 3;
+    for (int i = 0; i < 3 && fits; ++i) {
+        size[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(items, i));
+        fits = size[i] != (uint64_t)-1;
+    }
+    Py_DECREF(items);
+    if (PyErr_Occurred()) return -1;
+    if (!fits || size[0] != n) return refuse(name, "must be a matrix for each of the plan's experts");
+    *f = size[1];
+    *d = size[2];
+    return 0;
+}
+
+/* x has a row a token, or with `ordered` one a row. */
+static int check_x(const tensor *x, const char *name, const uint64_t d, const bt_expert_plan *plan, const int ordered) {
+    uint64_t rows;
+    if (rows_of(x, name, d, &rows) != 0) return -1;
+    if (rows != (ordered ? plan->tokens * plan->chosen : plan->tokens)) return refuse(name, ordered ? "must have a row for each of the plan's" : "must have a row for each token of the plan");
+    return 0;
+}
+
+/* (x, w_gate, w_up, h, index, slots, source, offsets, gate, up, workspace, activation, ordered, stream) */
+static PyObject *py_expert_gated_forward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"x", "w_gate", "w_up", "h", "index", "slots", "source", "offsets", "gate", "up", "workspace"};
+    tensor a[11];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    bt_expert_plan plan;
+    uint64_t rows, f, d;
+    int ordered;
+    if (expect_experts(nargs, 14) != 0 || needed(args, names, 8) != 0 || take_some(a, args, names, 11) != 0 || plan_of(a + 4, &plan, &rows) != 0 ||
+        flag(args[12], &ordered) != 0 || expert_weight(&a[1], "w_gate", plan.experts, &f, &d) != 0 || check_x(&a[0], "x", d, &plan, ordered) != 0)
+        return NULL;
+    const uint64_t weight = plan.experts * f * d, first[] = {a[0].numel, weight, weight, rows * f}, kept[] = {rows * f, rows * f};
+    if (check_all(a, names, 4, &a[0], first) != 0 || check_all(a + 8, names + 8, 2, &a[0], kept) != 0 || code_of(&a[0], &code) != 0) return NULL;
+    const long activation = PyLong_AsLong(args[11]);
+    if ((activation == -1 && PyErr_Occurred()) || stream_of(args[13], &stream) != 0) return NULL;
+    CALL("bt_expert_gated_forward", experts.gated_forward(a[0].ptr, a[1].ptr, a[2].ptr, &plan, d, f, code, (bt_activation)activation, ordered, a[3].ptr, a[8].ptr, a[9].ptr,
+                                                          a[10].ptr, a[10].numel * a[10].width, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* (grad_h, x, w_gate, w_up, gate, up, index, slots, source, offsets, grad_x, grad_w_gate, grad_w_up, workspace, activation, ordered, stream) */
+static PyObject *py_expert_gated_backward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"grad_h", "x", "w_gate", "w_up", "gate", "up", "index", "slots", "source", "offsets", "grad_x", "grad_w_gate", "grad_w_up", "workspace"};
+    tensor a[14];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    bt_expert_plan plan;
+    uint64_t rows, f, d;
+    int ordered;
+    if (expect_experts(nargs, 17) != 0 || needed(args, names, 10) != 0 || take_some(a, args, names, 14) != 0 || plan_of(a + 6, &plan, &rows) != 0 ||
+        flag(args[15], &ordered) != 0 || expert_weight(&a[2], "w_gate", plan.experts, &f, &d) != 0 || check_x(&a[1], "x", d, &plan, ordered) != 0)
+        return NULL;
+    const uint64_t weight = plan.experts * f * d, x = a[1].numel;
+    const uint64_t before[] = {rows * f, x, weight, weight, rows * f, rows * f}, behind[] = {x, weight, weight};
+    if (check_all(a, names, 6, &a[1], before) != 0 || check_all(a + 10, names + 10, 3, &a[1], behind) != 0 || code_of(&a[1], &code) != 0) return NULL;
+    const long activation = PyLong_AsLong(args[14]);
+    if ((activation == -1 && PyErr_Occurred()) || stream_of(args[16], &stream) != 0) return NULL;
+    CALL("bt_expert_gated_backward", experts.gated_backward(a[0].ptr, a[1].ptr, a[2].ptr, a[3].ptr, a[4].ptr, a[5].ptr, &plan, d, f, code, (bt_activation)activation, ordered,
+                                                            a[10].ptr, a[11].ptr, a[12].ptr, a[13].ptr, a[13].numel * a[13].width, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* (x, w, y, index, slots, source, offsets, workspace, ordered, stream) */
+static PyObject *py_expert_linear_forward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"x", "w", "y", "index", "slots", "source", "offsets", "workspace"};
+    tensor a[8];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    bt_expert_plan plan;
+    uint64_t rows, f, d;
+    int ordered;
+    if (expect_experts(nargs, 10) != 0 || needed(args, names, 7) != 0 || take_some(a, args, names, 8) != 0 || plan_of(a + 3, &plan, &rows) != 0 ||
+        flag(args[8], &ordered) != 0 || expert_weight(&a[1], "w", plan.experts, &f, &d) != 0 || check_x(&a[0], "x", d, &plan, ordered) != 0)
+        return NULL;
+    const uint64_t elements[] = {a[0].numel, plan.experts * f * d, rows * f};
+    if (check_all(a, names, 3, &a[0], elements) != 0 || code_of(&a[0], &code) != 0 || stream_of(args[9], &stream) != 0) return NULL;
+    CALL("bt_expert_linear_forward", experts.linear_forward(a[0].ptr, a[1].ptr, &plan, d, f, code, ordered, a[2].ptr, a[7].ptr, a[7].numel * a[7].width, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* (grad_y, x, w, index, slots, source, offsets, grad_x, grad_w, workspace, ordered, stream) */
+static PyObject *py_expert_linear_backward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"grad_y", "x", "w", "index", "slots", "source", "offsets", "grad_x", "grad_w", "workspace"};
+    tensor a[10];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    bt_expert_plan plan;
+    uint64_t rows, f, d;
+    int ordered;
+    if (expect_experts(nargs, 12) != 0 || needed(args, names, 7) != 0 || take_some(a, args, names, 10) != 0 || plan_of(a + 3, &plan, &rows) != 0 ||
+        flag(args[10], &ordered) != 0 || expert_weight(&a[2], "w", plan.experts, &f, &d) != 0 || check_x(&a[1], "x", d, &plan, ordered) != 0)
+        return NULL;
+    const uint64_t weight = plan.experts * f * d, x = a[1].numel, before[] = {rows * f, x, weight}, behind[] = {x, weight};
+    if (check_all(a, names, 3, &a[1], before) != 0 || check_all(a + 7, names + 7, 2, &a[1], behind) != 0 || code_of(&a[1], &code) != 0 ||
+        stream_of(args[11], &stream) != 0)
+        return NULL;
+    CALL("bt_expert_linear_backward", experts.linear_backward(a[0].ptr, a[1].ptr, a[2].ptr, &plan, d, f, code, ordered, a[7].ptr, a[8].ptr, a[9].ptr, a[9].numel * a[9].width,
+                                                              stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* (y, out, index, slots, source, offsets, weights, stream) */
+static PyObject *py_combine_forward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"y", "out", "index", "slots", "source", "offsets", "weights"};
+    tensor a[7];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    bt_expert_plan plan;
+    uint64_t rows, y_rows, cols = 0;
+    if (expect_experts(nargs, 8) != 0 || needed(args, names, 6) != 0 || take_some(a, args, names, 7) != 0 || plan_of(a + 2, &plan, &rows) != 0 ||
+        matrix_of(&a[0], "y", &y_rows, &cols) != 0)
+        return NULL;
+    if (y_rows != rows) return refuse("y", "must have a row for each of the plan's"), nullptr;
+    const uint64_t elements[] = {rows * cols, plan.tokens * cols};
+    if (check_all(a, names, 2, &a[0], elements) != 0 || floats(&a[6], "weights", rows) != 0 || code_of(&a[0], &code) != 0 || stream_of(args[7], &stream) != 0) return NULL;
+    CALL("bt_combine_forward", experts.combine_forward(a[0].ptr, &plan, a[6].ptr, cols, code, a[1].ptr, stream));
+    END_HANDLE_TH_ERRORS
+}
+
+/* (grad_out, y, index, slots, source, offsets, weights, grad_y, grad_weights, stream) */
+static PyObject *py_combine_backward(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    (void)self;
+    static const char *const names[] = {"grad_out", "y", "index", "slots", "source", "offsets", "weights", "grad_y", "grad_weights"};
+    tensor a[9];
+    bt_dtype code = BT_F32;
+    bt_stream stream = NULL;
+    bt_expert_plan plan;
+    uint64_t rows, y_rows, cols = 0;
+    if (expect_experts(nargs, 10) != 0 || needed(args, names, 6) != 0 || take_some(a, args, names, 9) != 0 || plan_of(a + 2, &plan, &rows) != 0 ||
+        matrix_of(&a[1], "y", &y_rows, &cols) != 0)
+        return NULL;
+    if (y_rows != rows) return refuse("y", "must have a row for each of the plan's"), nullptr;
+    const uint64_t elements[] = {plan.tokens * cols, rows * cols}, behind[] = {rows * cols};
+    if (check_all(a, names, 2, &a[1], elements) != 0 || check_all(a + 7, names + 7, 1, &a[1], behind) != 0 || floats(&a[6], "weights", rows) != 0 ||
+        floats(&a[8], "grad_weights", rows) != 0 || code_of(&a[1], &code) != 0 || stream_of(args[9], &stream) != 0)
+        return NULL;
+    CALL("bt_combine_backward", experts.combine_backward(a[0].ptr, a[1].ptr, &plan, a[6].ptr, cols, code, a[7].ptr, a[8].ptr, stream));
+    END_HANDLE_TH_ERRORS
+}
+
 /* The addresses of a tuple into the `count` pointers at `slots`, all or none. */
 static int take_addresses(PyObject *addresses, void **slots, const int count) {
     std::vector<uint64_t> at((size_t)count);
@@ -837,6 +1125,15 @@ static PyObject *py_bind_block(PyObject *self, PyObject *args) {
     PyObject *addresses;
     if (!PyArg_ParseTuple(args, "O!", &PyTuple_Type, &addresses)) return NULL;
     if (take_addresses(addresses, (void **)(void *)&block, (int)(sizeof(block) / sizeof(void *))) != 0) return NULL;
+    Py_RETURN_NONE;
+}
+
+/* (addresses of the calls in the order of `experts`) */
+static PyObject *py_bind_experts(PyObject *self, PyObject *args) {
+    (void)self;
+    PyObject *addresses;
+    if (!PyArg_ParseTuple(args, "O!", &PyTuple_Type, &addresses)) return NULL;
+    if (take_addresses(addresses, (void **)(void *)&experts, (int)(sizeof(experts) / sizeof(void *))) != 0) return NULL;
     Py_RETURN_NONE;
 }
 
@@ -862,7 +1159,10 @@ static PyMethodDef methods[] = {
     FAST(decompress), FAST(decompress_indexed), FAST(relu_backward), FAST(mask_apply), FAST(relu_forward),
     FAST(pack), FAST(unpack), FAST(relu), FAST(relu_gradient),
     FAST(gated_forward), FAST(gated_backward), FAST(residual_norm_forward), FAST(residual_norm_backward), FAST(grad_norm), FAST(clip_grads),
-    {"bind", py_bind, METH_VARARGS, NULL}, {"bind_block", py_bind_block, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL}};
+    FAST(route_forward), FAST(route_order), FAST(route_backward), FAST(expert_gated_forward), FAST(expert_gated_backward),
+    FAST(expert_linear_forward), FAST(expert_linear_backward), FAST(combine_forward), FAST(combine_backward),
+    {"experts_workspace", py_experts_workspace, METH_VARARGS, NULL},
+    {"bind", py_bind, METH_VARARGS, NULL}, {"bind_block", py_bind_block, METH_VARARGS, NULL}, {"bind_experts", py_bind_experts, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__call(void) {
