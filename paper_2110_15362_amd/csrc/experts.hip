@@ -40,9 +40,15 @@ __device__ inline uint32_t bound(const ExpertJob &a, const uint32_t e) {
     return o < 0 ? 0 : (uint32_t)o < a.rows ? (uint32_t)o : a.rows;
 }
 
-__device__ inline Group group_of(const ExpertJob &a, const uint32_t e) {
+// (By each lane for an expert of its own.)
+__device__ inline uint32_t rows_of(const ExpertJob &a, const uint32_t e) {
     const uint32_t first = bound(a, e), end = e < a.experts ? bound(a, e + 1) : a.rows;
-    return {e, first, end > first ? end - first : 0};
+    return end > first ? end - first : 0;
+}
+
+// (By all lanes for one: the numbers go to scalar registers, and what is addressed with them too.)
+__device__ inline Group group_of(const ExpertJob &a, const uint32_t e) {
+    return {e, (uint32_t)__builtin_amdgcn_readfirstlane(bound(a, e)), (uint32_t)__builtin_amdgcn_readfirstlane(rows_of(a, e))};
 }
 
 // The row of x that a row takes.
@@ -69,7 +75,7 @@ struct Tiles {
             for (uint32_t e0 = 0; e0 <= a.experts; e0 += kWave) {
                 const uint32_t e = e0 + threadIdx.x;
                 uint32_t n = 0;
-                if (e <= a.experts) n = (group_of(a, e).rows + a_tile - 1) / a_tile;
+                if (e <= a.experts) n = (rows_of(a, e) + a_tile - 1) / a_tile;
                 uint32_t x = n;
 #pragma unroll
                 for (int d = 1; d < kWave; d *= 2) {
@@ -92,7 +98,7 @@ struct Tiles {
             if ((uint32_t)__builtin_amdgcn_readfirstlane(starts[mid]) <= tile) low = mid;
             else high = mid;
         }
-        return low;
+        return __builtin_amdgcn_readfirstlane(low);
     }
 };
 
@@ -148,7 +154,7 @@ template <class T, Kind K> __device__ inline Operand operand_q(const ExpertJob &
     const uint64_t first = K <= kPlain && a.source ? 0 : g.first * a.pitch_q;
     return {(const T *)a.q[sum] + first, a.pitch_q, g.rows, K == kWeights ? a.m : a.k};
 }
-template <Kind K> __device__ inline uint32_t summed(const ExpertJob &a, const Group &g) { return K == kWeights ? g.rows : g.expert < a.experts ? a.k : 0; }
+template <Kind K> __device__ inline uint32_t summed(const ExpertJob &a, const Group &g) { return K == kWeights ? g.rows : __builtin_amdgcn_readfirstlane(g.expert < a.experts ? a.k : 0); }
 __device__ inline Taken taken(const ExpertJob &a, const Group &g) { return {a.source ? a.source + g.first : nullptr, a.tokens}; }
 
 // Stores that a lane makes of each output in the function below, of a tile that lies inside it: at the least.
@@ -293,6 +299,313 @@ template <class T, Kind K> __global__ __launch_bounds__(Small::THREADS, 2) void 
     end<T, K, Small>(a, acc, at);
 }
 
+// A ring of the tiles of two sums, one behind the other: what is fetched next goes from the end of either to the start of the other, so that nothing is waited for between them.
+// (As two sums in turn, each with its own first fetches, the kernel also had 161 registers too many.)
+template <class T, Order O, int N, int WAVES> struct DirectTwo : Direct<T, O, N, WAVES, false> {
+    typedef Direct<T, O, N, WAVES, false> One;
+    int64_t way, both;      // bytes from the end of the sum that is being fetched to the start of the other, and of both ways
+    uint32_t each;          // tiles of a sum
+
+    __device__ void fetch(char *tile) {
+        const __amdgpu_buffer_rsrc_t r = One::next();
+        // (By masks: with branches, or selects of 64 bits, these numbers go to vector registers, and a descriptor that lies there is read in a loop.)
+        --One::ahead;
+        const int32_t over = (int32_t)(One::ahead - 1) >> 31;      // all ones behind the last tile of a sum
+        const int64_t mask = over;
+        One::base += way & mask;
+        way ^= (way ^ (both - way)) & mask;
+        One::ahead += each & (uint32_t)over;
+#pragma unroll
+        for (int i = 0; i < One::PER; ++i) One::piece(r, tile, i);
+    }
+    __device__ static int64_t scalar(const int64_t x) {
+        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+    }
+    // `second`: bytes from the first sum's operand to the second's; begin at tile `at` of the 2 * `count`.
+    __device__ void rotate(const int64_t second, const uint32_t at, const uint32_t count) {
+        const int64_t length = (int64_t)(count * One::advance);
+        const bool late = at >= count;
+        each = count;
+        both = scalar(-2 * length);
+        way = scalar(late ? -second - length : second - length);
+        One::base = (const char *)scalar((int64_t)(One::base + (late ? second : 0) + (late ? at - count : at) * One::advance));
+        One::ahead = count - (late ? at - count : at);
+    }
+};
+
+// As gated_kernel: tiles of either operand in LDS, the next ones on their way while one is multiplied, workgroups of the largest tiles taking several.  x's rows are fetched from where their
+// tokens have them, or, for the weights' gradients, from a copy in the order of the experts.
+template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::FQ == 8 ? 2 : 1) void experts_kernel(const ExpertJob a) {
+    typedef FormOf<K> F;
+    typedef Work<T, F, S> W;
+    // Each XCD begins elsewhere in the summed index, as there; the weights' gradients sum over rows, of which each expert has other numbers.
+    constexpr bool kRound = K != kWeights;
+    constexpr bool kTwo = F::SUMS == 2;
+    typedef std::conditional_t<kTwo, DirectTwo<T, F::P, S::NP, S::WAVES>, Direct<T, F::P, S::NP, S::WAVES, kRound>> FetchP;
+    typedef std::conditional_t<kTwo, DirectTwo<T, F::Q, S::NQ, S::WAVES>, Direct<T, F::Q, S::NQ, S::WAVES, kRound>> FetchQ;
+    constexpr int kPlaces = S::PLACES, kTurn = kPlaces, kAhead = kPlaces - 1, kLeft = kAhead - 1;
+    static_assert(kTurn % 2 == 0);
+    constexpr int PB = W::P::BYTES, QB = W::Q::BYTES, kFetches = FetchP::PER + FetchQ::PER;      // kFetches: instructions of a tile
+    constexpr int kReadsP = S::FP * Reader<T, F::P, S::NP, S::FP>::READS, kReadsQ = S::FQ / 2 * Reader<T, F::Q, S::NQ, S::FQ>::READS;
+    constexpr int kProducts = S::FP * S::FQ / 2 * (sizeof(T) == 4 ? 4 : 1);
+    __shared__ __align__(1024) char tiles[kPlaces * (PB + QB)];
+    __shared__ Tiles map;
+    if constexpr (K != kWeights) map.find(a, S::NQ);
+    const uint32_t total = tiles_of<K>(a, map);
+    uint32_t number = a.first + blockIdx.x;
+    if (number >= total) return;
+    W w;
+    FetchP dp;
+    FetchQ dq;
+    const auto tile_p = [&](const int t) { return tiles + t % kPlaces * PB; };
+    const auto tile_q = [&](const int t) { return tiles + kPlaces * PB + t % kPlaces * QB; };
+    // A tile's first fetches are asked for; returns how many steps it has.
+    const auto begin = [&](const Place &at) {
+        const uint32_t each = summed<K>(a, at.of) / kK<T>, count = each * F::SUMS;      // whole tiles
+        if (count == 0) return 0u;
+        const uint32_t phase = kRound ? (uint32_t)((uint64_t)(blockIdx.x % 8) * count / 8) & ~1u : 0;
+        if constexpr (K == kPair) dp.template start_pair<S::FP>(operand_p<T, K>(a, at.of, 0), operand_p<T, K>(a, at.of, 1), at.n);
+        else dp.start(operand_p<T, K>(a, at.of, 0), at.n);
+        const Operand q = operand_q<T, K>(a, at.of, K == kWeights ? at.part : 0);
+        if constexpr (K <= kPlain) {
+            if (a.source) dq.start_rows(q, at.m, taken(a, at.of));
+            else dq.start(q, at.m);
+        } else dq.start(q, at.m);
+        if constexpr (kTwo) {
+            dp.rotate((const char *)a.p[1] - (const char *)a.p[0], phase, each);
+            dq.rotate((const char *)a.q[1] - (const char *)a.q[0], phase, each);
+        } else {
+            dp.rotate(0, phase, count);
+            dq.rotate(0, phase, count);
+        }
+#pragma unroll
+        for (int t = 0; t < kAhead; ++t)
+            if ((uint32_t)t < count) {
+                dp.fetch(tile_p(t));
+                dq.fetch(tile_q(t));
+            }
+        return count;
+    };
+    Place at = place_of<K>(a, map, number, total, S::NQ, W::COLS);
+    uint32_t count = begin(at);
+    bool stored = false;      // since the first tiles were asked for: by each lane, kStores of each output or more
+    constexpr int kStores = kStoresAtLeast<T, K, S::FP, S::FQ>;
+    for (;;) {
+        typename W::Sums acc = {};
+        // Tile i of a turn, which lies in place i % kPlaces, with `left` tiles from it to the end.
+        const auto tile = [&](auto turn_number, const uint32_t left) {
+            constexpr int i = decltype(turn_number)::value;
+            w.read_q(tile_q(i), 1);
+            if (left > kAhead) {
+                dp.fetch(tile_p(i + kAhead));
+                dq.fetch(tile_q(i + kAhead));
+            }
+            w.multiply(acc, i & 1, 0);
+            spread<kReadsQ, kFetches, kProducts>();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the last fragments of this tile are here
+            // The next tile has come: what is asked for behind it may still be on its way.
+            if (left > kAhead) wait_for_tiles<kLeft * kFetches>();
+            else wait_for_tiles<0>();
+            w.read_p(tile_p(i + 1), (i + 1) & 1);      // (behind the last tile: what lies there, unused)
+            w.read_q(tile_q(i + 1), 0);
+            w.multiply(acc, i & 1, 1);
+            spread<kReadsP + kReadsQ, 0, kProducts>();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        const uint32_t k = summed<K>(a, at.of), rest = k / kK<T> * kK<T>;
+        if (count != 0) {
+            // The first tile of every wave has to be in LDS.  Fetches and stores are counted together, in order: of those that may still be on their way,
+            // the first tile's fetches are followed by those of kLeft tiles and by the stores.
+            if (count < kAhead) wait_for_tiles<0>();
+            else if (!stored) wait_for_tiles<kLeft * kFetches>();
+            else if (K == kPair && a.gate) wait_for_tiles<kLeft * kFetches + (K == kPair ? 3 : 1) * kStores>();
+            else wait_for_tiles<kLeft * kFetches + kStores>();
+            w.read_p(tile_p(0), 0);
+            w.read_q(tile_q(0), 0);
+            __builtin_amdgcn_sched_barrier(0);
+            uint32_t t = 0;
+            for (; t + kTurn + kAhead <= count; t += kTurn) turn<kTurn>([&](auto i) { tile(i, kTurn + kAhead); });
+            for (; t < count; t += kTurn)
+                turn<kTurn>([&](auto i) {
+                    if (t + decltype(i)::value < count) tile(i, count - t - decltype(i)::value);
+                });
+        }
+        // The rest of the summed index, less than a tile, through registers.
+        const bool through = rest < k;
+        if (through) {
+#pragma unroll 1
+            for (int sum = 0; sum < F::SUMS; ++sum) {
+                const Operand p = operand_p<T, K>(a, at.of, sum), q = operand_q<T, K>(a, at.of, K == kWeights ? at.part : sum);
+                if constexpr (K <= kPlain)
+                    w.staged(p, operand_p<T, K>(a, at.of, 1), q, at.n, at.m, rest, tiles, tiles + PB, acc, InOrder{}, taken(a, at.of));
+                else w.staged(p, p, q, at.n, at.m, rest, tiles, tiles + PB, acc);
+            }
+        }
+        const Place here = at;
+        number += gridDim.x;
+        // (The smaller tiles' workgroups take one each; a launch has them all unless there are more than it holds.)
+        const bool more = S::THREADS == Large::THREADS && number < total;
+        if (more) {
+            if (through) __syncthreads();
+            at = place_of<K>(a, map, number, total, S::NQ, W::COLS);
+            count = begin(at);
+            asm volatile("" ::: "memory");      // (the stores stay behind the fetches: see the wait that counts both)
+        }
+        end<T, K, S>(a, acc, here);
+        if (!more) break;
+        stored = sizeof(T) == 2 && here.m + S::NQ <= (K == kWeights ? a.m : here.of.rows) && here.n + W::COLS <= a.n;
+    }
+}
+
+// Few rows an expert (tokens to answer with): as gated_tokens_kernel, for 16 columns and FQ times 16 rows of one expert.  The weights are read once for as many rows and bound
+// the time.
+constexpr int kTokenWaves = 8;
+template <class T> constexpr int kUnit = 128 / (int)sizeof(T);
+
+template <class T, Kind K, int FQ, bool ODD> __global__ __launch_bounds__(kTokenWaves * kWave) void experts_tokens_kernel(const ExpertJob a) {
+    constexpr int N = K == kPair ? 2 : 1;      // weights
+    constexpr int kUnits = K == kPair ? 4 : FQ == 1 ? 8 : 4;      // on their way at once
+    constexpr int kLane = sizeof(T) == 4 ? kPer<T> : 2 * kPer<T>, kNext = sizeof(T) == 4 ? 4 * kPer<T> : kPer<T>;      // from one lane's first vector to the next one's, to its second
+    __shared__ float sums[kTokenWaves][N][FQ][kWave][4];
+    __shared__ Tiles map;
+    map.find(a, FQ * 16);
+    const uint32_t tile = (a.first + blockIdx.x) / a.tiles_n, n = ((a.first + blockIdx.x) - tile * a.tiles_n) * 16;
+    if (tile >= map.count(a)) return;
+    const uint32_t expert = map.expert(a, tile), m = (tile - __builtin_amdgcn_readfirstlane(map.starts[expert])) * (FQ * 16);
+    const Group g = group_of(a, expert);
+    const Taken rows = taken(a, g);
+    const Operand oq = operand_q<T, K>(a, g, 0);
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / 16, t = lane % 16;
+    const T *p[N], *q[FQ];
+    // (Rows that are not there are others again: their results are not stored.)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const Operand op = operand_p<T, K>(a, g, i);
+        p[i] = (const T *)op.p + (n + t < a.n ? n + t : a.n - 1) * op.pitch + group * kLane;
+    }
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+        const uint32_t row = m + j * 16 + t < g.rows ? m + j * 16 + t : g.rows - 1;
+        q[j] = (const T *)oq.p + rows(row) * oq.pitch + group * kLane;
+    }
+    bool odd_p[N], odd_q[FQ];      // where a lane's vectors are read from the element before (`k` is even)
+#pragma unroll
+    for (int i = 0; i < N; ++i) odd_p[i] = ODD && ((uintptr_t)p[i] & 2) != 0;
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) odd_q[j] = ODD && ((uintptr_t)q[j] & 2) != 0;
+    acc4 acc[N][FQ] = {};
+    // The workgroups begin in different places of the summed index, or all would ask the same channels of the memory at a time.
+    const uint32_t k_end = summed<K>(a, g), whole = k_end / kUnit<T>, shift = whole == 0 ? 0 : blockIdx.x * kTokenWaves % whole;
+    uint32_t unit = wave;
+    const auto take = [&](auto many) {
+        constexpr int M = decltype(many)::value;
+        raw16 w[M][N][2], x[M][FQ][2];
+        uint32_t w_end[M][N], x_end[M][FQ];
+#pragma unroll
+        for (int s = 0; s < M; ++s) {
+            uint32_t at = unit + s * kTokenWaves + shift;
+            if (at >= whole) at -= whole;
+            const uint64_t k = (uint64_t)at * kUnit<T>;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) w[s][i][h] = reinterpret_cast<const Unaligned<T> *>(p[i] + k + h * kNext - (odd_p[i] ? 1 : 0))->v;
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) x[s][j][h] = reinterpret_cast<const Unaligned<T> *>(q[j] + k + h * kNext - (odd_q[j] ? 1 : 0))->v;
+            }
+            if constexpr (ODD) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) w_end[s][i] = bits_at(p[i] + k + (2 * kPer<T> - 1));
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) x_end[s][j] = bits_at(q[j] + k + (2 * kPer<T> - 1));
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);      // (all of them before the first product)
+        const auto move = [&](raw16 (&v)[2], const uint32_t end, const bool odd) {
+            v[0] = from_odd<T>(v[0], v[1][0], odd);
+            v[1] = from_odd<T>(v[1], end, odd);
+        };
+#pragma unroll
+        for (int s = 0; s < M; ++s) {
+            if constexpr (ODD) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) move(w[s][i], w_end[s][i], odd_p[i]);
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) move(x[s][j], x_end[s][j], odd_q[j]);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int j = 0; j < FQ; ++j) acc[i][j] = multiply<T>(w[s][i][h], x[s][j][h], acc[i][j]);
+        }
+        unit += M * kTokenWaves;
+    };
+    while (unit + (kUnits - 1) * kTokenWaves < whole) take(std::integral_constant<int, kUnits>{});
+    while (unit < whole) take(std::integral_constant<int, 1>{});
+    if (wave == 0 && whole * kUnit<T> < k_end) {      // the rest, less than a unit
+        const uint32_t k = whole * kUnit<T>;
+        const int left = (int)(k_end - k) - group * kLane;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            raw16 w[N], x[FQ];
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = load_vec(p[i] + k + h * kNext, left - h * kNext, (int)k_end - left + h * kNext);
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) x[j] = load_vec(q[j] + k + h * kNext, left - h * kNext, (int)k_end - left + h * kNext);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) acc[i][j] = multiply<T>(w[i], x[j], acc[i][j]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) *(acc4 *)sums[wave][i][j][lane] = acc[i][j];
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < FQ * 256; c += kTokenWaves * kWave) {
+        const uint32_t col = c % 16, token = c / 16, from = col / 4 * 16 + token % 16, r = col % 4, j = token / 16;
+        float s[2] = {};
+#pragma unroll
+        for (int w = 0; w < kTokenWaves; ++w)
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[i] += sums[w][i][j][from][r];
+        if (m + token >= g.rows || n + col >= a.n) continue;
+        const uint64_t at = (uint64_t)(g.first + m + token) * a.pitch + n + col;
+        if constexpr (K == kPair) {
+            ((T *)a.out[0])[at] = narrow<T>(gated<T>(a.activation, s[0], s[1]));
+            if (a.gate) {
+                ((T *)a.gate)[at] = narrow<T>(s[0]);
+                ((T *)a.up)[at] = narrow<T>(s[1]);
+            }
+        } else ((T *)a.out[0])[at] = narrow<T>(s[0]);
+    }
+}
+
+// Matrices to rows of `pitch`, zeros behind their `cols`: where rows are to begin on 16-byte boundaries, or to lie in another order.  One for each blockIdx.y.
+struct CopyJob {
+    const void *from[4];
+    void *to[4];
+    const int32_t *source[4];      // the row of `from` that a row takes; NULL: its own
+    uint32_t rows[4], cols[4], pitch[4];
+    uint32_t tokens;               // rows of `from` where there is a source
+};
+
+template <class T> __global__ __launch_bounds__(256) void copy_kernel(const CopyJob a) {
+    const int y = blockIdx.y;
+    const uint32_t cols = a.cols[y], a_row = a.pitch[y] / kPer<T>;
+    const uint64_t vectors = (uint64_t)a.rows[y] * a_row;
+    const Taken rows = {a.source[y], a.tokens};
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < vectors; i += (uint64_t)gridDim.x * 256) {
+        const uint64_t row = i / a_row;
+        const uint32_t col = (uint32_t)(i - row * a_row) * kPer<T>;
+        store_vec((T *)a.to[y] + i * kPer<T>, kPer<T>, load_vec((const T *)a.from[y] + (uint64_t)rows((uint32_t)row) * cols + col, (int)(cols - col), (int)col));
+    }
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------
 
 // Without `source` the plan's order is that of x.
@@ -311,29 +624,135 @@ struct Call {
     }
 };
 
+// Rows of an expert, where all have the same.
+uint64_t each(const bt_expert_plan &p) { return p.tokens * p.chosen / p.experts; }
+
+// Rows of an expert from which on operands whose rows do not begin on 16-byte boundaries are copied to ones that do, as with the dense projections.
+constexpr uint64_t kPadEach = 128;
+
+// Rows of an expert up to which the forward pass reads the weights straight to registers.
+constexpr uint64_t kTokensEach = 16;
+
+bool pads(const bt_expert_plan &p, const uint64_t cols, const int width) { return ragged(cols, width) && each(p) >= kPadEach; }
+
+enum Size { kSmall, kMiddle, kLarge };
+
+// Tiles of which size, by the model of the time that gated.hip's plan_of has: an expert's last tile is half empty as a rule.
+Size size_of(const Kind kind, const uint64_t rows, const uint64_t experts, const uint64_t m, const uint64_t n, const uint64_t k, const uint64_t parts, const int width) {
+    struct Form {
+        Size size;
+        int side, together;      // rows and columns of a tile, workgroups that a compute unit holds
+        double rate, alone;
+    };
+    static const Form forms[] = {{kSmall, 64, 4, 0.33, 0.28}, {kMiddle, 128, 2, 0.6, 0.38}, {kLarge, 256, 1, 0.95, 0.75}};
+    if (width == 4) return kSmall;
+    const double steps = (double)((kind == kWeights ? rows / experts : k) * width) / kKBytes * (kind == kBackPair ? 2 : 1);
+    Size best = kSmall;
+    double least = 1e300;
+    for (const Form &f : forms) {
+        const uint64_t tiles_m = kind == kWeights ? ceil_div(m, f.side) * experts * parts : rows / f.side + (rows / experts < (uint64_t)f.side / 2 ? experts : experts / 2);
+        const uint64_t tiles = (tiles_m > 0 ? tiles_m : 1) * ceil_div(n, kind == kPair ? f.side / 2 : f.side), a_unit = ceil_div(tiles, 256);
+        double time = (double)a_unit * 2.0 * f.side * f.side * (kKBytes / width) * steps / (5.9e6 * f.rate);
+        const double alone = steps * f.alone * (double)ceil_div(a_unit, f.together);
+        if (time < alone) time = alone;
+        if (time < least) {
+            least = time;
+            best = f.size;
+        }
+    }
+    return best;
+}
+
+// Rows of whole vectors on 16-byte boundaries, and a tile within 32 bits of offsets.
+template <class T> bool direct(const void *p, const uint64_t pitch) { return !misaligned(p, kVec) && pitch % kPer<T> == 0 && pitch * sizeof(T) * 320 < 1u << 31; }
+
 template <class T, Kind K> bt_status run_product(ExpertJob &a, hipStream_t hs) {
-    const auto go = [&](auto kernel, auto shape) {
-        typedef decltype(shape) S;
-        const uint64_t tiles_n = ceil_div(a.n, K == kPair ? S::NP / 2 : S::NP);
+    const auto go = [&](auto kernel, const uint32_t rows, const uint32_t cols, const int threads) {
+        const uint64_t tiles_n = ceil_div(a.n, cols);
         uint64_t tiles_m;
-        if (K == kWeights) tiles_m = ceil_div(a.m, S::NQ);
+        if (K == kWeights) tiles_m = ceil_div(a.m, rows);
         else {      // each group's last tile may be a part
-            tiles_m = a.rows / S::NQ + a.experts + 1;
+            tiles_m = a.rows / rows + a.experts + 1;
             if (tiles_m > a.rows) tiles_m = a.rows;
         }
         const uint64_t groups = tiles_m * tiles_n * (K == kWeights ? (uint64_t)a.experts * a.parts : 1);
         if (groups >= 1u << 31) return BT_ERR_SIZE;
         a.tiles_m = (uint32_t)tiles_m;
         a.tiles_n = (uint32_t)tiles_n;
+        a.first = 0;
+        // The largest tiles' workgroups, one to a compute unit, take several each.
+        if (threads == Large::THREADS && rows == Large::NQ) return launch(kernel, dim3((unsigned)(groups < 256 ? groups : 256)), threads, hs, a);
         constexpr uint64_t kMost = 1u << 22;      // of a launch: a grid holds less than 2^32 threads
         bt_status s = BT_OK;
         for (uint64_t first = 0; first < groups && s == BT_OK; first += kMost) {
             a.first = (uint32_t)first;
-            s = launch(kernel, dim3((unsigned)(groups - first < kMost ? groups - first : kMost)), S::THREADS, hs, a);
+            s = launch(kernel, dim3((unsigned)(groups - first < kMost ? groups - first : kMost)), threads, hs, a);
         }
         return s;
     };
-    return go(experts_any_kernel<T, K>, Small{});
+    const auto tiled = [&](auto kernel, auto shape) {
+        typedef decltype(shape) S;
+        return go(kernel, S::NQ, K == kPair ? S::NP / 2 : S::NP, S::THREADS);
+    };
+    const uint64_t each_has = a.rows / a.experts;
+    if constexpr (K <= kPlain) {
+        if (each_has <= kTokensEach) {
+            const auto tokens = [&](auto kernel, const uint32_t rows) { return go(kernel, rows, 16, kTokenWaves * kWave); };
+            if constexpr (sizeof(T) == 2)
+                if (a.pitch_p % 2 != 0 && !misaligned(a.p[0], 4) && !misaligned(a.p[1], 4) && !misaligned(a.q[0], 4))
+                    return each_has <= 4 ? tokens(experts_tokens_kernel<T, K, 1, true>, 16) : tokens(experts_tokens_kernel<T, K, 2, true>, 32);
+            return each_has <= 4 ? tokens(experts_tokens_kernel<T, K, 1, false>, 16) : tokens(experts_tokens_kernel<T, K, 2, false>, 32);
+        }
+    }
+    bool straight = direct<T>(a.p[0], a.pitch_p) && direct<T>(a.q[0], a.pitch_q);
+    if (K == kPair || K == kBackPair) straight = straight && direct<T>(a.p[1], a.pitch_p);
+    if (K == kBackPair || (K == kWeights && a.parts == 2)) straight = straight && direct<T>(a.q[1], a.pitch_q);
+    if (a.source) straight = straight && K <= kPlain && a.tokens * a.pitch_q * sizeof(T) < 1u << 31;
+    if (!straight) return tiled(experts_any_kernel<T, K>, Small{});
+    const Size size = size_of(K, a.rows, a.experts, a.m, a.n, a.k, a.parts, sizeof(T));
+    if constexpr (sizeof(T) == 2) {
+        if (size == kLarge) return tiled(experts_kernel<T, K, Large>, Large{});
+        if (size == kMiddle) return tiled(experts_kernel<T, K, Middle>, Middle{});
+    }
+    return tiled(experts_kernel<T, K, Small>, Small{});
+}
+
+// What is to be copied, and where to in the workspace.
+template <class T> struct Copies {
+    CopyJob job = {};
+    int count = 0;
+
+    T *add(char **ws, const void *from, const uint64_t rows, const uint64_t cols, const uint64_t pitch, const int32_t *source = nullptr, const bool wanted = true) {
+        T *const to = (T *)*ws;
+        *ws += whole(rows * pitch * sizeof(T));
+        if (wanted) {
+            job.from[count] = from;
+            job.to[count] = to;
+            job.source[count] = source;
+            job.rows[count] = (uint32_t)rows;
+            job.cols[count] = (uint32_t)cols;
+            job.pitch[count++] = (uint32_t)pitch;
+        }
+        return to;
+    }
+    bt_status run(const Call &c) {
+        if (count == 0) return BT_OK;
+        job.tokens = (uint32_t)c.plan.tokens;
+        uint64_t most = 1;
+        for (int i = 0; i < count; ++i) {
+            const uint64_t vectors = (uint64_t)job.rows[i] * (job.pitch[i] / kPer<T>);
+            most = vectors > most ? vectors : most;
+        }
+        const uint64_t blocks = ceil_div(most, 256);
+        return launch(copy_kernel<T>, dim3((unsigned)(blocks < 1u << 14 ? blocks : 1u << 14), (unsigned)count), 256, c.hs, job);
+    }
+};
+
+// Bytes of the copies that the forward pass makes of x and `weights` weights (f rows of each), and the backward pass of x, where it is not in the order of the rows, and of the weights.
+uint64_t copies_bytes(const bt_expert_plan &p, const uint64_t d, const uint64_t f, const int weights, const int width, const bool ordered, const bool back) {
+    const uint64_t rows = p.tokens * p.chosen, pitch = padded(d, width);
+    if (!pads(p, d, width)) return back && !ordered ? whole(rows * pitch * width) : 0;
+    return whole((back || ordered ? rows : p.tokens) * pitch * width) + weights * whole(p.experts * f * pitch * width);
 }
 
 bt_status check(const bt_expert_plan *plan, const uint64_t d, const uint64_t f, const bt_dtype dtype) {
@@ -348,20 +767,50 @@ bt_status check_tables(const bt_expert_plan &plan, const bool ordered, const boo
 
 template <class... P> bool any_misaligned(const size_t a, P... p) { return (misaligned(p, a) || ...); }
 
+// x and one weight (w_up NULL) or two of the forward pass, as they are or copied.
+template <class T>
+bt_status operands(const Call &c, ExpertJob &a, const void *x, const void *w_gate, const void *w_up, const uint64_t d, const uint64_t f, char *ws) {
+    bt_status s = BT_OK;
+    uint64_t pitch = d;
+    if (pads(c.plan, d, sizeof(T))) {
+        pitch = padded(d, sizeof(T));
+        Copies<T> copies;
+        x = copies.add(&ws, x, c.ordered ? c.rows() : c.plan.tokens, d, pitch);
+        w_gate = copies.add(&ws, w_gate, c.plan.experts * f, d, pitch);
+        if (w_up) w_up = copies.add(&ws, w_up, c.plan.experts * f, d, pitch);
+        s = copies.run(c);
+    }
+    a.p[0] = w_gate;
+    a.p[1] = w_up ? w_up : w_gate;
+    a.q[0] = a.q[1] = x;
+    a.pitch_p = a.pitch_q = pitch;
+    a.step = f * pitch;
+    a.k = (uint32_t)pitch;
+    return s;
+}
+
 // The gradient of x, and those of the weights, of one product (du NULL) or of both projections, whose factors are dg and du: rows of `pitch_g`.
 template <class T>
 bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch_g, const void *x, const void *w_gate, const void *w_up, const uint64_t d, const uint64_t f,
                    void *grad_x, void *grad_w_gate, void *grad_w_up, char *ws) {
-    bt_status s = BT_OK;
-    if (grad_x) {
+    const bool padded_too = pads(c.plan, d, sizeof(T));
+    const uint64_t pitch = padded_too ? padded(d, sizeof(T)) : d, pitch_x = c.ordered ? pitch : padded(d, sizeof(T));
+    Copies<T> copies;
+    if (!c.ordered || padded_too) x = copies.add(&ws, x, c.rows(), d, pitch_x, c.ordered ? nullptr : c.plan.d_source, grad_w_gate != nullptr);
+    if (padded_too) {
+        w_gate = copies.add(&ws, w_gate, c.plan.experts * f, d, pitch, nullptr, grad_x != nullptr);
+        if (du) w_up = copies.add(&ws, w_up, c.plan.experts * f, d, pitch, nullptr, grad_x != nullptr);
+    }
+    bt_status s = copies.run(c);
+    if (s == BT_OK && grad_x) {
         ExpertJob a = c.job();
         a.p[0] = w_gate;
         a.p[1] = w_up;
         a.q[0] = dg;
         a.q[1] = du;
-        a.pitch_p = d;
+        a.pitch_p = pitch;
         a.pitch_q = pitch_g;
-        a.step = f * d;
+        a.step = f * pitch;
         a.pitch = d;
         a.n = (uint32_t)d;
         a.k = (uint32_t)f;
@@ -378,7 +827,7 @@ bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch
         a.p[0] = x;
         a.q[0] = dg;
         a.q[1] = du;
-        a.pitch_p = d;
+        a.pitch_p = pitch_x;
         a.pitch_q = pitch_g;
         a.step = f * d;
         a.out[0] = grad_w_gate;
@@ -387,7 +836,6 @@ bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch
         a.m = (uint32_t)f;
         a.n = (uint32_t)d;
         a.parts = du ? 2 : 1;
-        a.source = c.ordered ? nullptr : c.plan.d_source;
         s = run_product<T, kWeights>(a, c.hs);
     }
     return s;
@@ -409,9 +857,9 @@ using namespace btb;
 extern "C" {
 
 size_t bt_expert_gated_workspace_bytes(const bt_expert_plan *plan, uint64_t d, uint64_t f, bt_dtype dtype, int ordered, int backward) {
-    if (check(plan, d, f, dtype) != BT_OK || plan->tokens == 0 || f == 0 || !backward) return 0;
-    const uint64_t rows = plan->tokens * plan->chosen, w = (uint64_t)width_of(dtype);
-    return (size_t)(2 * whole(rows * padded(f, (int)w) * w) + (ordered ? 0 : whole(4 * rows * d)));
+    if (check(plan, d, f, dtype) != BT_OK || plan->tokens == 0 || f == 0) return 0;
+    const uint64_t rows = plan->tokens * plan->chosen, w = (uint64_t)width_of(dtype), copies = copies_bytes(*plan, d, f, 2, (int)w, ordered != 0, backward != 0);
+    return (size_t)(copies + (backward ? 2 * whole(rows * padded(f, (int)w) * w) + (ordered ? 0 : whole(4 * rows * d)) : 0));
 }
 
 bt_status bt_expert_gated_forward(const void *d_x, const void *d_w_gate, const void *d_w_up, const bt_expert_plan *plan,
@@ -432,18 +880,14 @@ bt_status bt_expert_gated_forward(const void *d_x, const void *d_w_gate, const v
     return with_type(dtype, [&](auto type) {
         using T = decltype(type);
         ExpertJob a = c.job();
-        a.p[0] = d_w_gate;
-        a.p[1] = d_w_up;
-        a.q[0] = a.q[1] = d_x;
-        a.pitch_p = a.pitch_q = d;
-        a.step = f * d;
+        const bt_status s = operands<T>(c, a, d_x, d_w_gate, d_w_up, d, f, (char *)d_workspace);
+        if (s != BT_OK) return s;
         a.out[0] = d_h;
         a.gate = d_gate;
         a.up = d_up;
         a.pitch = f;
         a.source = c.ordered ? nullptr : plan->d_source;
         a.n = (uint32_t)f;
-        a.k = (uint32_t)d;
         a.activation = activation;
         return run_product<T, kPair>(a, c.hs);
     });
@@ -485,8 +929,10 @@ bt_status bt_expert_gated_backward(const void *d_grad_h, const void *d_x, const 
 }
 
 size_t bt_expert_linear_workspace_bytes(const bt_expert_plan *plan, uint64_t d_in, uint64_t d_out, bt_dtype dtype, int ordered, int backward) {
-    if (check(plan, d_in, d_out, dtype) != BT_OK || plan->tokens == 0 || d_out == 0 || !backward || ordered) return 0;
-    return (size_t)whole(4 * plan->tokens * plan->chosen * d_in);
+    if (check(plan, d_in, d_out, dtype) != BT_OK || plan->tokens == 0 || d_out == 0) return 0;
+    const uint64_t rows = plan->tokens * plan->chosen, w = (uint64_t)width_of(dtype), copies = copies_bytes(*plan, d_in, d_out, 1, (int)w, ordered != 0, backward != 0);
+    if (!backward) return (size_t)copies;
+    return (size_t)(copies + (pads(*plan, d_out, (int)w) ? whole(rows * padded(d_out, (int)w) * w) : 0) + (ordered ? 0 : whole(4 * rows * d_in)));
 }
 
 bt_status bt_expert_linear_forward(const void *d_x, const void *d_w, const bt_expert_plan *plan, uint64_t d_in, uint64_t d_out, bt_dtype dtype, int ordered,
@@ -505,15 +951,12 @@ bt_status bt_expert_linear_forward(const void *d_x, const void *d_w, const bt_ex
     return with_type(dtype, [&](auto type) {
         using T = decltype(type);
         ExpertJob a = c.job();
-        a.p[0] = a.p[1] = d_w;
-        a.q[0] = a.q[1] = d_x;
-        a.pitch_p = a.pitch_q = d_in;
-        a.step = d_out * d_in;
+        const bt_status s = operands<T>(c, a, d_x, d_w, nullptr, d_in, d_out, (char *)d_workspace);
+        if (s != BT_OK) return s;
         a.out[0] = d_y;
         a.pitch = d_out;
         a.source = c.ordered ? nullptr : plan->d_source;
         a.n = (uint32_t)d_out;
-        a.k = (uint32_t)d_in;
         return run_product<T, kPlain>(a, c.hs);
     });
 }
@@ -538,7 +981,17 @@ bt_status bt_expert_linear_backward(const void *d_grad_y, const void *d_x, const
     return with_type(dtype, [&](auto type) {
         using T = decltype(type);
         if (rows == 0 || d_out == 0) return nothing<T>(c, d_in, d_out, d_grad_x, d_grad_w, nullptr);
-        return backward<T>(c, (const T *)d_grad_y, nullptr, d_out, d_x, d_w, nullptr, d_in, d_out, d_grad_x, d_grad_w, nullptr, (char *)d_workspace);
+        char *ws = (char *)d_workspace;
+        const T *grad_y = (const T *)d_grad_y;
+        uint64_t pitch = d_out;
+        if (pads(*plan, d_out, sizeof(T))) {
+            pitch = padded(d_out, sizeof(T));
+            Copies<T> copy;
+            grad_y = copy.add(&ws, d_grad_y, rows, d_out, pitch);
+            const bt_status s = copy.run(c);
+            if (s != BT_OK) return s;
+        }
+        return backward<T>(c, grad_y, nullptr, pitch, d_x, d_w, nullptr, d_in, d_out, d_grad_x, d_grad_w, nullptr, ws);
     });
 }
 

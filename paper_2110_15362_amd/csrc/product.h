@@ -445,6 +445,19 @@ template <class T, Order O, int N, int WAVES, bool ROUND> struct Direct {
         base = (const char *)a.p + (O == kAlong ? n * a.pitch : (uint64_t)n) * S;
         advance = (O == kAlong ? kK<T> : kK<T> * a.pitch) * S;
     }
+    // Rows that do not lie one behind the other: those of `map` from n on, of the a.rows that there are.
+    template <class Map> __device__ void start_rows(const Operand &a, const uint32_t n, const Map &map) {
+        static_assert(O == kAlong);
+        const int lane = fresh(threadIdx.x) % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int q = (wave * PER + i) * kWave + lane, chunk = (L::place(q / L::CHUNKS, q % L::CHUNKS) / kVec) % L::CHUNKS;
+            const uint32_t row = n + q / L::CHUNKS < a.rows ? n + q / L::CHUNKS : n;
+            offset[i] = (uint32_t)(map(row) * a.pitch + chunk * kPer<T>) * S;
+        }
+        base = (const char *)a.p;
+        advance = kK<T> * S;
+    }
     // The forward pass: rows of the two weights in turn, 8 F of each.  The loading wave's part of the tile is one such run.
     template <int F> __device__ void start_pair(const Operand &gate, const Operand &up, const uint32_t n) {
         static_assert(2 * PER == F, "a wave's part belongs to one weight");

@@ -273,3 +273,19 @@ def test_results_do_not_change_from_call_to_call(experts):
         got = [t.cpu() for t in kept + _gated_backward(experts, c, "silu", *kept[1:]) + (_linear_forward(experts, c),) + _linear_backward(experts, c)]
         assert first is None or all(torch.equal(a, b) for a, b in zip(first, got))
         first = got
+
+
+# the larger tiles, several of the largest to a workgroup, whole ones and ragged ones, summed indices with and without a rest, copies to 16-byte boundaries
+@pytest.mark.parametrize("ordered", [False, True])
+@pytest.mark.parametrize("dtype,size", [("bf16", (2100, 3, 2, 264, 2056)), ("f16", (4096, 2, 1, 1024, 2048)), ("bf16", (4500, 4, 2, 520, 1032)), ("f16", (1500, 8, 2, 1001, 1003)),
+                                        ("f32", (700, 4, 2, 264, 520)), ("bf16", (1024, 2, 2, 2048, 4100))], ids=str)
+def test_larger_tiles(experts, dtype, size, ordered):
+    c = Case(experts, size, DTYPES[dtype], 18, how="holes" if ordered else "some", ordered=ordered)
+    kept = _gated_forward(experts, c, "silu")
+    _check_gated_forward(c, "silu", *kept)
+    assert torch.equal(_gated_forward(experts, c, "silu", keep=False)[0], kept[0])
+    grads = _gated_backward(experts, c, "silu", *kept[1:])
+    _check_gated_backward(c, "silu", *kept[1:], grads)
+    assert all(torch.equal(a, b) for a, b in zip(grads, _gated_backward(experts, c, "silu", *kept[1:])))
+    _check_linear_forward(c, _linear_forward(experts, c))
+    _check_linear_backward(c, *_linear_backward(experts, c))
