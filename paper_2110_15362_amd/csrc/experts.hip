@@ -107,17 +107,18 @@ struct Place {
     uint32_t m, n, part;
 };
 
-// Tiles that there are, and the tile of a number.  Workgroups go to the eight XCDs in turn, each of which has an L2 of its own: an XCD's are neighbours, in bands of four rows of
-// tiles of one expert, so that those that run at once share what they read.
+// Tiles that there are, and the tile of a number.  Workgroups go to the eight XCDs in turn, each of which has an L2 of its own.  Of the kRound tiles that run at once an XCD's are
+// neighbours, in bands of four rows of tiles of one expert, so that they share what they read; all XCDs are at the same expert, whose weights then come from memory once, and (the weights' gradients)
+// have sums of about the same length.  (kRound 256: one tile to a compute unit.)
 template <Kind K> __device__ inline uint32_t tiles_of(const ExpertJob &a, const Tiles &tiles) {
     if constexpr (K == kWeights) return a.experts * a.parts * a.tiles_m * a.tiles_n;
     else return tiles.count(a) * a.tiles_n;
 }
 
 template <Kind K> __device__ inline Place place_of(const ExpertJob &a, const Tiles &tiles, const uint32_t number, const uint32_t total, const uint32_t tile_m, const uint32_t tile_n) {
-    constexpr uint32_t kXcds = 8, kBand = 4;
-    const uint32_t xcd = number % kXcds, more = total % kXcds;
-    uint32_t tile = xcd * (total / kXcds) + (xcd < more ? xcd : more) + number / kXcds, rows;
+    constexpr uint32_t kXcds = 8, kBand = 4, kRound = 256;
+    const uint32_t first = number / kRound * kRound, here = total - first < kRound ? total - first : kRound, xcd = number % kXcds, more = here % kXcds;
+    uint32_t tile = first + xcd * (here / kXcds) + (xcd < more ? xcd : more) + number % kRound / kXcds, rows;
     Place at;
     if constexpr (K == kWeights) {
         const uint32_t a_part = a.tiles_m * a.tiles_n, e = tile / (a_part * a.parts);
