@@ -27,6 +27,7 @@ struct ExpertJob {
     uint32_t m, n, k;                  // kWeights: m by n of each expert, k is not used; else n columns and k summed indices
     uint32_t tiles_m, tiles_n, parts;  // kWeights: tiles of an output, outputs; else tiles_n alone
     uint32_t first;                    // tile that the launch begins with
+    uint32_t padded_q;                 // kBack, kBackPair: q's rows go on with zeros to the end of a tile
     int activation;
 };
 
@@ -300,20 +301,23 @@ template <class T, Kind K> __global__ __launch_bounds__(Small::THREADS, 2) void 
     end<T, K, Small>(a, acc, at);
 }
 
-// A ring of the tiles of two sums, one behind the other: what is fetched next goes from the end of either to the start of the other, so that nothing is waited for between them.
-// (As two sums in turn, each with its own first fetches, the kernel also had 161 registers too many.)
-template <class T, Order O, int N, int WAVES> struct DirectTwo : Direct<T, O, N, WAVES, false> {
+// An operand's tiles straight from memory to LDS, as a ring: of one sum, begun anywhere, or of two, one behind the other, so that nothing is waited for between them.
+// (As two sums in turn, each with its own first fetches, the kernel also had 161 registers too many.)  Where the summed index lies across, the last tile may be a part: what
+// its descriptor has not got is zeros.
+template <class T, Order O, int N, int WAVES> struct Looped : Direct<T, O, N, WAVES, false> {
     typedef Direct<T, O, N, WAVES, false> One;
-    int64_t way, both;      // bytes from the end of the sum that is being fetched to the start of the other, and of both ways
-    uint32_t each;          // tiles of a sum
+    int64_t way, both;      // bytes from the end of the sum that is being fetched to the start of the next, and of both ways
+    uint32_t each, last;    // tiles of a sum; bytes that its last one has
 
     __device__ void fetch(char *tile) {
-        const __amdgpu_buffer_rsrc_t r = One::next();
         // (By masks: with branches, or selects of 64 bits, these numbers go to vector registers, and a descriptor that lies there is read in a loop.)
+        uint32_t there = 0x7fffffff;
+        if constexpr (O == kAcross) there ^= (there ^ last) & (uint32_t)((int32_t)(One::ahead - 2) >> 31);
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)One::base, 0, there, 0x00020000);
         --One::ahead;
         const int32_t over = (int32_t)(One::ahead - 1) >> 31;      // all ones behind the last tile of a sum
         const int64_t mask = over;
-        One::base += way & mask;
+        One::base += (int64_t)One::advance + (way & mask);
         way ^= (way ^ (both - way)) & mask;
         One::ahead += each & (uint32_t)over;
 #pragma unroll
@@ -322,11 +326,12 @@ template <class T, Order O, int N, int WAVES> struct DirectTwo : Direct<T, O, N,
     __device__ static int64_t scalar(const int64_t x) {
         return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
     }
-    // `second`: bytes from the first sum's operand to the second's; begin at tile `at` of the 2 * `count`.
-    __device__ void rotate(const int64_t second, const uint32_t at, const uint32_t count) {
+    // `second`: bytes from the first sum's operand to the second's, 0 of one sum; `count`: tiles of a sum; begin at tile `at` of all; `k`: the summed index.
+    __device__ void rotate(const int64_t second, const uint32_t at, const uint32_t count, const uint32_t k) {
         const int64_t length = (int64_t)(count * One::advance);
         const bool late = at >= count;
         each = count;
+        last = (k - (count - 1) * kK<T>) * (uint32_t)(One::advance / kK<T>);
         both = scalar(-2 * length);
         way = scalar(late ? -second - length : second - length);
         One::base = (const char *)scalar((int64_t)(One::base + (late ? second : 0) + (late ? at - count : at) * One::advance));
@@ -341,9 +346,8 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
     typedef Work<T, F, S> W;
     // Each XCD begins elsewhere in the summed index, as there; the weights' gradients sum over rows, of which each expert has other numbers.
     constexpr bool kRound = K != kWeights;
-    constexpr bool kTwo = F::SUMS == 2;
-    typedef std::conditional_t<kTwo, DirectTwo<T, F::P, S::NP, S::WAVES>, Direct<T, F::P, S::NP, S::WAVES, kRound>> FetchP;
-    typedef std::conditional_t<kTwo, DirectTwo<T, F::Q, S::NQ, S::WAVES>, Direct<T, F::Q, S::NQ, S::WAVES, kRound>> FetchQ;
+    typedef Looped<T, F::P, S::NP, S::WAVES> FetchP;
+    typedef Looped<T, F::Q, S::NQ, S::WAVES> FetchQ;
     constexpr int kPlaces = S::PLACES, kTurn = kPlaces, kAhead = kPlaces - 1, kLeft = kAhead - 1;
     static_assert(kTurn % 2 == 0);
     constexpr int PB = W::P::BYTES, QB = W::Q::BYTES, kFetches = FetchP::PER + FetchQ::PER;      // kFetches: instructions of a tile
@@ -360,9 +364,12 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
     FetchQ dq;
     const auto tile_p = [&](const int t) { return tiles + t % kPlaces * PB; };
     const auto tile_q = [&](const int t) { return tiles + kPlaces * PB + t % kPlaces * QB; };
+    // The rest of the summed index, less than a tile, goes through registers where it lies along an operand's rows (there the next row follows), unless zeros follow (the two-sum and the padded
+    // gradients: the other operand, across, has zeros too).
+    const bool whole_only = K <= kPlain || (K != kWeights && a.padded_q == 0);
     // A tile's first fetches are asked for; returns how many steps it has.
     const auto begin = [&](const Place &at) {
-        const uint32_t each = summed<K>(a, at.of) / kK<T>, count = each * F::SUMS;      // whole tiles
+        const uint32_t k = summed<K>(a, at.of), each = whole_only ? k / kK<T> : (k + kK<T> - 1) / kK<T>, count = each * F::SUMS;
         if (count == 0) return 0u;
         const uint32_t phase = kRound ? (uint32_t)((uint64_t)(blockIdx.x % 8) * count / 8) & ~1u : 0;
         if constexpr (K == kPair) dp.template start_pair<S::FP>(operand_p<T, K>(a, at.of, 0), operand_p<T, K>(a, at.of, 1), at.n);
@@ -372,13 +379,8 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
             if (a.source) dq.start_rows(q, at.m, taken(a, at.of));
             else dq.start(q, at.m);
         } else dq.start(q, at.m);
-        if constexpr (kTwo) {
-            dp.rotate((const char *)a.p[1] - (const char *)a.p[0], phase, each);
-            dq.rotate((const char *)a.q[1] - (const char *)a.q[0], phase, each);
-        } else {
-            dp.rotate(0, phase, count);
-            dq.rotate(0, phase, count);
-        }
+        dp.rotate(F::SUMS == 2 ? (const char *)a.p[1] - (const char *)a.p[0] : 0, phase, each, k);
+        dq.rotate(F::SUMS == 2 ? (const char *)a.q[1] - (const char *)a.q[0] : 0, phase, each, k);
 #pragma unroll
         for (int t = 0; t < kAhead; ++t)
             if ((uint32_t)t < count) {
@@ -414,7 +416,7 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
             spread<kReadsP + kReadsQ, 0, kProducts>();
             __builtin_amdgcn_sched_barrier(0);
         };
-        const uint32_t k = summed<K>(a, at.of), rest = k / kK<T> * kK<T>;
+        const uint32_t k = summed<K>(a, at.of), rest = whole_only ? k / kK<T> * kK<T> : k;
         if (count != 0) {
             // The first tile of every wave has to be in LDS.  Fetches and stores are counted together, in order: of those that may still be on their way,
             // the first tile's fetches are followed by those of kLeft tiles and by the stores.
@@ -815,6 +817,7 @@ bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch
         a.pitch = d;
         a.n = (uint32_t)d;
         a.k = (uint32_t)f;
+        a.padded_q = pitch_g == padded(f, sizeof(T));
         if (c.ordered) a.out[0] = grad_x;
         else a.sums = (float *)ws;
         s = du ? run_product<T, kBackPair>(a, c.hs) : run_product<T, kBack>(a, c.hs);

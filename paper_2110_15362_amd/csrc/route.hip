@@ -222,14 +222,17 @@ __device__ inline uint32_t add_up(const RouteJob &a, const uint32_t *all, uint32
     return sum;
 }
 
-template <class T, int L, int R> __global__ __launch_bounds__(256) void choose_kernel(const RouteJob a) {
+// A workgroup's 64 tokens at once, or most of them.
+constexpr int kChooseThreads = 1024;
+
+template <class T, int L, int R> __global__ __launch_bounds__(kChooseThreads) void choose_kernel(const RouteJob a) {
     __shared__ uint32_t count[kMostExperts];
-    clear_counts<256>(a, count);
+    clear_counts<kChooseThreads>(a, count);
     __syncthreads();
     const uint32_t first = blockIdx.x * a.a_group, end = a.tokens - first < a.a_group ? a.tokens : first + a.a_group;
-    choose<T, L, R, 256>(a, first, end, count);
+    choose<T, L, R, kChooseThreads>(a, first, end, count);
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < a.experts; e += 256) a.counts[(uint64_t)blockIdx.x * a.experts + e] = (int32_t)count[e];
+    for (uint32_t e = threadIdx.x; e < a.experts; e += kChooseThreads) a.counts[(uint64_t)blockIdx.x * a.experts + e] = (int32_t)count[e];
 }
 
 // The counts of an index that is there already.
@@ -246,19 +249,34 @@ __global__ __launch_bounds__(256) void count_kernel(const RouteJob a) {
     for (uint32_t e = threadIdx.x; e < a.experts; e += 256) a.counts[(uint64_t)blockIdx.x * a.experts + e] = (int32_t)count[e];
 }
 
-constexpr int kOrderWaves = 4;
+// Bound by the way to the counts of the groups, which every workgroup reads: threads that have no expert of their own take a part of the groups, eight at once (us, 16384 tokens, 8 of 128 experts: 64 one
+// count after the other by 256 threads).
+constexpr int kOrderWaves = 8;
 
 __global__ __launch_bounds__(kOrderWaves * kWave) void order_kernel(const RouteJob a) {
+    constexpr uint32_t kThreads = kOrderWaves * kWave, kAtOnce = 8;
     __shared__ uint32_t base[(kOrderWaves + 1) * kMostExperts], all[kMostExperts], rows_there;
-    for (uint32_t e = threadIdx.x; e < a.experts; e += kOrderWaves * kWave) {
+    clear_counts<kThreads>(a, base);
+    clear_counts<kThreads>(a, all);
+    __syncthreads();
+    const uint32_t parts = a.experts >= kThreads ? 1 : kThreads / a.experts, a_part = (a.groups + parts - 1) / parts;
+    for (uint32_t i = threadIdx.x; i < parts * a.experts; i += kThreads) {
+        const uint32_t part = i / a.experts, e = i - part * a.experts, end = (part + 1) * a_part;
+        const uint32_t from = part * a_part < a.groups ? part * a_part : a.groups, to = end < a.groups ? end : a.groups;
         uint32_t before = 0, sum = 0;
-        for (uint32_t g = 0; g < a.groups; ++g) {
-            const uint32_t n = (uint32_t)a.counts[(uint64_t)g * a.experts + e];
-            if (g < blockIdx.x) before += n;
-            sum += n;
+        for (uint32_t g0 = from; g0 < to; g0 += kAtOnce) {
+            uint32_t n[kAtOnce];
+#pragma unroll
+            for (uint32_t j = 0; j < kAtOnce; ++j) n[j] = (uint32_t)a.counts[(uint64_t)(g0 + j < to ? g0 + j : to - 1) * a.experts + e];
+#pragma unroll
+            for (uint32_t j = 0; j < kAtOnce; ++j) {
+                if (g0 + j >= to) n[j] = 0;
+                if (g0 + j < blockIdx.x) before += n[j];
+                sum += n[j];
+            }
         }
-        base[e] = before;
-        all[e] = sum;
+        if (before) atomicAdd(&base[e], before);
+        if (sum) atomicAdd(&all[e], sum);
     }
     __syncthreads();
     if (threadIdx.x < kWave) {
@@ -361,46 +379,46 @@ struct CombineJob {
     const int32_t *slots;
     const float *weights;          // or NULL
     void *out;
-    uint64_t rows, cols, vectors;  // vectors: of all tokens, a_row of each
-    uint32_t chosen, a_row;
+    uint64_t tokens, rows, cols;
+    uint32_t chosen;
 };
 
-// Tin: the rows' type.  A thread has a vector of a token's sum: E columns of the output's type.  Bound by memory.
-template <class Tin, class T> __global__ __launch_bounds__(256) void combine_kernel(const CombineJob a) {
-    constexpr int E = kPer<T>, kAtOnce = 4;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < a.vectors; i += (uint64_t)gridDim.x * 256) {
-        const uint64_t token = i / a.a_row, col = (i - token * a.a_row) * E;
-        const int left = a.cols - col < E ? (int)(a.cols - col) : E, before = col == 0 ? 0 : E;
+// Tin: the rows' type.  G threads a token (a wave, or all 256), a vector of the output's type each, K rows on their way at once.  Bound by memory.
+template <class Tin, class T, int G, int K> __global__ __launch_bounds__(256) void combine_kernel(const CombineJob a) {
+    constexpr int E = kPer<T>, H = E / kPer<Tin>;      // columns of a thread, vectors that they are
+    const uint32_t t = threadIdx.x % G;
+    for (uint64_t token = (uint64_t)blockIdx.x * (256 / G) + threadIdx.x / G; token < a.tokens; token += (uint64_t)gridDim.x * (256 / G)) {
         const int32_t *const slots = a.slots + token * a.chosen;
-        float sum[E] = {};
-        for (uint32_t j0 = 0; j0 < a.chosen; j0 += kAtOnce) {
-            raw16 v[kAtOnce][E / kPer<Tin>];
-            float w[kAtOnce];
-            bool there[kAtOnce];
+        for (uint64_t col = (uint64_t)t * E; col < a.cols; col += G * E) {
+            const int left = a.cols - col < E ? (int)(a.cols - col) : E, before = col == 0 ? 0 : E;
+            float sum[E] = {};
+            for (uint32_t j0 = 0; j0 < a.chosen; j0 += K) {
+                raw16 v[K][H];
+                float w[K];
+                bool there[K];
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                const uint64_t slot = j0 + j < a.chosen ? (uint64_t)(int64_t)slots[j0 + j] : ~0ull;
-                there[j] = slot < a.rows;
-                w[j] = 0.0f;
-                if (!there[j]) continue;
-                w[j] = a.weights ? a.weights[token * a.chosen + j0 + j] : 1.0f;
-                const Tin *const p = (const Tin *)a.y + slot * a.cols + col;
+                for (int j = 0; j < K; ++j) {
+                    const uint64_t slot = j0 + j < a.chosen ? (uint64_t)(int64_t)slots[j0 + j] : ~0ull;
+                    there[j] = slot < a.rows;
+                    w[j] = there[j] ? a.weights ? a.weights[token * a.chosen + j0 + j] : 1.0f : 0.0f;
+                    const Tin *const p = (const Tin *)a.y + (there[j] ? slot : 0) * a.cols + col;
 #pragma unroll
-                for (int h = 0; h < E / kPer<Tin>; ++h) v[j][h] = load_vec(p + h * kPer<Tin>, left - h * kPer<Tin>, left - h * kPer<Tin> > 0 ? before + h * kPer<Tin> : 0);
-            }
+                    for (int h = 0; h < H; ++h) v[j][h] = load_vec(p + h * kPer<Tin>, there[j] ? left - h * kPer<Tin> : 0, left - h * kPer<Tin> > 0 ? before + h * kPer<Tin> : 0);
+                }
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                if (!there[j]) continue;
+                for (int j = 0; j < K; ++j) {
+                    if (!there[j]) continue;
 #pragma unroll
-                for (int h = 0; h < E / kPer<Tin>; ++h) {
-                    float x[kPer<Tin>];
-                    unpack<Tin>(v[j][h], x);
+                    for (int h = 0; h < H; ++h) {
+                        float x[kPer<Tin>];
+                        unpack<Tin>(v[j][h], x);
 #pragma unroll
-                    for (int e = 0; e < kPer<Tin>; ++e) sum[h * kPer<Tin> + e] += w[j] * x[e];
+                        for (int e = 0; e < kPer<Tin>; ++e) sum[h * kPer<Tin> + e] += w[j] * x[e];
+                    }
                 }
             }
+            store_vec((T *)a.out + token * a.cols + col, left, pack<T>(sum));
         }
-        store_vec((T *)a.out + token * a.cols + col, left, pack<T>(sum));
     }
 }
 
@@ -552,13 +570,18 @@ template <class Tin, class T> bt_status combine(const bt_expert_plan &p, const v
     a.slots = p.d_slots;
     a.weights = weights;
     a.out = out;
+    a.tokens = p.tokens;
     a.rows = p.tokens * p.chosen;
     a.cols = cols;
     a.chosen = (uint32_t)p.chosen;
-    a.a_row = (uint32_t)((cols + kPer<T> - 1) / kPer<T>);
-    a.vectors = p.tokens * a.a_row;
-    const uint64_t blocks = (a.vectors + 255) / 256;
-    return launch(combine_kernel<Tin, T>, dim3((unsigned)(blocks < 1u << 20 ? blocks : 1u << 20)), 256, hs, a);
+    const auto go = [&](auto kernel, const int a_group) {
+        const uint64_t blocks = (a.tokens + a_group - 1) / a_group;
+        return launch(kernel, dim3((unsigned)(blocks < 1u << 20 ? blocks : 1u << 20)), 256, hs, a);
+    };
+    const bool wide = cols > 64 * kPer<T> * 2;
+    if (a.chosen <= 2) return wide ? go(combine_kernel<Tin, T, 256, 2>, 1) : go(combine_kernel<Tin, T, 64, 2>, 4);
+    if (a.chosen <= 4) return wide ? go(combine_kernel<Tin, T, 256, 4>, 1) : go(combine_kernel<Tin, T, 64, 4>, 4);
+    return wide ? go(combine_kernel<Tin, T, 256, 8>, 1) : go(combine_kernel<Tin, T, 64, 8>, 4);
 }
 
 }  // namespace
@@ -604,7 +627,7 @@ bt_status bt_route_forward(const void *d_logits, bt_dtype dtype, int normalise, 
         return with_lanes(a.experts, [&](auto lanes, auto each) {
             constexpr int L = decltype(lanes)::value, R = decltype(each)::value;
             if (one(*plan)) return launch(route_one_kernel<T, L, R>, dim3(1), kOneThreads, hs, a);
-            const bt_status s = launch(choose_kernel<T, L, R>, dim3(a.groups), 256, hs, a);
+            const bt_status s = launch(choose_kernel<T, L, R>, dim3(a.groups), kChooseThreads, hs, a);
             return s == BT_OK ? order(a, hs) : s;
         });
     });
