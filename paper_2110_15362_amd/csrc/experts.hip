@@ -341,7 +341,7 @@ template <class T, Order O, int N, int WAVES> struct Looped : Direct<T, O, N, WA
 
 // As gated_kernel: tiles of either operand in LDS, the next ones on their way while one is multiplied, workgroups of the largest tiles taking several.  x's rows are fetched from where their
 // tokens have them, or, for the weights' gradients, from a copy in the order of the experts.
-template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::FQ == 8 ? 2 : 1) void experts_kernel(const ExpertJob a) {
+template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void experts_kernel(const ExpertJob a) {
     typedef FormOf<K> F;
     typedef Work<T, F, S> W;
     // Each XCD begins elsewhere in the summed index, as there; the weights' gradients sum over rows, of which each expert has other numbers.

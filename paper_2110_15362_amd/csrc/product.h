@@ -65,6 +65,8 @@ template <class T, Order O, int N> struct Tile {      // N rows or columns of th
     }
 };
 
+__device__ __attribute__((always_inline)) inline short4v transposed(BT_LDS short4v *__restrict from) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(from); }
+
 // A wave's fragments of a tile: F times 16 rows or columns from `first` on.  Where a lane reads depends on the fragment and the tile by constants
 // alone, but for one address (summed index along) or one a fragment (across).
 template <class T, Order O, int N, int F> struct Reader {
@@ -92,8 +94,8 @@ template <class T, Order O, int N, int F> struct Reader {
             // 16 lanes read 4 summed indices by 16 columns, 4 columns a lane, and get one column each
             typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
             const char *const from = tile + at[i];
-            const uint2v low = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((BT_LDS short4v *)from));
-            const uint2v high = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((BT_LDS short4v *)(from + 4 * ROW)));
+            const uint2v low = __builtin_bit_cast(uint2v, transposed((BT_LDS short4v *)from));
+            const uint2v high = __builtin_bit_cast(uint2v, transposed((BT_LDS short4v *)(from + 4 * ROW)));
             return raw16{low[0], low[1], high[0], high[1]};
         } else {
             raw16 v;
