@@ -27,7 +27,7 @@ struct ExpertJob {
     uint32_t m, n, k;                  // kWeights: m by n of each expert, k is not used; else n columns and k summed indices
     uint32_t tiles_m, tiles_n, parts;  // kWeights: tiles of an output, outputs; else tiles_n alone
     uint32_t first;                    // tile that the launch begins with
-    uint32_t padded_q;                 // kBack, kBackPair: q's rows go on with zeros to the end of a tile
+    uint32_t padded_q;                 // kBack: q's rows go on with zeros to the end of a tile, as those of kBackPair do
     int activation;
 };
 
@@ -254,9 +254,9 @@ template <class T, Kind K> __global__ __launch_bounds__(Small::THREADS, 2) void 
     if (K == kWeights || p[0].cols < kPer<T> || q[0].cols < kPer<T>) {
         for (; t < last; ++t) {
             const uint32_t s = sum_of(t);
-            if constexpr (K == kWeights) w.staged(p[0], p[0], q[0], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, acc, rows);
-            else if constexpr (K <= kPlain) w.staged(p[s], p[1], q[s], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, acc, InOrder{}, rows);
-            else w.staged(p[s], p[1], q[s], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, acc);
+            if constexpr (K == kWeights) w.staged(p[0], p[0], q[0], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, tiles[0] + W::P::BYTES, acc, rows);
+            else if constexpr (K <= kPlain) w.staged(p[s], p[1], q[s], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, tiles[0] + W::P::BYTES, acc, InOrder{}, rows);
+            else w.staged(p[s], p[1], q[s], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, tiles[0] + W::P::BYTES, acc);
         }
         end<T, K, Small>(a, acc, at);
         return;
@@ -304,24 +304,37 @@ template <class T, Kind K> __global__ __launch_bounds__(Small::THREADS, 2) void 
 // An operand's tiles straight from memory to LDS, as a ring: of one sum, begun anywhere, or of two, one behind the other, so that nothing is waited for between them.
 // (As two sums in turn, each with its own first fetches, the kernel also had 161 registers too many.)  Where the summed index lies across, the last tile may be a part: what
 // its descriptor has not got is zeros.
-template <class T, Order O, int N, int WAVES> struct Looped : Direct<T, O, N, WAVES, false> {
-    typedef Direct<T, O, N, WAVES, false> One;
+template <class T, Order O, int N, int WAVES, int KB> struct Looped : Direct<T, O, N, WAVES, false, KB> {
+    typedef Direct<T, O, N, WAVES, false, KB> One;
     int64_t way, both;      // bytes from the end of the sum that is being fetched to the start of the next, and of both ways
     uint32_t each, last;    // tiles of a sum; bytes that its last one has
+    // Across, of the largest tiles: instructions two apart are four rows apart, in the same order of the chunks, and share their offsets' registers.
+    static constexpr bool kShared = O == kAcross && One::PER == 4 && sizeof(T) == 2 && N == 256;
+    static_assert(!kShared || One::L::place(4, 1) - One::L::place(0, 1) == 4 * N * (int)sizeof(T));
+    uint32_t four;          // rows, in bytes
 
     __device__ void fetch(char *tile) {
         // (By masks: with branches, or selects of 64 bits, these numbers go to vector registers, and a descriptor that lies there is read in a loop.)
         uint32_t there = 0x7fffffff;
-        if constexpr (O == kAcross) there ^= (there ^ last) & (uint32_t)((int32_t)(One::ahead - 2) >> 31);
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)One::base, 0, there, 0x00020000);
+        if constexpr (O == kAcross) there = __builtin_amdgcn_readfirstlane(there ^ ((there ^ last) & (uint32_t)((int32_t)(One::ahead - 2) >> 31)));
+        const char *const start = One::base;
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)start, 0, there, 0x00020000);
         --One::ahead;
         const int32_t over = (int32_t)(One::ahead - 1) >> 31;      // all ones behind the last tile of a sum
         const int64_t mask = over;
         One::base += (int64_t)One::advance + (way & mask);
         way ^= (way ^ (both - way)) & mask;
         One::ahead += each & (uint32_t)over;
+        if constexpr (kShared) {
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), behind = (int)there - (int)four;
+            const __amdgpu_buffer_rsrc_t s = __builtin_amdgcn_make_buffer_rsrc((void *)(start + four), 0, behind > 0 ? behind : 0, 0x00020000);
 #pragma unroll
-        for (int i = 0; i < One::PER; ++i) One::piece(r, tile, i);
+            for (int i = 0; i < 4; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < 2 ? r : s, (BT_LDS void *)(tile + (wave * 4 + i) * 1024), 16, (int)One::offset[i % 2], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < One::PER; ++i) One::piece(r, tile, i);
+        }
     }
     __device__ static int64_t scalar(const int64_t x) {
         return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
@@ -330,30 +343,39 @@ template <class T, Order O, int N, int WAVES> struct Looped : Direct<T, O, N, WA
     __device__ void rotate(const int64_t second, const uint32_t at, const uint32_t count, const uint32_t k) {
         const int64_t length = (int64_t)(count * One::advance);
         const bool late = at >= count;
-        each = count;
-        last = (k - (count - 1) * kK<T>) * (uint32_t)(One::advance / kK<T>);
+        const uint32_t row = (uint32_t)(One::advance / kK<T, KB>);
+        each = __builtin_amdgcn_readfirstlane(count);
+        last = __builtin_amdgcn_readfirstlane((k - (count - 1) * kK<T, KB>) * row);
+        four = __builtin_amdgcn_readfirstlane(4 * row);
         both = scalar(-2 * length);
         way = scalar(late ? -second - length : second - length);
         One::base = (const char *)scalar((int64_t)(One::base + (late ? second : 0) + (late ? at - count : at) * One::advance));
-        One::ahead = count - (late ? at - count : at);
+        One::ahead = __builtin_amdgcn_readfirstlane(count - (late ? at - count : at));
     }
 };
 
-// As gated_kernel: tiles of either operand in LDS, the next ones on their way while one is multiplied, workgroups of the largest tiles taking several.  x's rows are fetched from where their
-// tokens have them, or, for the weights' gradients, from a copy in the order of the experts.
+// Tiles of either operand in LDS, the next ones on their way while one is multiplied, in steps of 64 bytes of the summed index; workgroups of the largest tiles take several.  A step's products are made in two halves
+// (of Q's fragments): while the first is made the second's fragments are read, while the second is made the next step's first ones.  Behind the barrier in a tile's last step, between its halves, the next tile has
+// landed and all waves have read what they need of this one: another is asked for in its place.  x's rows are fetched from where their tokens have them, or, for the weights' gradients, from a copy in the order of the
+// experts.
+//
+// Where the summed index lies along an operand's rows a tile has whole 128-byte lines, and two lie in LDS: with tiles of 64 bytes, of which there were four, the L2 was read twice as often (32768 rows, eight
+// weights of [2048, 4096] in bf16: forward @585@ us, grad_x @520@).  The weights' gradients, whose tiles have lines of 512 bytes, have four of 64.
+template <Kind K> constexpr int kTileBytes = K == kWeights ? kKBytes : 2 * kKBytes;
+template <Kind K> constexpr int kPlaces = K == kWeights ? 4 : 2;
+
 template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void experts_kernel(const ExpertJob a) {
+    constexpr int KB = kTileBytes<K>, PLACES = kPlaces<K>, STEPS = KB / kKBytes, kKs = kK<T, KB>;
     typedef FormOf<K> F;
-    typedef Work<T, F, S> W;
-    // Each XCD begins elsewhere in the summed index, as there; the weights' gradients sum over rows, of which each expert has other numbers.
+    typedef Work<T, F, S, KB> W;
+    // Each XCD begins elsewhere in the summed index, as the dense projections do; the weights' gradients sum over rows, of which each expert has other numbers.
     constexpr bool kRound = K != kWeights;
-    typedef Looped<T, F::P, S::NP, S::WAVES> FetchP;
-    typedef Looped<T, F::Q, S::NQ, S::WAVES> FetchQ;
-    constexpr int kPlaces = S::PLACES, kTurn = kPlaces, kAhead = kPlaces - 1, kLeft = kAhead - 1;
-    static_assert(kTurn % 2 == 0);
+    typedef Looped<T, F::P, S::NP, S::WAVES, KB> FetchP;
+    typedef Looped<T, F::Q, S::NQ, S::WAVES, KB> FetchQ;
     constexpr int PB = W::P::BYTES, QB = W::Q::BYTES, kFetches = FetchP::PER + FetchQ::PER;      // kFetches: instructions of a tile
     constexpr int kReadsP = S::FP * Reader<T, F::P, S::NP, S::FP>::READS, kReadsQ = S::FQ / 2 * Reader<T, F::Q, S::NQ, S::FQ>::READS;
     constexpr int kProducts = S::FP * S::FQ / 2 * (sizeof(T) == 4 ? 4 : 1);
-    __shared__ __align__(1024) char tiles[kPlaces * (PB + QB)];
+    __shared__ __align__(1024) char tiles[PLACES * (PB + QB)];
     __shared__ Tiles map;
     if constexpr (K != kWeights) map.find(a, S::NQ);
     const uint32_t total = tiles_of<K>(a, map);
@@ -362,16 +384,18 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
     W w;
     FetchP dp;
     FetchQ dq;
-    const auto tile_p = [&](const int t) { return tiles + t % kPlaces * PB; };
-    const auto tile_q = [&](const int t) { return tiles + kPlaces * PB + t % kPlaces * QB; };
+    const auto tile_p = [&](const int t) { return tiles + t % PLACES * PB; };
+    const auto tile_q = [&](const int t) { return tiles + PLACES * PB + t % PLACES * QB; };
+    const auto read_q = [&](const int t, const int half, const int step) { w.read_q(tiles + t % PLACES * QB, half, step); };
+    w.rq.move(PLACES * PB);
     // The rest of the summed index, less than a tile, goes through registers where it lies along an operand's rows (there the next row follows), unless zeros follow (the two-sum and the padded
-    // gradients: the other operand, across, has zeros too).
-    const bool whole_only = K <= kPlain || (K != kWeights && a.padded_q == 0);
-    // A tile's first fetches are asked for; returns how many steps it has.
+    // gradients; the other operand, across, has zeros there too).
+    const bool whole_only = K <= kPlain || (K == kBack && a.padded_q == 0);
+    // A tile's first fetches are asked for; returns how many tiles of the summed index it has.
     const auto begin = [&](const Place &at) {
-        const uint32_t k = summed<K>(a, at.of), each = whole_only ? k / kK<T> : (k + kK<T> - 1) / kK<T>, count = each * F::SUMS;
+        const uint32_t k = summed<K>(a, at.of), each = __builtin_amdgcn_readfirstlane(whole_only ? k / kKs : (k + kKs - 1) / kKs), count = each * F::SUMS;
         if (count == 0) return 0u;
-        const uint32_t phase = kRound ? (uint32_t)((uint64_t)(blockIdx.x % 8) * count / 8) & ~1u : 0;
+        const uint32_t phase = kRound ? (uint32_t)((uint64_t)(blockIdx.x % 8) * count / 8) : 0;
         if constexpr (K == kPair) dp.template start_pair<S::FP>(operand_p<T, K>(a, at.of, 0), operand_p<T, K>(a, at.of, 1), at.n);
         else dp.start(operand_p<T, K>(a, at.of, 0), at.n);
         const Operand q = operand_q<T, K>(a, at.of, K == kWeights ? at.part : 0);
@@ -382,7 +406,7 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
         dp.rotate(F::SUMS == 2 ? (const char *)a.p[1] - (const char *)a.p[0] : 0, phase, each, k);
         dq.rotate(F::SUMS == 2 ? (const char *)a.q[1] - (const char *)a.q[0] : 0, phase, each, k);
 #pragma unroll
-        for (int t = 0; t < kAhead; ++t)
+        for (int t = 0; t < PLACES; ++t)
             if ((uint32_t)t < count) {
                 dp.fetch(tile_p(t));
                 dq.fetch(tile_q(t));
@@ -395,54 +419,67 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
     constexpr int kStores = kStoresAtLeast<T, K, S::FP, S::FQ>;
     for (;;) {
         typename W::Sums acc = {};
-        // Tile i of a turn, which lies in place i % kPlaces, with `left` tiles from it to the end.
+        // Tile i of a turn, which lies in place i % PLACES, with `left` tiles from it to the end.
         const auto tile = [&](auto turn_number, const uint32_t left) {
-            constexpr int i = decltype(turn_number)::value;
-            w.read_q(tile_q(i), 1);
-            if (left > kAhead) {
-                dp.fetch(tile_p(i + kAhead));
-                dq.fetch(tile_q(i + kAhead));
+            constexpr int i = decltype(turn_number)::value, kParity = STEPS == 1 ? i & 1 : 0;
+            if constexpr (STEPS == 2) {
+                read_q(i, 1, 0);
+                w.multiply(acc, 0, 0);
+                spread<kReadsQ, 0, kProducts>();
+                __builtin_amdgcn_sched_barrier(0);
+                w.read_p(tile_p(i), 1, 1);
+                read_q(i, 0, 1);
+                w.multiply(acc, 0, 1);
+                spread<kReadsP + kReadsQ, 0, kProducts>();
+                __builtin_amdgcn_sched_barrier(0);
             }
-            w.multiply(acc, i & 1, 0);
-            spread<kReadsQ, kFetches, kProducts>();
+            constexpr int kLast = STEPS == 1 ? kParity : 1, kNext = STEPS == 1 ? 1 - kParity : 0;
+            read_q(i, 1, STEPS - 1);
+            w.multiply(acc, kLast, 0);
+            spread<kReadsQ, 0, kProducts>();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the last fragments of this tile are here
             // The next tile has come: what is asked for behind it may still be on its way.
-            if (left > kAhead) wait_for_tiles<kLeft * kFetches>();
+            if (PLACES > 2 && left >= PLACES) wait_for_tiles<(PLACES - 2) * kFetches>();
             else wait_for_tiles<0>();
-            w.read_p(tile_p(i + 1), (i + 1) & 1);      // (behind the last tile: what lies there, unused)
-            w.read_q(tile_q(i + 1), 0);
-            w.multiply(acc, i & 1, 1);
-            spread<kReadsP + kReadsQ, 0, kProducts>();
+            w.read_p(tile_p(i + 1), kNext, 0);      // (behind the last tile: what lies there, unused)
+            read_q(i + 1, 0, 0);
+            if (left > PLACES) {
+                dp.fetch(tile_p(i));
+                dq.fetch(tile_q(i));
+            }
+            w.multiply(acc, kLast, 1);
+            spread<kReadsP + kReadsQ, kFetches, kProducts>();
             __builtin_amdgcn_sched_barrier(0);
         };
-        const uint32_t k = summed<K>(a, at.of), rest = whole_only ? k / kK<T> * kK<T> : k;
+        const uint32_t k = summed<K>(a, at.of), rest = whole_only ? k / kKs * kKs : k;
         if (count != 0) {
-            // The first tile of every wave has to be in LDS.  Fetches and stores are counted together, in order: of those that may still be on their way,
-            // the first tile's fetches are followed by those of kLeft tiles and by the stores.
-            if (count < kAhead) wait_for_tiles<0>();
-            else if (!stored) wait_for_tiles<kLeft * kFetches>();
-            else if (K == kPair && a.gate) wait_for_tiles<kLeft * kFetches + (K == kPair ? 3 : 1) * kStores>();
-            else wait_for_tiles<kLeft * kFetches + kStores>();
-            w.read_p(tile_p(0), 0);
-            w.read_q(tile_q(0), 0);
+            // The first tile of every wave has to be in LDS.  Fetches and stores are counted together, in order: of those that may still be on their way, the first tile's fetches are
+            // followed by those of the other places and by the stores.
+            constexpr int kBehind = (PLACES - 1) * kFetches;
+            if (count < PLACES) wait_for_tiles<0>();
+            else if (!stored) wait_for_tiles<kBehind>();
+            else if (K == kPair && a.gate) wait_for_tiles<kBehind + (K == kPair ? 3 : 1) * kStores>();
+            else wait_for_tiles<kBehind + kStores>();
+            w.read_p(tile_p(0), 0, 0);
+            read_q(0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
             uint32_t t = 0;
-            for (; t + kTurn + kAhead <= count; t += kTurn) turn<kTurn>([&](auto i) { tile(i, kTurn + kAhead); });
-            for (; t < count; t += kTurn)
-                turn<kTurn>([&](auto i) {
+            for (; t + 2 * PLACES <= count; t += PLACES) turn<PLACES>([&](auto i) { tile(i, 2 * PLACES); });
+            for (; t < count; t += PLACES)
+                turn<PLACES>([&](auto i) {
                     if (t + decltype(i)::value < count) tile(i, count - t - decltype(i)::value);
                 });
         }
         // The rest of the summed index, less than a tile, through registers.
-        const bool through = rest < k;
+        const bool through = (K <= kPlain || K == kBack) && rest < k;
         if (through) {
 #pragma unroll 1
             for (int sum = 0; sum < F::SUMS; ++sum) {
                 const Operand p = operand_p<T, K>(a, at.of, sum), q = operand_q<T, K>(a, at.of, K == kWeights ? at.part : sum);
                 if constexpr (K <= kPlain)
-                    w.staged(p, operand_p<T, K>(a, at.of, 1), q, at.n, at.m, rest, tiles, tiles + PB, acc, InOrder{}, taken(a, at.of));
-                else w.staged(p, p, q, at.n, at.m, rest, tiles, tiles + PB, acc);
+                    w.staged(p, operand_p<T, K>(a, at.of, 1), q, at.n, at.m, rest, tiles, tiles + PLACES * PB, tiles, acc, InOrder{}, taken(a, at.of));
+                else w.staged(p, p, q, at.n, at.m, rest, tiles, tiles + PLACES * PB, tiles, acc);
             }
         }
         const Place here = at;
@@ -627,6 +664,9 @@ struct Call {
     }
 };
 
+// Elements of a row that goes on with zeros to the end of a tile.
+uint64_t filled(const uint64_t cols, const int width) { return ceil_div(cols * width, 2 * kKBytes) * (2 * kKBytes) / width; }
+
 // Rows of an expert, where all have the same.
 uint64_t each(const bt_expert_plan &p) { return p.tokens * p.chosen / p.experts; }
 
@@ -753,7 +793,7 @@ template <class T> struct Copies {
 
 // Bytes of the copies that the forward pass makes of x and `weights` weights (f rows of each), and the backward pass of x, where it is not in the order of the rows, and of the weights.
 uint64_t copies_bytes(const bt_expert_plan &p, const uint64_t d, const uint64_t f, const int weights, const int width, const bool ordered, const bool back) {
-    const uint64_t rows = p.tokens * p.chosen, pitch = padded(d, width);
+    const uint64_t rows = p.tokens * p.chosen, pitch = filled(d, width);
     if (!pads(p, d, width)) return back && !ordered ? whole(rows * pitch * width) : 0;
     return whole((back || ordered ? rows : p.tokens) * pitch * width) + weights * whole(p.experts * f * pitch * width);
 }
@@ -776,7 +816,7 @@ bt_status operands(const Call &c, ExpertJob &a, const void *x, const void *w_gat
     bt_status s = BT_OK;
     uint64_t pitch = d;
     if (pads(c.plan, d, sizeof(T))) {
-        pitch = padded(d, sizeof(T));
+        pitch = filled(d, sizeof(T));
         Copies<T> copies;
         x = copies.add(&ws, x, c.ordered ? c.rows() : c.plan.tokens, d, pitch);
         w_gate = copies.add(&ws, w_gate, c.plan.experts * f, d, pitch);
@@ -796,11 +836,11 @@ bt_status operands(const Call &c, ExpertJob &a, const void *x, const void *w_gat
 template <class T>
 bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch_g, const void *x, const void *w_gate, const void *w_up, const uint64_t d, const uint64_t f,
                    void *grad_x, void *grad_w_gate, void *grad_w_up, char *ws) {
-    const bool padded_too = pads(c.plan, d, sizeof(T));
-    const uint64_t pitch = padded_too ? padded(d, sizeof(T)) : d, pitch_x = c.ordered ? pitch : padded(d, sizeof(T));
+    const bool filled_too = pads(c.plan, d, sizeof(T));
+    const uint64_t pitch = filled_too ? filled(d, sizeof(T)) : d, pitch_x = c.ordered ? pitch : filled(d, sizeof(T));
     Copies<T> copies;
-    if (!c.ordered || padded_too) x = copies.add(&ws, x, c.rows(), d, pitch_x, c.ordered ? nullptr : c.plan.d_source, grad_w_gate != nullptr);
-    if (padded_too) {
+    if (!c.ordered || filled_too) x = copies.add(&ws, x, c.rows(), d, pitch_x, c.ordered ? nullptr : c.plan.d_source, grad_w_gate != nullptr);
+    if (filled_too) {
         w_gate = copies.add(&ws, w_gate, c.plan.experts * f, d, pitch, nullptr, grad_x != nullptr);
         if (du) w_up = copies.add(&ws, w_up, c.plan.experts * f, d, pitch, nullptr, grad_x != nullptr);
     }
@@ -817,7 +857,7 @@ bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch
         a.pitch = d;
         a.n = (uint32_t)d;
         a.k = (uint32_t)f;
-        a.padded_q = pitch_g == padded(f, sizeof(T));
+        a.padded_q = pitch_g == filled(f, sizeof(T));
         if (c.ordered) a.out[0] = grad_x;
         else a.sums = (float *)ws;
         s = du ? run_product<T, kBackPair>(a, c.hs) : run_product<T, kBack>(a, c.hs);
@@ -863,7 +903,7 @@ extern "C" {
 size_t bt_expert_gated_workspace_bytes(const bt_expert_plan *plan, uint64_t d, uint64_t f, bt_dtype dtype, int ordered, int backward) {
     if (check(plan, d, f, dtype) != BT_OK || plan->tokens == 0 || f == 0) return 0;
     const uint64_t rows = plan->tokens * plan->chosen, w = (uint64_t)width_of(dtype), copies = copies_bytes(*plan, d, f, 2, (int)w, ordered != 0, backward != 0);
-    return (size_t)(copies + (backward ? 2 * whole(rows * padded(f, (int)w) * w) + (ordered ? 0 : whole(4 * rows * d)) : 0));
+    return (size_t)(copies + (backward ? 2 * whole(rows * filled(f, (int)w) * w) + (ordered ? 0 : whole(4 * rows * d)) : 0));
 }
 
 bt_status bt_expert_gated_forward(const void *d_x, const void *d_w_gate, const void *d_w_up, const bt_expert_plan *plan,
@@ -922,7 +962,7 @@ bt_status bt_expert_gated_backward(const void *d_grad_h, const void *d_x, const 
         using T = decltype(type);
         if (rows == 0 || f == 0) return nothing<T>(c, d, f, d_grad_x, d_grad_w_gate, d_grad_w_up);
         char *ws = (char *)d_workspace;
-        const uint64_t pitch = padded(f, sizeof(T)), vectors = rows * pitch / kPer<T>, blocks = ceil_div(vectors, 256);
+        const uint64_t pitch = filled(f, sizeof(T)), vectors = rows * pitch / kPer<T>, blocks = ceil_div(vectors, 256);
         T *const dg = (T *)ws, *const du = (T *)(ws + whole(rows * pitch * sizeof(T)));
         ws += 2 * whole(rows * pitch * sizeof(T));
         const bt_status s = launch(gated_slopes_kernel<T>, dim3((unsigned)(blocks < 1u << 20 ? blocks : 1u << 20)), 256, c.hs, (const T *)d_grad_h, (const T *)d_gate,
@@ -936,7 +976,7 @@ size_t bt_expert_linear_workspace_bytes(const bt_expert_plan *plan, uint64_t d_i
     if (check(plan, d_in, d_out, dtype) != BT_OK || plan->tokens == 0 || d_out == 0) return 0;
     const uint64_t rows = plan->tokens * plan->chosen, w = (uint64_t)width_of(dtype), copies = copies_bytes(*plan, d_in, d_out, 1, (int)w, ordered != 0, backward != 0);
     if (!backward) return (size_t)copies;
-    return (size_t)(copies + (pads(*plan, d_out, (int)w) ? whole(rows * padded(d_out, (int)w) * w) : 0) + (ordered ? 0 : whole(4 * rows * d_in)));
+    return (size_t)(copies + (pads(*plan, d_out, (int)w) ? whole(rows * filled(d_out, (int)w) * w) : 0) + (ordered ? 0 : whole(4 * rows * d_in)));
 }
 
 bt_status bt_expert_linear_forward(const void *d_x, const void *d_w, const bt_expert_plan *plan, uint64_t d_in, uint64_t d_out, bt_dtype dtype, int ordered,
@@ -989,7 +1029,7 @@ bt_status bt_expert_linear_backward(const void *d_grad_y, const void *d_x, const
         const T *grad_y = (const T *)d_grad_y;
         uint64_t pitch = d_out;
         if (pads(*plan, d_out, sizeof(T))) {
-            pitch = padded(d_out, sizeof(T));
+            pitch = filled(d_out, sizeof(T));
             Copies<T> copy;
             grad_y = copy.add(&ws, d_grad_y, rows, d_out, pitch);
             const bt_status s = copy.run(c);

@@ -152,7 +152,7 @@ template <class T, Product K> __global__ __launch_bounds__(Small::THREADS, 2) vo
     const auto sum_of = [&](const uint32_t i) { return W::SUMS == 2 && i >= a_sum ? 1u : 0u; };
     const auto start_of = [&](const uint32_t i) { return (i - sum_of(i) * a_sum) * kK<T>; };
     if (K == kGradW || a.p[0].cols < kPer<T> || a.q[0].cols < kPer<T>) {
-        for (; t < last; ++t) w.staged(a.p[sum_of(t)], a.p[1], a.q[sum_of(t) + at.part], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, acc);
+        for (; t < last; ++t) w.staged(a.p[sum_of(t)], a.p[1], a.q[sum_of(t) + at.part], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, tiles[0] + W::P::BYTES, acc);
         end<T, K, Small>(a, acc, at);
         return;
     }
@@ -304,7 +304,7 @@ template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, 
             // The rest of the summed index, less than a tile, through registers: of the split that has the last whole tile, or the only one.
             const uint32_t behind = (sum + 1) * a_sum;
             if (a_sum * kK<T> < a.k && (a.splits == 1 || (split_start(a, at.split, a_sum * W::SUMS) < behind && behind <= split_start(a, at.split + 1, a_sum * W::SUMS)))) {
-                w.staged(a.p[sum], a.p[1], a.q[sum + at.part], at.n, at.m, a_sum * kK<T>, tiles, tiles + PB, acc);
+                w.staged(a.p[sum], a.p[1], a.q[sum + at.part], at.n, at.m, a_sum * kK<T>, tiles, tiles + PB, tiles + PB, acc);
                 through = true;
             }
         }

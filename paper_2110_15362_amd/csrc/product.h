@@ -26,8 +26,8 @@ __device__ inline int fresh(int x) {
 // Q) in element r of lane l: with P the operand along which the output is contiguous, a lane holds four neighbours of a row.
 
 template <class T> constexpr int kKStep = 4 * kPer<T>;       // 32 or, in single precision, 16
-constexpr int kKBytes = 64;                                  // of the summed index in a tile: one step
-template <class T> constexpr int kK = kKBytes / (int)sizeof(T);
+constexpr int kKBytes = 64;                                  // of the summed index in a step, and in a tile where it is not said otherwise (KB)
+template <class T, int KB = kKBytes> constexpr int kK = KB / (int)sizeof(T);
 
 template <class T> __device__ inline acc4 multiply(const raw16 p, const raw16 q, acc4 c) {
     if constexpr (std::is_same_v<T, bf16>) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p), __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
@@ -49,15 +49,15 @@ template <class T> __device__ inline acc4 multiply(const raw16 p, const raw16 q,
 
 enum Order { kAlong, kAcross };      // the summed index: along memory rows, across them
 
-template <class T, Order O, int N> struct Tile {      // N rows or columns of the product
-    static constexpr int ROWS = O == kAlong ? N : kK<T>;
-    static constexpr int CHUNKS = (O == kAlong ? kKBytes : N * (int)sizeof(T)) / kVec;      // of a row
+template <class T, Order O, int N, int KB = kKBytes> struct Tile {      // N rows or columns of the product
+    static constexpr int ROWS = O == kAlong ? N : kK<T, KB>;
+    static constexpr int CHUNKS = (O == kAlong ? KB : N * (int)sizeof(T)) / kVec;      // of a row
     static constexpr int BYTES = ROWS * CHUNKS * kVec;
 
     // (Of the rows that one fragment has, those of a lane share the key.)
-    __device__ static int place(const int row, const int chunk) {
-        int key;
-        if constexpr (O == kAlong) key = (row >> 1) & 2;
+    __host__ __device__ static constexpr int place(const int row, const int chunk) {
+        int key = 0;
+        if constexpr (O == kAlong) key = (row >> 1) & (KB == kKBytes ? 2 : 7);
         else if constexpr (sizeof(T) == 2 && CHUNKS == 8) key = 2 * (((row >> 1) & 1) | ((row >> 2) & 2));
         else if constexpr (sizeof(T) == 2) key = 2 * ((row & 3) | ((row >> 1) & 4));
         else key = 4 * ((row >> 2) & 3);
@@ -69,15 +69,17 @@ __device__ __attribute__((always_inline)) inline short4v transposed(BT_LDS short
 
 // A wave's fragments of a tile: F times 16 rows or columns from `first` on.  Where a lane reads depends on the fragment and the tile by constants
 // alone, but for one address (summed index along) or one a fragment (across).
-template <class T, Order O, int N, int F> struct Reader {
-    typedef Tile<T, O, N> L;
-    static constexpr int ROW = L::CHUNKS * kVec, READS = O == kAlong ? 1 : sizeof(T) == 2 ? 2 : 4;      // instructions a fragment
-    uint32_t at[O == kAlong ? 1 : F];
+template <class T, Order O, int N, int F, int KB = kKBytes> struct Reader {
+    typedef Tile<T, O, N, KB> L;
+    static constexpr int STEPS = KB / kKBytes, ROW = L::CHUNKS * kVec, READS = O == kAlong ? 1 : sizeof(T) == 2 ? 2 : 4;      // instructions a fragment
+    uint32_t at[O == kAlong ? STEPS : F];
 
     __device__ void start(const int first) {
         const int lane = threadIdx.x % kWave, group = lane / 16, t = lane % 16;
-        if constexpr (O == kAlong) at[0] = L::place(first + t, group);
-        else {
+        if constexpr (O == kAlong) {
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) at[s] = L::place(first + t, s * 4 + group);
+        } else {
 #pragma unroll
             for (int i = 0; i < F; ++i) {
                 const int n = first + i * 16;
@@ -87,20 +89,27 @@ template <class T, Order O, int N, int F> struct Reader {
         }
     }
 
-    __device__ raw16 read(const char *tile, const int i) const {
+    // The operand's tiles begin `bytes` into the LDS, as the compiler is not to know: it would add the constants of beyond 64 KiB up to a register for each read.
+    __device__ void move(const uint32_t bytes) {
+#pragma unroll
+        for (uint32_t &a : at) a = fresh(a + bytes);
+    }
+
+    // Fragment i of a step of the tile.
+    __device__ raw16 read(const char *tile, const int i, const int step = 0) const {
         if constexpr (O == kAlong) {
-            return *(const raw16 *)(tile + at[0] + i * 16 * ROW);
+            return *(const raw16 *)(tile + at[step] + i * 16 * ROW);
         } else if constexpr (sizeof(T) == 2) {
             // 16 lanes read 4 summed indices by 16 columns, 4 columns a lane, and get one column each
             typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
-            const char *const from = tile + at[i];
+            const char *const from = tile + at[i] + step * kK<T> * ROW;
             const uint2v low = __builtin_bit_cast(uint2v, transposed((BT_LDS short4v *)from));
             const uint2v high = __builtin_bit_cast(uint2v, transposed((BT_LDS short4v *)(from + 4 * ROW)));
             return raw16{low[0], low[1], high[0], high[1]};
         } else {
             raw16 v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = *(const uint32_t *)(tile + at[i] + j * ROW);
+            for (int j = 0; j < 4; ++j) v[j] = *(const uint32_t *)(tile + at[i] + (step * kK<T> + j) * ROW);
             return v;
         }
     }
@@ -139,8 +148,8 @@ struct InOrder {
 };
 
 // Chunks of a tile on their way from memory to LDS, in registers.  (F: of the forward pass, fragments of a wave.)
-template <class T, Order O, int N, int F, int kThreads> struct Staged {
-    typedef Tile<T, O, N> L;
+template <class T, Order O, int N, int F, int kThreads, int KB = kKBytes> struct Staged {
+    typedef Tile<T, O, N, KB> L;
     static constexpr int PER = L::ROWS * L::CHUNKS / kThreads;
     raw16 v[PER];
 
@@ -357,15 +366,15 @@ __device__ inline raw16 eight_neighbours(uint32_t (&low)[2], uint32_t (&high)[2]
 constexpr int kTogether = 2;
 
 // What the kernels of a product share: their waves, tiles and steps.
-template <class T, class F, class S> struct Work {
-    typedef Tile<T, F::P, S::NP> P;
-    typedef Tile<T, F::Q, S::NQ> Q;
+template <class T, class F, class S, int KB = kKBytes> struct Work {
+    typedef Tile<T, F::P, S::NP, KB> P;
+    typedef Tile<T, F::Q, S::NQ, KB> Q;
     typedef acc4 Sums[S::FP][S::FQ];
     static constexpr int COLS = F::PAIR ? S::NP / 2 : S::NP;      // columns of the output in a tile
     static constexpr int SUMS = F::SUMS;
 
-    Reader<T, F::P, S::NP, S::FP> rp;
-    Reader<T, F::Q, S::NQ, S::FQ> rq;
+    Reader<T, F::P, S::NP, S::FP, KB> rp;
+    Reader<T, F::Q, S::NQ, S::FQ, KB> rq;
     raw16 p[2][S::FP], q[S::FQ];      // fragments: of P of a tile and the next one, of Q the halves in turn
 
     __device__ Work() {
@@ -373,13 +382,13 @@ template <class T, class F, class S> struct Work {
         rp.start((wave / 2) * S::FP * 16);
         rq.start((wave % 2) * S::FQ * 16);
     }
-    __device__ void read_p(const char *tile, const int parity) {
+    __device__ void read_p(const char *tile, const int parity, const int step = 0) {
 #pragma unroll
-        for (int i = 0; i < S::FP; ++i) p[parity][i] = rp.read(tile, i);
+        for (int i = 0; i < S::FP; ++i) p[parity][i] = rp.read(tile, i, step);
     }
-    __device__ void read_q(const char *tile, const int half) {
+    __device__ void read_q(const char *tile, const int half, const int step = 0) {
 #pragma unroll
-        for (int j = half * S::FQ / 2; j < (half + 1) * S::FQ / 2; ++j) q[j] = rq.read(tile, j);
+        for (int j = half * S::FQ / 2; j < (half + 1) * S::FQ / 2; ++j) q[j] = rq.read(tile, j, step);
     }
     __device__ void multiply(Sums &acc, const int parity, const int half) {
 #pragma unroll
@@ -390,21 +399,25 @@ template <class T, class F, class S> struct Work {
 
     // The products of two tiles that lie in LDS, with nothing else on its way.
     __device__ void multiply_all(Sums &acc, const char *tile_p, const char *tile_q) {
-        read_p(tile_p, 0);
-        read_q(tile_q, 0);
-        read_q(tile_q, 1);
-        multiply(acc, 0, 0);
-        multiply(acc, 0, 1);
+#pragma unroll
+        for (int step = 0; step < KB / kKBytes; ++step) {
+            read_p(tile_p, 0, step);
+            read_q(tile_q, 0, step);
+            read_q(tile_q, 1, step);
+            multiply(acc, 0, 0);
+            multiply(acc, 0, 1);
+        }
     }
 
     // Tiles through registers.
-    typedef Staged<T, F::P, S::NP, S::FP, S::THREADS> ThroughP;
-    typedef Staged<T, F::Q, S::NQ, S::FQ, S::THREADS> ThroughQ;
+    typedef Staged<T, F::P, S::NP, S::FP, S::THREADS, KB> ThroughP;
+    typedef Staged<T, F::Q, S::NQ, S::FQ, S::THREADS, KB> ThroughQ;
 
-    // The tiles that begin at column n and row m of the output and at k of the summed index, and their products.  (`other`: of a pair the second weight.)
+    // The tiles that begin at column n and row m of the output and at k of the summed index, and their products.  (`other`: of a pair the second weight; `from_q`: as the reader, which
+    // may have been moved, is to be given tile_q.)
     template <class MapP = InOrder, class MapQ = InOrder>
     __device__ void staged(const Operand &op, const Operand &other, const Operand &oq, const uint32_t n, const uint32_t m, const uint32_t k, char *tile_p, char *tile_q,
-                           Sums &acc, const MapP &rows_p = {}, const MapQ &rows_q = {}) {
+                           const char *from_q, Sums &acc, const MapP &rows_p = {}, const MapQ &rows_q = {}) {
         __syncthreads();
         {
             ThroughP sp;
@@ -417,16 +430,16 @@ template <class T, class F, class S> struct Work {
             sq.store(tile_q);
         }
         __syncthreads();
-        multiply_all(acc, tile_p, tile_q);
+        multiply_all(acc, tile_p, from_q);
     }
 };
 
 // An operand's tiles straight from memory to LDS, 1 KiB an instruction of a wave, an equal part of the tile a wave.  Needs rows of whole vectors on
 // 16-byte boundaries.  What a tile has beyond the operand's rows (or, where the summed index lies across, columns) is read from inside of it: it
 // belongs to rows or columns of the product that are not stored.
-template <class T, Order O, int N, int WAVES, bool ROUND> struct Direct {
-    typedef Tile<T, O, N> L;
-    static constexpr int S = (int)sizeof(T), PER = N / 16 / WAVES;
+template <class T, Order O, int N, int WAVES, bool ROUND, int KB = kKBytes> struct Direct {
+    typedef Tile<T, O, N, KB> L;
+    static constexpr int S = (int)sizeof(T), PER = N * KB / 1024 / WAVES;
     uint32_t offset[PER];        // of the lane's vector in each instruction's KiB, from the tile's first
     const char *base;
     uint64_t advance, round;     // bytes from one tile to the next; of all tiles
@@ -445,7 +458,7 @@ template <class T, Order O, int N, int WAVES, bool ROUND> struct Direct {
             offset[i] = (uint32_t)(row * a.pitch + col) * S;
         }
         base = (const char *)a.p + (O == kAlong ? n * a.pitch : (uint64_t)n) * S;
-        advance = (O == kAlong ? kK<T> : kK<T> * a.pitch) * S;
+        advance = (O == kAlong ? kK<T, KB> : kK<T, KB> * a.pitch) * S;
     }
     // Rows that do not lie one behind the other: those of `map` from n on, of the a.rows that there are.
     template <class Map> __device__ void start_rows(const Operand &a, const uint32_t n, const Map &map) {
@@ -458,11 +471,11 @@ template <class T, Order O, int N, int WAVES, bool ROUND> struct Direct {
             offset[i] = (uint32_t)(map(row) * a.pitch + chunk * kPer<T>) * S;
         }
         base = (const char *)a.p;
-        advance = kK<T> * S;
+        advance = kK<T, KB> * S;
     }
     // The forward pass: rows of the two weights in turn, 8 F of each.  The loading wave's part of the tile is one such run.
     template <int F> __device__ void start_pair(const Operand &gate, const Operand &up, const uint32_t n) {
-        static_assert(2 * PER == F, "a wave's part belongs to one weight");
+        static_assert(N / WAVES == 8 * F, "a wave's part belongs to one weight");
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const uint32_t first = n + wave / 2 * F * 8;         // row of the weight that the part begins with
         const Operand &a = wave % 2 ? up : gate;
