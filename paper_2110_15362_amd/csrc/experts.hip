@@ -356,16 +356,17 @@ template <class T, Order O, int N, int WAVES, int KB> struct Looped : Direct<T, 
 
 // Tiles of either operand in LDS, the next ones on their way while one is multiplied, in steps of 64 bytes of the summed index; workgroups of the largest tiles take several.  A step's products are made in two halves
 // (of Q's fragments): while the first is made the second's fragments are read, while the second is made the next step's first ones.  Behind the barrier in a tile's last step, between its halves, the next tile has
-// landed and all waves have read what they need of this one: another is asked for in its place.  x's rows are fetched from where their tokens have them, or, for the weights' gradients, from a copy in the order of the
-// experts.
+// landed and all waves have read what they need of this one.  x's rows are fetched from where their tokens have them, or, for the weights' gradients, from a copy in the order of the experts.
 //
-// Where the summed index lies along an operand's rows a tile has whole 128-byte lines, and two lie in LDS: with tiles of 64 bytes, of which there were four, the L2 was read twice as often (32768 rows, eight
-// weights of [2048, 4096] in bf16: forward @585@ us, grad_x @520@).  The weights' gradients, whose tiles have lines of 512 bytes, have four of 64.
-template <Kind K> constexpr int kTileBytes = K == kWeights ? kKBytes : 2 * kKBytes;
-template <Kind K> constexpr int kPlaces = K == kWeights ? 4 : 2;
+// The forward pass, both of whose operands have the summed index along their rows, has tiles of whole 128-byte lines, two of them in LDS, and asks for a tile as soon as its place is free.  The others have four of 64
+// bytes, and ask for one among the first products of a step.  (us, 32768 rows, eight weights of [2048, 4096] in bf16, both ways: forward 567 and 590, grad_x 545 and 521, the weights' gradients 430 and 405.)
+template <Kind K> constexpr int kTileBytes = K <= kPlain ? 2 * kKBytes : kKBytes;
+template <Kind K> constexpr int kPlaces = K <= kPlain ? 2 : 4;
 
 template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void experts_kernel(const ExpertJob a) {
     constexpr int KB = kTileBytes<K>, PLACES = kPlaces<K>, STEPS = KB / kKBytes, kKs = kK<T, KB>;
+    constexpr int kAhead = STEPS == 1 ? PLACES - 1 : PLACES;      // from a tile to the furthest that it asks for
+    constexpr int kLeft = STEPS == 1 ? kAhead - 1 : PLACES - 2;   // tiles that may be on their way behind the next
     typedef FormOf<K> F;
     typedef Work<T, F, S, KB> W;
     // Each XCD begins elsewhere in the summed index, as the dense projections do; the weights' gradients sum over rows, of which each expert has other numbers.
@@ -406,7 +407,7 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
         dp.rotate(F::SUMS == 2 ? (const char *)a.p[1] - (const char *)a.p[0] : 0, phase, each, k);
         dq.rotate(F::SUMS == 2 ? (const char *)a.q[1] - (const char *)a.q[0] : 0, phase, each, k);
 #pragma unroll
-        for (int t = 0; t < PLACES; ++t)
+        for (int t = 0; t < kAhead; ++t)
             if ((uint32_t)t < count) {
                 dp.fetch(tile_p(t));
                 dq.fetch(tile_q(t));
@@ -415,13 +416,25 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
     };
     Place at = place_of<K>(a, map, number, total, S::NQ, W::COLS);
     uint32_t count = begin(at);
+    number += gridDim.x;
+    // (The smaller tiles' workgroups take one each; a launch has them all unless there are more than it holds.)
+    constexpr bool kSeveral = S::THREADS == Large::THREADS;
     bool stored = false;      // since the first tiles were asked for: by each lane, kStores of each output or more
     constexpr int kStores = kStoresAtLeast<T, K, S::FP, S::FQ>;
     for (;;) {
+        // The next tile's place is looked up while this one's first fetches are on their way.
+        const bool more = kSeveral && number < total;
+        Place next = at;
+        if (more) next = place_of<K>(a, map, number, total, S::NQ, W::COLS);
         typename W::Sums acc = {};
-        // Tile i of a turn, which lies in place i % PLACES, with `left` tiles from it to the end.
-        const auto tile = [&](auto turn_number, const uint32_t left) {
+#pragma unroll
+        for (auto &row : acc)
+#pragma unroll
+            for (acc4 &x : row) asm volatile("" : "+v"(x));      // (or the first turn, which begins with zeros, gets registers of its own)
+        // Tile i of a turn, which lies in place i % PLACES, with `left` tiles from it to the end.  FIRST: of the first turn, whose next tiles but the last one were asked for before the stores.
+        const auto tile = [&](auto turn_number, const uint32_t left, auto first) {
             constexpr int i = decltype(turn_number)::value, kParity = STEPS == 1 ? i & 1 : 0;
+            constexpr bool FIRST = decltype(first)::value && i < kAhead - 1;
             if constexpr (STEPS == 2) {
                 read_q(i, 1, 0);
                 w.multiply(acc, 0, 0);
@@ -435,40 +448,51 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
             }
             constexpr int kLast = STEPS == 1 ? kParity : 1, kNext = STEPS == 1 ? 1 - kParity : 0;
             read_q(i, 1, STEPS - 1);
+            if (STEPS == 1 && left > kAhead) {
+                dp.fetch(tile_p(i + kAhead));
+                dq.fetch(tile_q(i + kAhead));
+            }
             w.multiply(acc, kLast, 0);
-            spread<kReadsQ, 0, kProducts>();
+            spread<kReadsQ, STEPS == 1 ? kFetches : 0, kProducts>();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the last fragments of this tile are here
             // The next tile has come: what is asked for behind it may still be on its way.
-            if (PLACES > 2 && left >= PLACES) wait_for_tiles<(PLACES - 2) * kFetches>();
+            if (FIRST && K == kPair && a.gate) wait_for_tiles<kLeft * kFetches + (K == kPair ? 3 : 1) * kStores>();
+            else if (FIRST) wait_for_tiles<kLeft * kFetches + kStores>();
+            else if (kLeft != 0 && left > kAhead) wait_for_tiles<kLeft * kFetches>();
             else wait_for_tiles<0>();
             w.read_p(tile_p(i + 1), kNext, 0);      // (behind the last tile: what lies there, unused)
             read_q(i + 1, 0, 0);
-            if (left > PLACES) {
+            if (STEPS == 2 && left > kAhead) {
                 dp.fetch(tile_p(i));
                 dq.fetch(tile_q(i));
             }
             w.multiply(acc, kLast, 1);
-            spread<kReadsP + kReadsQ, kFetches, kProducts>();
+            spread<kReadsP + kReadsQ, STEPS == 2 ? kFetches : 0, kProducts>();
             __builtin_amdgcn_sched_barrier(0);
         };
         const uint32_t k = summed<K>(a, at.of), rest = whole_only ? k / kKs * kKs : k;
         if (count != 0) {
             // The first tile of every wave has to be in LDS.  Fetches and stores are counted together, in order: of those that may still be on their way, the first tile's fetches are
             // followed by those of the other places and by the stores.
-            constexpr int kBehind = (PLACES - 1) * kFetches;
-            if (count < PLACES) wait_for_tiles<0>();
+            constexpr int kBehind = (kAhead - 1) * kFetches;
+            if (count < kAhead) wait_for_tiles<0>();
             else if (!stored) wait_for_tiles<kBehind>();
             else if (K == kPair && a.gate) wait_for_tiles<kBehind + (K == kPair ? 3 : 1) * kStores>();
             else wait_for_tiles<kBehind + kStores>();
             w.read_p(tile_p(0), 0, 0);
             read_q(0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
+            constexpr uint32_t kMany = PLACES + kAhead;
             uint32_t t = 0;
-            for (; t + 2 * PLACES <= count; t += PLACES) turn<PLACES>([&](auto i) { tile(i, 2 * PLACES); });
+            if (S::THREADS == Large::THREADS && stored && count >= kMany) {
+                turn<PLACES>([&](auto i) { tile(i, kMany, std::true_type{}); });
+                t = PLACES;
+            }
+            for (; t + kMany <= count; t += PLACES) turn<PLACES>([&](auto i) { tile(i, kMany, std::false_type{}); });
             for (; t < count; t += PLACES)
                 turn<PLACES>([&](auto i) {
-                    if (t + decltype(i)::value < count) tile(i, count - t - decltype(i)::value);
+                    if (t + decltype(i)::value < count) tile(i, count - t - decltype(i)::value, std::false_type{});
                 });
         }
         // The rest of the summed index, less than a tile, through registers.
@@ -483,12 +507,10 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
             }
         }
         const Place here = at;
-        number += gridDim.x;
-        // (The smaller tiles' workgroups take one each; a launch has them all unless there are more than it holds.)
-        const bool more = S::THREADS == Large::THREADS && number < total;
         if (more) {
             if (through) __syncthreads();
-            at = place_of<K>(a, map, number, total, S::NQ, W::COLS);
+            at = next;
+            number += gridDim.x;
             count = begin(at);
             asm volatile("" ::: "memory");      // (the stores stay behind the fetches: see the wait that counts both)
         }
