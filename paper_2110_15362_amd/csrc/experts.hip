@@ -25,8 +25,10 @@ struct ExpertJob {
     const int32_t *offsets, *source;   // source: x has a row a token; else NULL
     uint32_t experts, rows, tokens;
     uint32_t m, n, k;                  // kWeights: m by n of each expert, k is not used; else n columns and k summed indices
-    uint32_t tiles_m, tiles_n, parts;  // kWeights: tiles of an output, outputs; else tiles_n alone
+    uint32_t tiles_m, tiles_n, outputs;  // kWeights: tiles of an output, outputs; else tiles_n alone
     uint32_t first;                    // tile that the launch begins with
+    float *parts;                      // sums of the parts of tiles, see Round
+    uint32_t most_splits;              // parts that a tile may be in
     uint32_t padded_q;                 // kBack: q's rows go on with zeros to the end of a tile, as those of kBackPair do
     int activation;
 };
@@ -103,28 +105,46 @@ struct Tiles {
     }
 };
 
+// Workgroups that run at once, of a shape.
+template <class S> constexpr uint32_t kSlots = 256 * (S::THREADS == 512 ? 1 : S::FQ == 4 ? 2 : 4);
+
+// Parts of a tile's summed index are other workgroups' work where the last tiles, kSlots of which run at once, would leave most compute units idle: the tiles from `full` on are in `splits` parts each, whose sums
+// experts_join_kernel adds up.  How many there are follows from the tiles' number, and so from the experts' rows alone.
+struct Round {
+    uint32_t full, splits, tiles;
+
+    __device__ void find(const uint32_t total, const uint32_t slots, const uint32_t most) {
+        full = total / slots * slots;
+        const uint32_t rest = total - full;
+        splits = 1;
+        while (splits < most && rest * splits * 2 <= slots) splits *= 2;
+        tiles = full + rest * splits;
+    }
+};
+
 struct Place {
     Group of;
     uint32_t m, n, part;
+    uint32_t slot;      // of a part of a tile: which of the parts' sums are its, of a tile's parts in a row (else beyond them)
 };
 
-// Tiles that there are, and the tile of a number.  Workgroups go to the eight XCDs in turn, each of which has an L2 of its own.  Of the kRound tiles that run at once an XCD's are
+// Tiles that there are, and the tile of a number.  Workgroups go to the eight XCDs in turn, each of which has an L2 of its own.  Of the 256 tiles that run at once an XCD's are
 // neighbours, in bands of four rows of tiles of one expert, so that they share what they read; all XCDs are at the same expert, whose weights then come from memory once, and (the weights' gradients)
-// have sums of about the same length.  (kRound 256: one tile to a compute unit.)
+// have sums of about the same length.  (256: one tile to a compute unit.)
 template <Kind K> __device__ inline uint32_t tiles_of(const ExpertJob &a, const Tiles &tiles) {
-    if constexpr (K == kWeights) return a.experts * a.parts * a.tiles_m * a.tiles_n;
+    if constexpr (K == kWeights) return a.experts * a.outputs * a.tiles_m * a.tiles_n;
     else return tiles.count(a) * a.tiles_n;
 }
 
-template <Kind K> __device__ inline Place place_of(const ExpertJob &a, const Tiles &tiles, const uint32_t number, const uint32_t total, const uint32_t tile_m, const uint32_t tile_n) {
-    constexpr uint32_t kXcds = 8, kBand = 4, kRound = 256;
-    const uint32_t first = number / kRound * kRound, here = total - first < kRound ? total - first : kRound, xcd = number % kXcds, more = here % kXcds;
-    uint32_t tile = first + xcd * (here / kXcds) + (xcd < more ? xcd : more) + number % kRound / kXcds, rows;
+template <Kind K> __device__ inline Place tile_of(const ExpertJob &a, const Tiles &tiles, uint32_t tile, const uint32_t tile_m, const uint32_t tile_n) {
+    constexpr uint32_t kBand = 4;
     Place at;
+    at.slot = ~0u;
+    uint32_t rows;
     if constexpr (K == kWeights) {
-        const uint32_t a_part = a.tiles_m * a.tiles_n, e = tile / (a_part * a.parts);
+        const uint32_t a_part = a.tiles_m * a.tiles_n, e = tile / (a_part * a.outputs);
         at.of = group_of(a, e);
-        tile -= e * a_part * a.parts;
+        tile -= e * a_part * a.outputs;
         at.part = tile / a_part;
         tile -= at.part * a_part;
         rows = a.tiles_m;
@@ -140,6 +160,16 @@ template <Kind K> __device__ inline Place place_of(const ExpertJob &a, const Til
     tile -= band * kBand * a.tiles_n;
     at.m = (band * kBand + tile % high) * tile_m;
     at.n = tile / high * tile_n;
+    return at;
+}
+
+template <Kind K> __device__ inline Place place_of(const ExpertJob &a, const Tiles &tiles, const uint32_t number, const Round &r, const uint32_t tile_m, const uint32_t tile_n) {
+    constexpr uint32_t kXcds = 8, kTogether = 256;
+    const uint32_t first = number / kTogether * kTogether, here = r.tiles - first < kTogether ? r.tiles - first : kTogether, xcd = number % kXcds, more = here % kXcds;
+    const uint32_t item = first + xcd * (here / kXcds) + (xcd < more ? xcd : more) + number % kTogether / kXcds, slot = item - r.full;
+    const bool in_parts = item >= r.full;      // (or a whole one of the last)
+    Place at = tile_of<K>(a, tiles, in_parts ? r.full + slot / r.splits : item, tile_m, tile_n);
+    at.slot = in_parts && r.splits != 1 ? slot : ~0u;
     return at;
 }
 
@@ -238,7 +268,7 @@ template <class T, Kind K> __global__ __launch_bounds__(Small::THREADS, 2) void 
     if constexpr (K != kWeights) map.find(a, Small::NQ);
     const uint32_t total = tiles_of<K>(a, map), number = a.first + blockIdx.x;
     if (number >= total) return;
-    const Place at = place_of<K>(a, map, number, total, Small::NQ, W::COLS);
+    const Place at = place_of<K>(a, map, number, Round{total, 1, total}, Small::NQ, W::COLS);
     typename W::Sums acc = {};
     W w;
     const uint32_t k = summed<K>(a, at.of), a_sum = (k + kK<T> - 1) / kK<T>, last = a_sum * W::SUMS;
@@ -379,9 +409,10 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
     __shared__ __align__(1024) char tiles[PLACES * (PB + QB)];
     __shared__ Tiles map;
     if constexpr (K != kWeights) map.find(a, S::NQ);
-    const uint32_t total = tiles_of<K>(a, map);
+    Round r;
+    r.find(tiles_of<K>(a, map), kSlots<S>, a.most_splits);
     uint32_t number = a.first + blockIdx.x;
-    if (number >= total) return;
+    if (number >= r.tiles) return;
     W w;
     FetchP dp;
     FetchQ dq;
@@ -394,9 +425,14 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
     const bool whole_only = K <= kPlain || (K == kBack && a.padded_q == 0);
     // A tile's first fetches are asked for; returns how many tiles of the summed index it has.
     const auto begin = [&](const Place &at) {
-        const uint32_t k = summed<K>(a, at.of), each = __builtin_amdgcn_readfirstlane(whole_only ? k / kKs : (k + kKs - 1) / kKs), count = each * F::SUMS;
+        const uint32_t k = summed<K>(a, at.of), each = __builtin_amdgcn_readfirstlane(whole_only ? k / kKs : (k + kKs - 1) / kKs);
+        uint32_t count = each * F::SUMS, phase = kRound ? (uint32_t)((uint64_t)(blockIdx.x % 8) * count / 8) : 0;
+        if (at.slot != ~0u) {
+            const uint32_t split = at.slot % r.splits;
+            phase = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)count * split / r.splits));
+            count = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)count * (split + 1) / r.splits)) - phase;
+        }
         if (count == 0) return 0u;
-        const uint32_t phase = kRound ? (uint32_t)((uint64_t)(blockIdx.x % 8) * count / 8) : 0;
         if constexpr (K == kPair) dp.template start_pair<S::FP>(operand_p<T, K>(a, at.of, 0), operand_p<T, K>(a, at.of, 1), at.n);
         else dp.start(operand_p<T, K>(a, at.of, 0), at.n);
         const Operand q = operand_q<T, K>(a, at.of, K == kWeights ? at.part : 0);
@@ -414,7 +450,7 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
             }
         return count;
     };
-    Place at = place_of<K>(a, map, number, total, S::NQ, W::COLS);
+    Place at = place_of<K>(a, map, number, r, S::NQ, W::COLS);
     uint32_t count = begin(at);
     number += gridDim.x;
     // (The smaller tiles' workgroups take one each; a launch has them all unless there are more than it holds.)
@@ -423,18 +459,13 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
     constexpr int kStores = kStoresAtLeast<T, K, S::FP, S::FQ>;
     for (;;) {
         // The next tile's place is looked up while this one's first fetches are on their way.
-        const bool more = kSeveral && number < total;
+        const bool more = kSeveral && number < r.tiles;
         Place next = at;
-        if (more) next = place_of<K>(a, map, number, total, S::NQ, W::COLS);
+        if (more) next = place_of<K>(a, map, number, r, S::NQ, W::COLS);
         typename W::Sums acc = {};
-#pragma unroll
-        for (auto &row : acc)
-#pragma unroll
-            for (acc4 &x : row) asm volatile("" : "+v"(x));      // (or the first turn, which begins with zeros, gets registers of its own)
-        // Tile i of a turn, which lies in place i % PLACES, with `left` tiles from it to the end.  FIRST: of the first turn, whose next tiles but the last one were asked for before the stores.
-        const auto tile = [&](auto turn_number, const uint32_t left, auto first) {
+        // Tile i of a turn, which lies in place i % PLACES, with `left` tiles from it to the end.
+        const auto tile = [&](auto turn_number, const uint32_t left) {
             constexpr int i = decltype(turn_number)::value, kParity = STEPS == 1 ? i & 1 : 0;
-            constexpr bool FIRST = decltype(first)::value && i < kAhead - 1;
             if constexpr (STEPS == 2) {
                 read_q(i, 1, 0);
                 w.multiply(acc, 0, 0);
@@ -457,9 +488,7 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the last fragments of this tile are here
             // The next tile has come: what is asked for behind it may still be on its way.
-            if (FIRST && K == kPair && a.gate) wait_for_tiles<kLeft * kFetches + (K == kPair ? 3 : 1) * kStores>();
-            else if (FIRST) wait_for_tiles<kLeft * kFetches + kStores>();
-            else if (kLeft != 0 && left > kAhead) wait_for_tiles<kLeft * kFetches>();
+            if (kLeft != 0 && left > kAhead) wait_for_tiles<kLeft * kFetches>();
             else wait_for_tiles<0>();
             w.read_p(tile_p(i + 1), kNext, 0);      // (behind the last tile: what lies there, unused)
             read_q(i + 1, 0, 0);
@@ -485,18 +514,15 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
             __builtin_amdgcn_sched_barrier(0);
             constexpr uint32_t kMany = PLACES + kAhead;
             uint32_t t = 0;
-            if (S::THREADS == Large::THREADS && stored && count >= kMany) {
-                turn<PLACES>([&](auto i) { tile(i, kMany, std::true_type{}); });
-                t = PLACES;
-            }
-            for (; t + kMany <= count; t += PLACES) turn<PLACES>([&](auto i) { tile(i, kMany, std::false_type{}); });
+            for (; t + kMany <= count; t += PLACES) turn<PLACES>([&](auto i) { tile(i, kMany); });
             for (; t < count; t += PLACES)
                 turn<PLACES>([&](auto i) {
-                    if (t + decltype(i)::value < count) tile(i, count - t - decltype(i)::value, std::false_type{});
+                    if (t + decltype(i)::value < count) tile(i, count - t - decltype(i)::value);
                 });
         }
         // The rest of the summed index, less than a tile, through registers.
-        const bool through = (K <= kPlain || K == kBack) && rest < k;
+        const bool in_parts = at.slot != ~0u;
+        const bool through = (K <= kPlain || K == kBack) && rest < k && (!in_parts || at.slot % r.splits + 1 == r.splits);
         if (through) {
 #pragma unroll 1
             for (int sum = 0; sum < F::SUMS; ++sum) {
@@ -514,10 +540,50 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
             count = begin(at);
             asm volatile("" ::: "memory");      // (the stores stay behind the fetches: see the wait that counts both)
         }
-        end<T, K, S>(a, acc, here);
+        if (in_parts) {
+            float *const to = a.parts + (uint64_t)here.slot * (S::NP * S::NQ) + threadIdx.x * 4;
+#pragma unroll
+            for (int i = 0; i < S::FP; ++i)
+#pragma unroll
+                for (int j = 0; j < S::FQ; ++j) *(acc4 *)(to + (i * S::FQ + j) * (S::THREADS * 4)) = acc[i][j];
+        } else end<T, K, S>(a, acc, here);
         if (!more) break;
-        stored = sizeof(T) == 2 && here.m + S::NQ <= (K == kWeights ? a.m : here.of.rows) && here.n + W::COLS <= a.n;
+        stored = sizeof(T) == 2 && !in_parts && here.m + S::NQ <= (K == kWeights ? a.m : here.of.rows) && here.n + W::COLS <= a.n;
     }
+}
+
+// The parts of the last tiles added up, in order, and what becomes of the sums: kSlice of Q's fragments a workgroup, each lane those that it has in experts_kernel.  Bound by memory.
+constexpr int kSlice = 2;
+
+template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS) void experts_join_kernel(const ExpertJob a) {
+    constexpr int kCols = Work<T, FormOf<K>, S>::COLS, kSlices = S::FQ / kSlice;
+    __shared__ Tiles map;
+    if constexpr (K != kWeights) map.find(a, S::NQ);
+    Round r;
+    r.find(tiles_of<K>(a, map), kSlots<S>, a.most_splits);
+    const uint32_t tile = blockIdx.x / kSlices, slice = blockIdx.x % kSlices;
+    if (r.splits == 1 || tile * r.splits >= r.tiles - r.full) return;
+    acc4 acc[S::FP][kSlice] = {};
+    const float *const from = a.parts + (uint64_t)tile * r.splits * (S::NP * S::NQ) + slice * kSlice * (S::THREADS * 4) + threadIdx.x * 4;
+    for (uint32_t split = 0; split < r.splits; split += 2) {
+        acc4 x[2][S::FP][kSlice];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < S::FP; ++i)
+#pragma unroll
+                for (int j = 0; j < kSlice; ++j) x[h][i][j] = *(const acc4 *)(from + (uint64_t)(split + h) * (S::NP * S::NQ) + (i * S::FQ + j) * (S::THREADS * 4));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < S::FP; ++i)
+#pragma unroll
+                for (int j = 0; j < kSlice; ++j) acc[i][j] += x[h][i][j];
+    }
+    // (As the place of a whole tile.)
+    const Place at = tile_of<K>(a, map, r.full + tile, S::NQ, kCols);
+    const int wave = threadIdx.x / kWave;
+    finish<T, K, S::FP, kSlice>(a, acc, at.m + (wave % 2) * S::FQ * 16 + slice * kSlice * 16, at.n + (wave / 2) * (kCols / S::WP), at);
 }
 
 // Few rows an expert (tokens to answer with): as gated_tokens_kernel, for 16 columns and FQ times 16 rows of one expert.  The weights are read once for as many rows and bound
@@ -728,11 +794,33 @@ Size size_of(const Kind kind, const uint64_t rows, const uint64_t experts, const
     return best;
 }
 
+// Into how many parts the last tiles may go (a power of two), and the bytes that the parts' sums take: none where the time of a tile that parts would save, by the steps' time that size_of's model has and the number of
+// tiles that experts with the same number of rows would have, is not well above that of the join, 5 to 15 us (bf16 [32768, 4096] x 8 weights of [4096, 2048] twice, grad_x: 1183 -> 1080 us; with parts
+// everywhere bf16 [65536, 1024] x 32 weights of [2048, 1024] 333 -> 342).
+struct Parts {
+    uint32_t most;
+    uint64_t bytes;
+};
+Parts parts_of(const Kind kind, const Size size, const uint64_t rows, const uint64_t experts, const uint64_t m, const uint64_t n, const uint64_t k, const uint64_t outputs, const int width) {
+    const uint64_t side = size == kLarge ? 256 : size == kMiddle ? 128 : 64, slots = size == kLarge ? 256 : size == kMiddle ? 512 : 1024;
+    const uint64_t steps = ceil_div((kind == kWeights ? rows / experts : k) * width, kKBytes) * (kind == kBackPair ? 2 : 1);
+    const uint64_t tiles_m = kind == kWeights ? ceil_div(m, side) * experts * outputs : rows / side + experts / 2 + 1, tiles = tiles_m * ceil_div(n, kind == kPair ? side / 2 : side);
+    Parts p = {1, 0};
+    const double step = size == kLarge ? 0.75 : size == kMiddle ? 0.38 : 0.28;      // us
+    const uint64_t rest = tiles % slots;
+    uint64_t splits = 1;
+    while (splits < 16 && rest * splits * 2 <= slots && steps / (splits * 2) >= 16) splits *= 2;
+    if ((double)steps * step * (1.0 - 1.0 / (double)splits) < 20.0) return p;
+    while (p.most < 16 && steps / (p.most * 2) >= 16) p.most *= 2;
+    p.bytes = slots * side * side * 4;
+    return p;
+}
+
 // Rows of whole vectors on 16-byte boundaries, and a tile within 32 bits of offsets.
 template <class T> bool direct(const void *p, const uint64_t pitch) { return !misaligned(p, kVec) && pitch % kPer<T> == 0 && pitch * sizeof(T) * 320 < 1u << 31; }
 
 template <class T, Kind K> bt_status run_product(ExpertJob &a, hipStream_t hs) {
-    const auto go = [&](auto kernel, const uint32_t rows, const uint32_t cols, const int threads) {
+    const auto go = [&](auto kernel, const uint32_t rows, const uint32_t cols, const int threads, const uint32_t slots = 0) {
         const uint64_t tiles_n = ceil_div(a.n, cols);
         uint64_t tiles_m;
         if (K == kWeights) tiles_m = ceil_div(a.m, rows);
@@ -740,24 +828,31 @@ template <class T, Kind K> bt_status run_product(ExpertJob &a, hipStream_t hs) {
             tiles_m = a.rows / rows + a.experts + 1;
             if (tiles_m > a.rows) tiles_m = a.rows;
         }
-        const uint64_t groups = tiles_m * tiles_n * (K == kWeights ? (uint64_t)a.experts * a.parts : 1);
+        const uint64_t groups = tiles_m * tiles_n * (K == kWeights ? (uint64_t)a.experts * a.outputs : 1);
         if (groups >= 1u << 31) return BT_ERR_SIZE;
         a.tiles_m = (uint32_t)tiles_m;
         a.tiles_n = (uint32_t)tiles_n;
         a.first = 0;
+        // (What is in parts are at most as many workgroups as run at once.)
+        const uint64_t items = a.most_splits > 1 ? groups + slots : groups;
         // The largest tiles' workgroups, one to a compute unit, take several each.
-        if (threads == Large::THREADS && rows == Large::NQ) return launch(kernel, dim3((unsigned)(groups < 256 ? groups : 256)), threads, hs, a);
+        if (threads == Large::THREADS && rows == Large::NQ) return launch(kernel, dim3((unsigned)(items < 256 ? items : 256)), threads, hs, a);
         constexpr uint64_t kMost = 1u << 22;      // of a launch: a grid holds less than 2^32 threads
         bt_status s = BT_OK;
-        for (uint64_t first = 0; first < groups && s == BT_OK; first += kMost) {
+        for (uint64_t first = 0; first < items && s == BT_OK; first += kMost) {
             a.first = (uint32_t)first;
-            s = launch(kernel, dim3((unsigned)(groups - first < kMost ? groups - first : kMost)), threads, hs, a);
+            s = launch(kernel, dim3((unsigned)(items - first < kMost ? items - first : kMost)), threads, hs, a);
         }
         return s;
     };
-    const auto tiled = [&](auto kernel, auto shape) {
+    a.most_splits = 1;
+    const auto tiled = [&](auto kernel, auto join, auto shape) {
         typedef decltype(shape) S;
-        return go(kernel, S::NQ, K == kPair ? S::NP / 2 : S::NP, S::THREADS);
+        const Parts parts = parts_of(K, S::THREADS == 512 ? kLarge : S::FQ == 4 ? kMiddle : kSmall, a.rows, a.experts, a.m, a.n, a.k, a.outputs, sizeof(T));
+        a.most_splits = parts.most;
+        const bt_status s = go(kernel, S::NQ, K == kPair ? S::NP / 2 : S::NP, S::THREADS, kSlots<S>);
+        if (s != BT_OK || parts.most == 1) return s;
+        return launch(join, dim3(kSlots<S> / 2 * (S::FQ / kSlice)), S::THREADS, hs, a);
     };
     const uint64_t each_has = a.rows / a.experts;
     if constexpr (K <= kPlain) {
@@ -771,15 +866,15 @@ template <class T, Kind K> bt_status run_product(ExpertJob &a, hipStream_t hs) {
     }
     bool straight = direct<T>(a.p[0], a.pitch_p) && direct<T>(a.q[0], a.pitch_q);
     if (K == kPair || K == kBackPair) straight = straight && direct<T>(a.p[1], a.pitch_p);
-    if (K == kBackPair || (K == kWeights && a.parts == 2)) straight = straight && direct<T>(a.q[1], a.pitch_q);
+    if (K == kBackPair || (K == kWeights && a.outputs == 2)) straight = straight && direct<T>(a.q[1], a.pitch_q);
     if (a.source) straight = straight && K <= kPlain && a.tokens * a.pitch_q * sizeof(T) < 1u << 31;
-    if (!straight) return tiled(experts_any_kernel<T, K>, Small{});
-    const Size size = size_of(K, a.rows, a.experts, a.m, a.n, a.k, a.parts, sizeof(T));
+    if (!straight) return go(experts_any_kernel<T, K>, Small::NQ, K == kPair ? Small::NP / 2 : Small::NP, Small::THREADS);
+    const Size size = size_of(K, a.rows, a.experts, a.m, a.n, a.k, a.outputs, sizeof(T));
     if constexpr (sizeof(T) == 2) {
-        if (size == kLarge) return tiled(experts_kernel<T, K, Large>, Large{});
-        if (size == kMiddle) return tiled(experts_kernel<T, K, Middle>, Middle{});
+        if (size == kLarge) return tiled(experts_kernel<T, K, Large>, experts_join_kernel<T, K, Large>, Large{});
+        if (size == kMiddle) return tiled(experts_kernel<T, K, Middle>, experts_join_kernel<T, K, Middle>, Middle{});
     }
-    return tiled(experts_kernel<T, K, Small>, Small{});
+    return tiled(experts_kernel<T, K, Small>, experts_join_kernel<T, K, Small>, Small{});
 }
 
 // What is to be copied, and where to in the workspace.
@@ -832,6 +927,20 @@ bt_status check_tables(const bt_expert_plan &plan, const bool ordered, const boo
 
 template <class... P> bool any_misaligned(const size_t a, P... p) { return (misaligned(p, a) || ...); }
 
+// Bytes of the sums of parts of tiles, of the forward pass and of the larger of both backward products.
+uint64_t parts_bytes(const bt_expert_plan &p, const Kind kind, const uint64_t m, const uint64_t n, const uint64_t k, const uint64_t outputs, const int width) {
+    const uint64_t rows = p.tokens * p.chosen;
+    if (kind <= kPlain && each(p) <= kTokensEach) return 0;
+    return whole(parts_of(kind, size_of(kind, rows, p.experts, m, n, k, outputs, width), rows, p.experts, m, n, k, outputs, width).bytes);
+}
+uint64_t forward_parts(const bt_expert_plan &p, const uint64_t d, const uint64_t f, const bool pair, const int width) {
+    return parts_bytes(p, pair ? kPair : kPlain, 0, f, pads(p, d, width) ? filled(d, width) : d, 0, width);
+}
+uint64_t backward_parts(const bt_expert_plan &p, const uint64_t d, const uint64_t f, const bool pair, const int width) {
+    const uint64_t x = parts_bytes(p, pair ? kBackPair : kBack, 0, d, f, 0, width), weights = parts_bytes(p, kWeights, f, d, 0, pair ? 2 : 1, width);
+    return x > weights ? x : weights;
+}
+
 // x and one weight (w_up NULL) or two of the forward pass, as they are or copied.
 template <class T>
 bt_status operands(const Call &c, ExpertJob &a, const void *x, const void *w_gate, const void *w_up, const uint64_t d, const uint64_t f, char *ws) {
@@ -851,6 +960,7 @@ bt_status operands(const Call &c, ExpertJob &a, const void *x, const void *w_gat
     a.pitch_p = a.pitch_q = pitch;
     a.step = f * pitch;
     a.k = (uint32_t)pitch;
+    a.parts = (float *)ws;
     return s;
 }
 
@@ -866,9 +976,11 @@ bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch
         w_gate = copies.add(&ws, w_gate, c.plan.experts * f, d, pitch, nullptr, grad_x != nullptr);
         if (du) w_up = copies.add(&ws, w_up, c.plan.experts * f, d, pitch, nullptr, grad_x != nullptr);
     }
+    float *const sums = (float *)ws, *const parts = (float *)(ws + (c.ordered ? 0 : whole(4 * c.rows() * d)));
     bt_status s = copies.run(c);
     if (s == BT_OK && grad_x) {
         ExpertJob a = c.job();
+        a.parts = parts;
         a.p[0] = w_gate;
         a.p[1] = w_up;
         a.q[0] = dg;
@@ -881,7 +993,7 @@ bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch
         a.k = (uint32_t)f;
         a.padded_q = pitch_g == filled(f, sizeof(T));
         if (c.ordered) a.out[0] = grad_x;
-        else a.sums = (float *)ws;
+        else a.sums = sums;
         s = du ? run_product<T, kBackPair>(a, c.hs) : run_product<T, kBack>(a, c.hs);
         if (s == BT_OK && !c.ordered) {
             const bt_dtype dtype = std::is_same_v<T, float> ? BT_F32 : std::is_same_v<T, f16> ? BT_F16 : BT_BF16;
@@ -890,6 +1002,7 @@ bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch
     }
     if (s == BT_OK && grad_w_gate) {
         ExpertJob a = c.job();
+        a.parts = parts;
         a.p[0] = x;
         a.q[0] = dg;
         a.q[1] = du;
@@ -901,7 +1014,7 @@ bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch
         a.pitch = d;
         a.m = (uint32_t)f;
         a.n = (uint32_t)d;
-        a.parts = du ? 2 : 1;
+        a.outputs = du ? 2 : 1;
         s = run_product<T, kWeights>(a, c.hs);
     }
     return s;
@@ -925,7 +1038,8 @@ extern "C" {
 size_t bt_expert_gated_workspace_bytes(const bt_expert_plan *plan, uint64_t d, uint64_t f, bt_dtype dtype, int ordered, int backward) {
     if (check(plan, d, f, dtype) != BT_OK || plan->tokens == 0 || f == 0) return 0;
     const uint64_t rows = plan->tokens * plan->chosen, w = (uint64_t)width_of(dtype), copies = copies_bytes(*plan, d, f, 2, (int)w, ordered != 0, backward != 0);
-    return (size_t)(copies + (backward ? 2 * whole(rows * filled(f, (int)w) * w) + (ordered ? 0 : whole(4 * rows * d)) : 0));
+    if (!backward) return (size_t)(copies + forward_parts(*plan, d, f, true, (int)w));
+    return (size_t)(copies + 2 * whole(rows * filled(f, (int)w) * w) + (ordered ? 0 : whole(4 * rows * d)) + backward_parts(*plan, d, f, true, (int)w));
 }
 
 bt_status bt_expert_gated_forward(const void *d_x, const void *d_w_gate, const void *d_w_up, const bt_expert_plan *plan,
@@ -997,8 +1111,8 @@ bt_status bt_expert_gated_backward(const void *d_grad_h, const void *d_x, const 
 size_t bt_expert_linear_workspace_bytes(const bt_expert_plan *plan, uint64_t d_in, uint64_t d_out, bt_dtype dtype, int ordered, int backward) {
     if (check(plan, d_in, d_out, dtype) != BT_OK || plan->tokens == 0 || d_out == 0) return 0;
     const uint64_t rows = plan->tokens * plan->chosen, w = (uint64_t)width_of(dtype), copies = copies_bytes(*plan, d_in, d_out, 1, (int)w, ordered != 0, backward != 0);
-    if (!backward) return (size_t)copies;
-    return (size_t)(copies + (pads(*plan, d_out, (int)w) ? whole(rows * filled(d_out, (int)w) * w) : 0) + (ordered ? 0 : whole(4 * rows * d_in)));
+    if (!backward) return (size_t)(copies + forward_parts(*plan, d_in, d_out, false, (int)w));
+    return (size_t)(copies + backward_parts(*plan, d_in, d_out, false, (int)w) + (pads(*plan, d_out, (int)w) ? whole(rows * filled(d_out, (int)w) * w) : 0) + (ordered ? 0 : whole(4 * rows * d_in)));
 }
 
 bt_status bt_expert_linear_forward(const void *d_x, const void *d_w, const bt_expert_plan *plan, uint64_t d_in, uint64_t d_out, bt_dtype dtype, int ordered,
