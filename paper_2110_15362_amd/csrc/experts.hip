@@ -67,7 +67,7 @@ struct Taken {
 
 constexpr int kMostExperts = BT_MAX_EXPERTS;
 
-// The experts' tiles of `a_tile` rows, added up: those of expert e are numbered from starts[e] on; starts[experts + 1] is how many there are.
+// The experts' tiles of `a_tile` rows, added up: those of expert e are numbered from starts[e] on; starts[experts + 1] is how many there are.  For workgroups that take several tiles.
 struct Tiles {
     uint32_t starts[kMostExperts + 2];
 
@@ -76,15 +76,7 @@ struct Tiles {
         if (threadIdx.x < kWave) {
             uint32_t sum = 0;
             for (uint32_t e0 = 0; e0 <= a.experts; e0 += kWave) {
-                const uint32_t e = e0 + threadIdx.x;
-                uint32_t n = 0;
-                if (e <= a.experts) n = (rows_of(a, e) + a_tile - 1) / a_tile;
-                uint32_t x = n;
-#pragma unroll
-                for (int d = 1; d < kWave; d *= 2) {
-                    const uint32_t y = __shfl_up(x, d);
-                    if ((int)threadIdx.x >= d) x += y;
-                }
+                const uint32_t e = e0 + threadIdx.x, n = e <= a.experts ? (rows_of(a, e) + a_tile - 1) / a_tile : 0, x = before_and(n);
                 if (e <= a.experts) starts[e] = sum + x - n;
                 sum += __shfl(x, kWave - 1);
             }
@@ -92,16 +84,63 @@ struct Tiles {
         }
         __syncthreads();
     }
+    // (The sum of the lanes up to this one.)
+    __device__ static uint32_t before_and(uint32_t x) {
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const uint32_t y = __shfl_up(x, d);
+            if ((int)(threadIdx.x % kWave) >= d) x += y;
+        }
+        return x;
+    }
     __device__ uint32_t count(const ExpertJob &a) const { return __builtin_amdgcn_readfirstlane(starts[a.experts + 1]); }
-    // The expert that a tile belongs to.
-    __device__ uint32_t expert(const ExpertJob &a, const uint32_t tile) const {
+    // The group that a tile belongs to, and the tiles before and of it.
+    __device__ Group group(const ExpertJob &a, const uint32_t tile, uint32_t *start, uint32_t *tiles) const {
         uint32_t low = 0, high = a.experts + 1;      // starts[low] <= tile < starts[high]
         while (high - low > 1) {
             const uint32_t mid = (low + high) / 2;
             if ((uint32_t)__builtin_amdgcn_readfirstlane(starts[mid]) <= tile) low = mid;
             else high = mid;
         }
-        return __builtin_amdgcn_readfirstlane(low);
+        *start = __builtin_amdgcn_readfirstlane(starts[low]);
+        *tiles = __builtin_amdgcn_readfirstlane(starts[low + 1]) - *start;
+        return group_of(a, __builtin_amdgcn_readfirstlane(low));
+    }
+};
+
+// The same for workgroups of one tile: each wave for itself, without LDS and without a wait for the others, 64 experts at a time.
+struct TilesOnce {
+    uint32_t a_tile, sum;
+    // of the last 64 experts that were looked at, the lane's one: from where it begins, rows and tiles up to it and of it
+    uint32_t first, rows, upto, n;
+
+    __device__ uint32_t look(const ExpertJob &a, const uint32_t e0) {
+        const uint32_t e = e0 + threadIdx.x % kWave;
+        first = e <= a.experts ? bound(a, e) : 0;
+        const uint32_t end = e < a.experts ? bound(a, e + 1) : a.rows;
+        rows = e <= a.experts && end > first ? end - first : 0;
+        n = (rows + a_tile - 1) / a_tile;
+        upto = Tiles::before_and(n);
+        return __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    __device__ void find(const ExpertJob &a, const uint32_t tile_rows) {
+        a_tile = tile_rows;
+        sum = 0;
+        for (uint32_t e0 = 0; e0 <= a.experts; e0 += kWave) sum += look(a, e0);
+    }
+    __device__ uint32_t count(const ExpertJob &) const { return sum; }
+    __device__ Group group(const ExpertJob &a, const uint32_t tile, uint32_t *start, uint32_t *tiles) {
+        uint32_t before = 0;
+        for (uint32_t e0 = 0;; e0 += kWave) {
+            const uint32_t here = a.experts < kWave ? sum : look(a, e0);      // (of so few they have all been looked at)
+            if (tile < before + here) {
+                const int lane = __builtin_ctzll(__ballot(before + upto > tile));
+                *tiles = __builtin_amdgcn_readlane(n, lane);
+                *start = before + __builtin_amdgcn_readlane(upto, lane) - *tiles;
+                return {e0 + lane, (uint32_t)__builtin_amdgcn_readlane(first, lane), (uint32_t)__builtin_amdgcn_readlane(rows, lane)};
+            }
+            before += here;
+        }
     }
 };
 
@@ -131,12 +170,12 @@ struct Place {
 // Tiles that there are, and the tile of a number.  Workgroups go to the eight XCDs in turn, each of which has an L2 of its own.  Of the 256 tiles that run at once an XCD's are
 // neighbours, in bands of four rows of tiles of one expert, so that they share what they read; all XCDs are at the same expert, whose weights then come from memory once, and (the weights' gradients)
 // have sums of about the same length.  (256: one tile to a compute unit.)
-template <Kind K> __device__ inline uint32_t tiles_of(const ExpertJob &a, const Tiles &tiles) {
+template <Kind K, class Map> __device__ inline uint32_t tiles_of(const ExpertJob &a, const Map &tiles) {
     if constexpr (K == kWeights) return a.experts * a.outputs * a.tiles_m * a.tiles_n;
     else return tiles.count(a) * a.tiles_n;
 }
 
-template <Kind K> __device__ inline Place tile_of(const ExpertJob &a, const Tiles &tiles, uint32_t tile, const uint32_t tile_m, const uint32_t tile_n) {
+template <Kind K, class Map> __device__ inline Place tile_of(const ExpertJob &a, Map &tiles, uint32_t tile, const uint32_t tile_m, const uint32_t tile_n) {
     constexpr uint32_t kBand = 4;
     Place at;
     at.slot = ~0u;
@@ -149,11 +188,9 @@ template <Kind K> __device__ inline Place tile_of(const ExpertJob &a, const Tile
         tile -= at.part * a_part;
         rows = a.tiles_m;
     } else {
-        const uint32_t e = tiles.expert(a, tile / a.tiles_n);
-        at.of = group_of(a, e);
+        uint32_t start;
+        at.of = tiles.group(a, tile / a.tiles_n, &start, &rows);
         at.part = 0;
-        const uint32_t start = __builtin_amdgcn_readfirstlane(tiles.starts[e]);
-        rows = __builtin_amdgcn_readfirstlane(tiles.starts[e + 1]) - start;
         tile -= start * a.tiles_n;
     }
     const uint32_t band = tile / (kBand * a.tiles_n), left = rows - band * kBand, high = left < kBand ? left : kBand;
@@ -163,7 +200,7 @@ template <Kind K> __device__ inline Place tile_of(const ExpertJob &a, const Tile
     return at;
 }
 
-template <Kind K> __device__ inline Place place_of(const ExpertJob &a, const Tiles &tiles, const uint32_t number, const Round &r, const uint32_t tile_m, const uint32_t tile_n) {
+template <Kind K, class Map> __device__ inline Place place_of(const ExpertJob &a, Map &tiles, const uint32_t number, const Round &r, const uint32_t tile_m, const uint32_t tile_n) {
     constexpr uint32_t kXcds = 8, kTogether = 256;
     const uint32_t first = number / kTogether * kTogether, here = r.tiles - first < kTogether ? r.tiles - first : kTogether, xcd = number % kXcds, more = here % kXcds;
     const uint32_t item = first + xcd * (here / kXcds) + (xcd < more ? xcd : more) + number % kTogether / kXcds, slot = item - r.full;
@@ -264,7 +301,7 @@ template <class T, Kind K> __global__ __launch_bounds__(Small::THREADS, 2) void 
     typedef Ring<T, F::Q, Small::NQ, Small::FQ, Small::THREADS> RingQ;
     constexpr int kDeep = 4;
     __shared__ __align__(16) char tiles[2][W::P::BYTES + W::Q::BYTES];
-    __shared__ Tiles map;
+    TilesOnce map;
     if constexpr (K != kWeights) map.find(a, Small::NQ);
     const uint32_t total = tiles_of<K>(a, map), number = a.first + blockIdx.x;
     if (number >= total) return;
@@ -407,7 +444,14 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
     constexpr int kReadsP = S::FP * Reader<T, F::P, S::NP, S::FP>::READS, kReadsQ = S::FQ / 2 * Reader<T, F::Q, S::NQ, S::FQ>::READS;
     constexpr int kProducts = S::FP * S::FQ / 2 * (sizeof(T) == 4 ? 4 : 1);
     __shared__ __align__(1024) char tiles[PLACES * (PB + QB)];
-    __shared__ Tiles map;
+    constexpr bool kSeveral = S::THREADS == Large::THREADS;      // tiles to a workgroup
+    using Map = std::conditional_t<kSeveral && K != kWeights, Tiles, TilesOnce>;      // (the weights' gradients have all experts' tiles: nothing is looked up)
+    __shared__ std::conditional_t<std::is_same_v<Map, Tiles>, Tiles, char> shared_map;
+    TilesOnce own_map;
+    Map &map = [&]() -> Map & {
+        if constexpr (std::is_same_v<Map, Tiles>) return shared_map;
+        else return own_map;
+    }();
     if constexpr (K != kWeights) map.find(a, S::NQ);
     Round r;
     r.find(tiles_of<K>(a, map), kSlots<S>, a.most_splits);
@@ -453,8 +497,6 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
     Place at = place_of<K>(a, map, number, r, S::NQ, W::COLS);
     uint32_t count = begin(at);
     number += gridDim.x;
-    // (The smaller tiles' workgroups take one each; a launch has them all unless there are more than it holds.)
-    constexpr bool kSeveral = S::THREADS == Large::THREADS;
     bool stored = false;      // since the first tiles were asked for: by each lane, kStores of each output or more
     constexpr int kStores = kStoresAtLeast<T, K, S::FP, S::FQ>;
     for (;;) {
@@ -557,7 +599,7 @@ constexpr int kSlice = 2;
 
 template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS) void experts_join_kernel(const ExpertJob a) {
     constexpr int kCols = Work<T, FormOf<K>, S>::COLS, kSlices = S::FQ / kSlice;
-    __shared__ Tiles map;
+    TilesOnce map;
     if constexpr (K != kWeights) map.find(a, S::NQ);
     Round r;
     r.find(tiles_of<K>(a, map), kSlots<S>, a.most_splits);
@@ -593,15 +635,16 @@ template <class T> constexpr int kUnit = 128 / (int)sizeof(T);
 
 template <class T, Kind K, int FQ, bool ODD> __global__ __launch_bounds__(kTokenWaves * kWave) void experts_tokens_kernel(const ExpertJob a) {
     constexpr int N = K == kPair ? 2 : 1;      // weights
-    constexpr int kUnits = K == kPair ? 4 : FQ == 1 ? 8 : 4;      // on their way at once
+    constexpr int kUnits = 4;      // on their way at once (of one weight and 16 rows eight: 21.4 us where four take 18.9, 16 rows at 16 experts, 4096 to 1024 features in bf16)
     constexpr int kLane = sizeof(T) == 4 ? kPer<T> : 2 * kPer<T>, kNext = sizeof(T) == 4 ? 4 * kPer<T> : kPer<T>;      // from one lane's first vector to the next one's, to its second
     __shared__ float sums[kTokenWaves][N][FQ][kWave][4];
-    __shared__ Tiles map;
+    TilesOnce map;
     map.find(a, FQ * 16);
     const uint32_t tile = (a.first + blockIdx.x) / a.tiles_n, n = ((a.first + blockIdx.x) - tile * a.tiles_n) * 16;
     if (tile >= map.count(a)) return;
-    const uint32_t expert = map.expert(a, tile), m = (tile - __builtin_amdgcn_readfirstlane(map.starts[expert])) * (FQ * 16);
-    const Group g = group_of(a, expert);
+    uint32_t start, tiles;
+    const Group g = map.group(a, tile, &start, &tiles);
+    const uint32_t m = (tile - start) * (FQ * 16);
     const Taken rows = taken(a, g);
     const Operand oq = operand_q<T, K>(a, g, 0);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / 16, t = lane % 16;

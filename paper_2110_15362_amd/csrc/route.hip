@@ -249,12 +249,12 @@ __global__ __launch_bounds__(256) void count_kernel(const RouteJob a) {
     for (uint32_t e = threadIdx.x; e < a.experts; e += 256) a.counts[(uint64_t)blockIdx.x * a.experts + e] = (int32_t)count[e];
 }
 
-// Bound by the way to the counts of the groups, which every workgroup reads: threads that have no expert of their own take a part of the groups, eight at once (us, 16384 tokens, 8 of 128 experts: 64 one
+// Bound by the way to the counts of the groups, which every workgroup reads: threads that have no expert of their own take a part of the groups, 32 at once (us, 16384 tokens, 8 of 128 experts: 64 one
 // count after the other by 256 threads).
 constexpr int kOrderWaves = 8;
 
 __global__ __launch_bounds__(kOrderWaves * kWave) void order_kernel(const RouteJob a) {
-    constexpr uint32_t kThreads = kOrderWaves * kWave, kAtOnce = 8;
+    constexpr uint32_t kThreads = kOrderWaves * kWave, kAtOnce = 32;
     __shared__ uint32_t base[(kOrderWaves + 1) * kMostExperts], all[kMostExperts], rows_there;
     clear_counts<kThreads>(a, base);
     clear_counts<kThreads>(a, all);
