@@ -3,9 +3,11 @@
 
 Each sublayer is norm -> gated projections -> projection back -> norm, gate and residual sum; the norm behind one is joined with the norm before
 the next (residual_norm).  The gates are ReLUs, so what the gated projections keep for backward, and their output, are zero in the same
-places: with --stash a BitmapStash keeps all of it compressed.  The gradients are clipped to a common norm before each step.
+places: with --stash a BitmapStash keeps all of it compressed.  The gradients are clipped to a common norm before each step.  With --experts the
+projections are those of several experts, of which a router gives each token a few.
 
     python examples/feed_forward.py --layers 4 --features 1024 --hidden 4096 --rows 4096 --steps 10 --stash
+    python examples/feed_forward.py --layers 4 --features 1024 --hidden 1024 --experts 16 --chosen 2 --rows 4096 --steps 10 --stash
 """
 import argparse
 import contextlib
@@ -17,13 +19,14 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
-from paper_2110_15362_amd import autograd, block  # noqa: E402
+from paper_2110_15362_amd import autograd, block, experts  # noqa: E402
 
 
 class FeedForwardStack(torch.nn.Module):
-    """`layers` sublayers of `features`, `hidden` between their projections; one gate for each sequence, from its condition."""
+    """`layers` sublayers of `features`, `hidden` between their projections (of each of `count` experts, if there are any, of which a token uses `chosen`); one gate for each
+    sequence, from its condition."""
 
-    def __init__(self, layers, features, hidden, conditions, activation="relu", dtype=torch.bfloat16, device="cuda", seed=0):
+    def __init__(self, layers, features, hidden, conditions, activation="relu", dtype=torch.bfloat16, device="cuda", seed=0, count=0, chosen=2):
         super().__init__()
         g = torch.Generator().manual_seed(seed)
 
@@ -32,22 +35,32 @@ class FeedForwardStack(torch.nn.Module):
 
         def ones():
             return torch.nn.Parameter(torch.ones(features, device=device, dtype=dtype))
-        self.activation, self.scale = activation, 1.0 / math.sqrt(2.0 * layers)
+        self.activation, self.scale, self.chosen = activation, 1.0 / math.sqrt(2.0 * layers), chosen
+        each = (count,) if count else ()
         self.first_norm = ones()
-        self.w_gate = torch.nn.ParameterList([weight(hidden, features) for _ in range(layers)])
-        self.w_up = torch.nn.ParameterList([weight(hidden, features) for _ in range(layers)])
-        self.w_down = torch.nn.ParameterList([weight(features, hidden) for _ in range(layers)])
+        self.w_gate = torch.nn.ParameterList([weight(*each, hidden, features) for _ in range(layers)])
+        self.w_up = torch.nn.ParameterList([weight(*each, hidden, features) for _ in range(layers)])
+        self.w_down = torch.nn.ParameterList([weight(*each, features, hidden) for _ in range(layers)])
         self.post_norm = torch.nn.ParameterList([ones() for _ in range(layers)])
         self.pre_norm = torch.nn.ParameterList([ones() for _ in range(layers)])      # of the next sublayer; the last one's is the output norm
         self.w_condition = torch.nn.ParameterList([weight(features, conditions) for _ in range(layers)])
+        self.w_router = torch.nn.ParameterList([weight(count, features) for _ in range(layers)] if count else [])
+
+    def block(self, i, y):
+        """The block of sublayer i: y through the projections and back."""
+        if not len(self.w_router):
+            return torch.nn.functional.linear(block.gated_linear(y, self.w_gate[i], self.w_up[i], self.activation), self.w_down[i])
+        tokens = y.reshape(-1, y.shape[-1])
+        weights, plan = experts.route(torch.nn.functional.linear(tokens, self.w_router[i]), self.chosen)
+        h = experts.gated_linear(tokens, plan, self.w_gate[i], self.w_up[i], self.activation)
+        return experts.combine(experts.linear(h, plan, self.w_down[i]), plan, weights).view(y.shape)
 
     def forward(self, x, condition):
         """x [sequences, tokens, features], condition [sequences, conditions] -> normed output of the same shape as x."""
         y = block.rms_norm(x, self.first_norm)
         for i in range(len(self.w_gate)):
-            h = block.gated_linear(y, self.w_gate[i], self.w_up[i], self.activation)
             gate = torch.nn.functional.linear(condition, self.w_condition[i])
-            x, y = block.residual_norm(x, torch.nn.functional.linear(h, self.w_down[i]), self.post_norm[i], gate, self.pre_norm[i], scale=self.scale)
+            x, y = block.residual_norm(x, self.block(i, y), self.post_norm[i], gate, self.pre_norm[i], scale=self.scale)
         return y
 
 
@@ -70,6 +83,8 @@ def main(argv=None):
     ap.add_argument("--layers", type=int, default=4)
     ap.add_argument("--features", type=int, default=1024)
     ap.add_argument("--hidden", type=int, default=4096)
+    ap.add_argument("--experts", type=int, default=0, help="experts of a sublayer; 0: one that all tokens use, without a router")
+    ap.add_argument("--chosen", type=int, default=2, help="experts that a token uses")
     ap.add_argument("--rows", type=int, default=4096, help="tokens of a step, over 8 sequences")
     ap.add_argument("--steps", type=int, default=10)
     ap.add_argument("--rate", type=float, default=0.5)
@@ -82,7 +97,7 @@ def main(argv=None):
     sequences = 8
     x, target = (torch.randn(sequences, a.rows // sequences, a.features, generator=g, device="cuda").to(dtype) for _ in range(2))
     condition = torch.randn(sequences, 32, generator=g, device="cuda").to(dtype)
-    model = FeedForwardStack(a.layers, a.features, a.hidden, 32, dtype=dtype)
+    model = FeedForwardStack(a.layers, a.features, a.hidden, 32, dtype=dtype, count=a.experts, chosen=a.chosen)
     stash = autograd.BitmapStash() if a.stash else None
     torch.cuda.reset_peak_memory_stats()
     before, losses = torch.cuda.memory_allocated(), []

@@ -197,6 +197,10 @@ template <Kind K, class Map> __device__ inline Place tile_of(const ExpertJob &a,
     tile -= band * kBand * a.tiles_n;
     at.m = (band * kBand + tile % high) * tile_m;
     at.n = tile / high * tile_n;
+    if (K != kWeights && (at.m >= at.of.rows || at.n >= a.n)) {      // (offsets that do not ascend may add up to anything)
+        at.of = {a.experts, 0, 0};
+        at.m = at.n = 0;
+    }
     return at;
 }
 
@@ -628,51 +632,47 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS) voi
     finish<T, K, S::FP, kSlice>(a, acc, at.m + (wave % 2) * S::FQ * 16 + slice * kSlice * 16, at.n + (wave / 2) * (kCols / S::WP), at);
 }
 
-// Few rows an expert (tokens to answer with): as gated_tokens_kernel, for 16 columns and FQ times 16 rows of one expert.  The weights are read once for as many rows and bound
+// Few rows an expert (tokens to answer with): as gated_tokens_kernel, for 16 columns and 16 rows of one expert.  The weights are read once for as many rows and bound
 // the time.
 constexpr int kTokenWaves = 8;
 template <class T> constexpr int kUnit = 128 / (int)sizeof(T);
 
-template <class T, Kind K, int FQ, bool ODD> __global__ __launch_bounds__(kTokenWaves * kWave) void experts_tokens_kernel(const ExpertJob a) {
+template <class T, Kind K, bool ODD> __global__ __launch_bounds__(kTokenWaves * kWave) void experts_tokens_kernel(const ExpertJob a) {
     constexpr int N = K == kPair ? 2 : 1;      // weights
     constexpr int kUnits = 4;      // on their way at once (of one weight and 16 rows eight: 21.4 us where four take 18.9, 16 rows at 16 experts, 4096 to 1024 features in bf16)
     constexpr int kLane = sizeof(T) == 4 ? kPer<T> : 2 * kPer<T>, kNext = sizeof(T) == 4 ? 4 * kPer<T> : kPer<T>;      // from one lane's first vector to the next one's, to its second
-    __shared__ float sums[kTokenWaves][N][FQ][kWave][4];
+    __shared__ float sums[kTokenWaves][N][kWave][4];
     TilesOnce map;
-    map.find(a, FQ * 16);
+    map.find(a, 16);
     const uint32_t tile = (a.first + blockIdx.x) / a.tiles_n, n = ((a.first + blockIdx.x) - tile * a.tiles_n) * 16;
     if (tile >= map.count(a)) return;
     uint32_t start, tiles;
     const Group g = map.group(a, tile, &start, &tiles);
-    const uint32_t m = (tile - start) * (FQ * 16);
+    const uint32_t m = (tile - start) * 16;
+    if (m >= g.rows) return;
     const Taken rows = taken(a, g);
     const Operand oq = operand_q<T, K>(a, g, 0);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / 16, t = lane % 16;
-    const T *p[N], *q[FQ];
+    const T *p[N];
     // (Rows that are not there are others again: their results are not stored.)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const Operand op = operand_p<T, K>(a, g, i);
         p[i] = (const T *)op.p + (n + t < a.n ? n + t : a.n - 1) * op.pitch + group * kLane;
     }
-#pragma unroll
-    for (int j = 0; j < FQ; ++j) {
-        const uint32_t row = m + j * 16 + t < g.rows ? m + j * 16 + t : g.rows - 1;
-        q[j] = (const T *)oq.p + rows(row) * oq.pitch + group * kLane;
-    }
-    bool odd_p[N], odd_q[FQ];      // where a lane's vectors are read from the element before (`k` is even)
+    const T *const q = (const T *)oq.p + rows(m + t < g.rows ? m + t : g.rows - 1) * oq.pitch + group * kLane;
+    bool odd_p[N];      // where a lane's vectors are read from the element before (`k` is even)
 #pragma unroll
     for (int i = 0; i < N; ++i) odd_p[i] = ODD && ((uintptr_t)p[i] & 2) != 0;
-#pragma unroll
-    for (int j = 0; j < FQ; ++j) odd_q[j] = ODD && ((uintptr_t)q[j] & 2) != 0;
-    acc4 acc[N][FQ] = {};
+    const bool odd_q = ODD && ((uintptr_t)q & 2) != 0;
+    acc4 acc[N] = {};
     // The workgroups begin in different places of the summed index, or all would ask the same channels of the memory at a time.
     const uint32_t k_end = summed<K>(a, g), whole = k_end / kUnit<T>, shift = whole == 0 ? 0 : blockIdx.x * kTokenWaves % whole;
     uint32_t unit = wave;
     const auto take = [&](auto many) {
         constexpr int M = decltype(many)::value;
-        raw16 w[M][N][2], x[M][FQ][2];
-        uint32_t w_end[M][N], x_end[M][FQ];
+        raw16 w[M][N][2], x[M][2];
+        uint32_t w_end[M][N], x_end[M];
 #pragma unroll
         for (int s = 0; s < M; ++s) {
             uint32_t at = unit + s * kTokenWaves + shift;
@@ -682,14 +682,12 @@ template <class T, Kind K, int FQ, bool ODD> __global__ __launch_bounds__(kToken
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) w[s][i][h] = reinterpret_cast<const Unaligned<T> *>(p[i] + k + h * kNext - (odd_p[i] ? 1 : 0))->v;
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) x[s][j][h] = reinterpret_cast<const Unaligned<T> *>(q[j] + k + h * kNext - (odd_q[j] ? 1 : 0))->v;
+                x[s][h] = reinterpret_cast<const Unaligned<T> *>(q + k + h * kNext - (odd_q ? 1 : 0))->v;
             }
             if constexpr (ODD) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) w_end[s][i] = bits_at(p[i] + k + (2 * kPer<T> - 1));
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) x_end[s][j] = bits_at(q[j] + k + (2 * kPer<T> - 1));
+                x_end[s] = bits_at(q + k + (2 * kPer<T> - 1));
             }
         }
         __builtin_amdgcn_sched_barrier(0);      // (all of them before the first product)
@@ -702,15 +700,12 @@ template <class T, Kind K, int FQ, bool ODD> __global__ __launch_bounds__(kToken
             if constexpr (ODD) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) move(w[s][i], w_end[s][i], odd_p[i]);
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) move(x[s][j], x_end[s][j], odd_q[j]);
+                move(x[s], x_end[s], odd_q);
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-#pragma unroll
-                    for (int j = 0; j < FQ; ++j) acc[i][j] = multiply<T>(w[s][i][h], x[s][j][h], acc[i][j]);
+                for (int i = 0; i < N; ++i) acc[i] = multiply<T>(w[s][i][h], x[s][h], acc[i]);
         }
         unit += M * kTokenWaves;
     };
@@ -721,29 +716,24 @@ template <class T, Kind K, int FQ, bool ODD> __global__ __launch_bounds__(kToken
         const int left = (int)(k_end - k) - group * kLane;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            raw16 w[N], x[FQ];
+            raw16 w[N];
 #pragma unroll
             for (int i = 0; i < N; ++i) w[i] = load_vec(p[i] + k + h * kNext, left - h * kNext, (int)k_end - left + h * kNext);
+            const raw16 x = load_vec(q + k + h * kNext, left - h * kNext, (int)k_end - left + h * kNext);
 #pragma unroll
-            for (int j = 0; j < FQ; ++j) x[j] = load_vec(q[j] + k + h * kNext, left - h * kNext, (int)k_end - left + h * kNext);
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) acc[i][j] = multiply<T>(w[i], x[j], acc[i][j]);
+            for (int i = 0; i < N; ++i) acc[i] = multiply<T>(w[i], x, acc[i]);
         }
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int j = 0; j < FQ; ++j) *(acc4 *)sums[wave][i][j][lane] = acc[i][j];
+    for (int i = 0; i < N; ++i) *(acc4 *)sums[wave][i][lane] = acc[i];
     __syncthreads();
-    for (uint32_t c = threadIdx.x; c < FQ * 256; c += kTokenWaves * kWave) {
-        const uint32_t col = c % 16, token = c / 16, from = col / 4 * 16 + token % 16, r = col % 4, j = token / 16;
+    for (uint32_t c = threadIdx.x; c < 256; c += kTokenWaves * kWave) {
+        const uint32_t col = c % 16, token = c / 16, from = col / 4 * 16 + token, r = col % 4;
         float s[2] = {};
 #pragma unroll
         for (int w = 0; w < kTokenWaves; ++w)
 #pragma unroll
-            for (int i = 0; i < N; ++i) s[i] += sums[w][i][j][from][r];
+            for (int i = 0; i < N; ++i) s[i] += sums[w][i][from][r];
         if (m + token >= g.rows || n + col >= a.n) continue;
         const uint64_t at = (uint64_t)(g.first + m + token) * a.pitch + n + col;
         if constexpr (K == kPair) {
@@ -804,8 +794,12 @@ uint64_t each(const bt_expert_plan &p) { return p.tokens * p.chosen / p.experts;
 // Rows of an expert from which on operands whose rows do not begin on 16-byte boundaries are copied to ones that do, as with the dense projections.
 constexpr uint64_t kPadEach = 128;
 
-// Rows of an expert up to which the forward pass reads the weights straight to registers.
-constexpr uint64_t kTokensEach = 16;
+// Whether the forward pass reads the weights straight to registers: with long sums few rows an expert, with short ones so few tiles that each has a compute unit (us, bf16, that way and in tiles: one product, 16 experts of
+// [1024, 4096], 64 rows 30 and 36, 256 rows 37 and 37; 64 experts of [2048, 768], 64 rows 50 and 33; both projections, 8 experts of [11008, 4096], 16 rows 209 and 229, 32 rows 241 and 241).
+bool few_rows(const bool pair, const uint64_t rows, const uint64_t experts, const uint64_t n, const uint64_t k, const int width) {
+    if (k * width >= 8192) return rows <= experts * (pair ? 2 : 8);
+    return (rows < experts ? rows : experts) * ceil_div(n, pair ? 32 : 64) <= 256;
+}
 
 bool pads(const bt_expert_plan &p, const uint64_t cols, const int width) { return ragged(cols, width) && each(p) >= kPadEach; }
 
@@ -897,14 +891,12 @@ template <class T, Kind K> bt_status run_product(ExpertJob &a, hipStream_t hs) {
         if (s != BT_OK || parts.most == 1) return s;
         return launch(join, dim3(kSlots<S> / 2 * (S::FQ / kSlice)), S::THREADS, hs, a);
     };
-    const uint64_t each_has = a.rows / a.experts;
     if constexpr (K <= kPlain) {
-        if (each_has <= kTokensEach) {
-            const auto tokens = [&](auto kernel, const uint32_t rows) { return go(kernel, rows, 16, kTokenWaves * kWave); };
+        if (few_rows(K == kPair, a.rows, a.experts, a.n, a.k, sizeof(T))) {
+            const auto tokens = [&](auto kernel) { return go(kernel, 16, 16, kTokenWaves * kWave); };
             if constexpr (sizeof(T) == 2)
-                if (a.pitch_p % 2 != 0 && !misaligned(a.p[0], 4) && !misaligned(a.p[1], 4) && !misaligned(a.q[0], 4))
-                    return each_has <= 4 ? tokens(experts_tokens_kernel<T, K, 1, true>, 16) : tokens(experts_tokens_kernel<T, K, 2, true>, 32);
-            return each_has <= 4 ? tokens(experts_tokens_kernel<T, K, 1, false>, 16) : tokens(experts_tokens_kernel<T, K, 2, false>, 32);
+                if (a.pitch_p % 2 != 0 && !misaligned(a.p[0], 4) && !misaligned(a.p[1], 4) && !misaligned(a.q[0], 4)) return tokens(experts_tokens_kernel<T, K, true>);
+            return tokens(experts_tokens_kernel<T, K, false>);
         }
     }
     bool straight = direct<T>(a.p[0], a.pitch_p) && direct<T>(a.q[0], a.pitch_q);
@@ -973,7 +965,7 @@ template <class... P> bool any_misaligned(const size_t a, P... p) { return (misa
 // Bytes of the sums of parts of tiles, of the forward pass and of the larger of both backward products.
 uint64_t parts_bytes(const bt_expert_plan &p, const Kind kind, const uint64_t m, const uint64_t n, const uint64_t k, const uint64_t outputs, const int width) {
     const uint64_t rows = p.tokens * p.chosen;
-    if (kind <= kPlain && each(p) <= kTokensEach) return 0;
+    if (kind <= kPlain && few_rows(kind == kPair, rows, p.experts, n, k, width)) return 0;
     return whole(parts_of(kind, size_of(kind, rows, p.experts, m, n, k, outputs, width), rows, p.experts, m, n, k, outputs, width).bytes);
 }
 uint64_t forward_parts(const bt_expert_plan &p, const uint64_t d, const uint64_t f, const bool pair, const int width) {

@@ -289,3 +289,254 @@ def test_larger_tiles(experts, dtype, size, ordered):
     assert all(torch.equal(a, b) for a, b in zip(grads, _gated_backward(experts, c, "silu", *kept[1:])))
     _check_linear_forward(c, _linear_forward(experts, c))
     _check_linear_backward(c, *_linear_backward(experts, c))
+
+
+# ---- which kernel
+
+@pytest.mark.parametrize("dtype,size", [("bf16", (4, 16, 2, 4104, 72)), ("f16", (40, 8, 2, 4101, 50)), ("f32", (30, 6, 2, 2050, 40)), ("bf16", (2, 64, 8, 33, 4100)), ("bf16", (24, 4, 1, 4096, 300))], ids=str)
+def test_few_rows(experts, dtype, size):
+    """Weights straight to registers, an expert's rows in several sixteens; rows of an odd number of 16-bit elements."""
+    for how in ("some", "one", "holes"):
+        for offset in (0, 1, 2):
+            c = Case(experts, size, DTYPES[dtype], 30 + offset, how=how)
+            _check_gated_forward(c, "silu", *_gated_forward(experts, c, "silu", offset=offset))
+            _check_linear_forward(c, _linear_forward(experts, c, offset))
+
+
+@pytest.mark.parametrize("ordered", [False, True])
+@pytest.mark.parametrize("dtype,size", [("bf16", (300, 2, 1, 4096, 264)), ("f16", (260, 3, 2, 2056, 200)), ("f32", (200, 2, 2, 1024, 136)), ("bf16", (700, 2, 2, 1032, 4104)), ("bf16", (4200, 2, 1, 2048, 520))], ids=str)
+def test_tiles_in_parts(experts, dtype, size, ordered):
+    """Long sums and few tiles, or few beyond whole rounds of them: parts of a tile's sum, joined."""
+    c = Case(experts, size, DTYPES[dtype], 31, how="holes", ordered=ordered)
+    kept = _gated_forward(experts, c, "gelu_tanh")
+    _check_gated_forward(c, "gelu_tanh", *kept)
+    grads = _gated_backward(experts, c, "gelu_tanh", *kept[1:])
+    _check_gated_backward(c, "gelu_tanh", *kept[1:], grads)
+    _check_linear_forward(c, _linear_forward(experts, c))
+    both = _linear_backward(experts, c)
+    _check_linear_backward(c, *both)
+    for a, b in zip(grads + both, _gated_backward(experts, c, "gelu_tanh", *kept[1:]) + _linear_backward(experts, c)):
+        assert torch.equal(a, b)
+
+
+def test_infinities_and_nans_stay_in_their_rows(experts):
+    """Rows of no expert that hold NaNs are not read, and what one row or one expert holds does not reach another's results."""
+    t = torch.bfloat16
+    for size in ((9, 5, 2, 72, 40), (300, 6, 2, 264, 200), (700, 4, 2, 520, 264)):
+        c = Case(experts, size, t, 32, how="holes", ordered=True)
+        e, first, end = max(c.groups, key=lambda g: g[2] - g[1])
+        clean = _gated_forward(experts, c, "silu") + (_linear_forward(experts, c),)
+        grads = _gated_backward(experts, c, "silu", *clean[1:3]) + _linear_backward(experts, c)
+        c.x[first] = float("nan")
+        c.x[end - 1] = float("inf")
+        c.grad[first] = float("inf")
+        other = torch.ones(c.rows, dtype=torch.bool)
+        other[[first, end - 1]] = False
+        got = _gated_forward(experts, c, "silu") + (_linear_forward(experts, c),)
+        for a, b in zip(clean, got):
+            assert torch.equal(a[other], b[other]) and not bool(torch.isfinite(b[first].float()).all())
+        rest = torch.arange(c.n) != e
+        got = _gated_backward(experts, c, "silu", *clean[1:3]) + _linear_backward(experts, c)
+        for a, b, of_x in zip(grads, got, (True, False, False, True, False)):
+            assert torch.equal(a[other], b[other]) if of_x else torch.equal(a[rest], b[rest])
+
+
+def test_tables_that_reach_beyond_are_cut(experts):
+    """Offsets and tokens outside of their ranges: results without meaning, inside of their tensors."""
+    c = Case(experts, (40, 4, 2, 72, 40), torch.bfloat16, 33)
+    for name, value in (("offsets", 1 << 30), ("offsets", -5), ("source", 1 << 30), ("source", -7), ("slots", 1 << 30), ("slots", -9)):
+        plan, _, _ = plan_on_device(experts, choices(40, 4, 2, 34), 4)
+        table = getattr(plan, name)
+        table.view(-1)[1::2] = value
+        c.plan = plan
+        _, gate, up = _gated_forward(experts, c, "silu")
+        _linear_forward(experts, c)
+        gate, up = torch.zeros_like(gate), torch.zeros_like(up)
+        _gated_backward(experts, c, "silu", gate, up)
+        _linear_backward(experts, c)
+        out = torch.empty(40, 40, dtype=torch.bfloat16, device="cuda")
+        m = Guarded()
+        y = m.put(c.grad)
+        weights, grad_y, grad_w = torch.rand(40, 2, device="cuda"), m.out(c.grad.shape, torch.bfloat16), m.out((40, 2), torch.float32)
+        experts.bt_combine_forward(y, plan, weights, out)
+        experts.bt_combine_backward(out, y, plan, weights, grad_y, grad_w)
+        torch.cuda.synchronize()
+        m.check()
+
+
+# ---- with autograd
+
+def _sublayer(experts, x, w_router, wg, wu, wd, chosen, activation="silu", normalise=True):
+    weights, plan = experts.route(x @ w_router.t(), chosen, normalise)
+    return experts.combine(experts.linear(experts.gated_linear(x, plan, wg, wu, activation), plan, wd), plan, weights), plan
+
+
+def _reference(x, w_router, wg, wu, wd, index, activation="silu", normalise=True):
+    """The sublayer with given choices, in 64 bits, one expert after the other."""
+    logits = x @ w_router.t()
+    p = torch.softmax(torch.gather(logits, 1, index) if normalise else logits, dim=1)
+    weights = p if normalise else torch.gather(p, 1, index)
+    out = torch.zeros_like(x)
+    for e in range(len(wg)):
+        token, j = torch.nonzero(index == e, as_tuple=True)
+        h = _act(activation, x[token] @ wg[e].t())[0] * (x[token] @ wu[e].t())
+        out = out.index_add(0, token, (h @ wd[e].t()) * weights[token, j, None])
+    return out
+
+
+def _sublayer_inputs(tokens, n, d, f, seed):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(tokens, d, generator=g), torch.randn(n, d, generator=g) / d ** 0.5, torch.randn(n, f, d, generator=g) / d ** 0.5, torch.randn(n, f, d, generator=g) / d ** 0.5,
+            torch.randn(n, d, f, generator=g) / f ** 0.5), torch.randn(tokens, d, generator=g)
+
+
+@pytest.mark.parametrize("normalise", [True, False])
+@pytest.mark.parametrize("activation", ["relu", "silu", "gelu_tanh"])
+def test_a_sublayer_and_its_gradients(experts, activation, normalise):
+    """Choice, gated projections, product back and sum together, in single precision: the output and every gradient within 1e-4 of its norm of the definition's by differentiation in 64 bits (a few
+    thousand 32-bit operations lie between), and along a direction the difference of the definition's values."""
+    inputs, v = _sublayer_inputs(90, 7, 72, 40, 40)
+    dev = [t.cuda().requires_grad_() for t in inputs]
+    out, plan = _sublayer(experts, *dev, 3, activation, normalise)
+    out.backward(v.cuda())
+    ref = [t.double().requires_grad_() for t in inputs]
+    index = plan.index.cpu().long()
+    want = _reference(*ref, index, activation, normalise)
+    want.backward(v.double())
+    assert float((out.detach().cpu().double() - want.detach()).norm()) <= 1e-4 * float(want.detach().norm())
+    gen = torch.Generator().manual_seed(41)
+    for i, (got, r) in enumerate(zip(dev, ref)):
+        assert float((got.grad.cpu().double() - r.grad).norm()) <= 1e-4 * float(r.grad.norm()), i
+        if activation == "relu":
+            continue                                         # (whose gradient jumps)
+        way = torch.randn(r.shape, generator=gen, dtype=torch.float64) / r.numel() ** 0.5
+
+        def value(step):
+            a = [t.double() for t in inputs]
+            a[i] = a[i] + step * way
+            return float((_reference(*a, index, activation, normalise) * v.double()).sum())
+        slope = (value(1e-4) - value(-1e-4)) / 2e-4
+        size = float((got.grad.cpu().double() * way).abs().sum())
+        assert abs(float((got.grad.cpu().double() * way).sum()) - slope) <= 1e-5 * size + 1e-6 * max(1.0, abs(slope)), i
+
+
+def test_strides_streams_and_frozen_weights(experts):
+    """Transposed and expanded inputs and gradients, another stream, weights and inputs that need no gradient, no_grad."""
+    inputs, v = _sublayer_inputs(60, 4, 48, 64, 42)
+    x = inputs[0].t().contiguous().cuda().t().requires_grad_()
+    wg = inputs[2].transpose(1, 2).contiguous().cuda().transpose(1, 2).requires_grad_()
+    rest = [t.cuda().requires_grad_() for t in (inputs[1], inputs[3], inputs[4])]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out, plan = _sublayer(experts, x, rest[0], wg, rest[1], rest[2], 2)
+        out.sum().backward()                                 # (a gradient of strides 0)
+    torch.cuda.current_stream().wait_stream(side)
+    ref = [t.double().requires_grad_() for t in inputs]
+    _reference(*ref, plan.index.cpu().long()).sum().backward()
+    for got, r in zip((x, rest[0], wg, rest[1], rest[2]), ref):
+        assert float((got.grad.cpu().double() - r.grad).norm()) <= 1e-4 * float(r.grad.norm())
+    frozen = [t.detach() for t in (rest[0], wg, rest[1], rest[2])]
+    out, _ = _sublayer(experts, x, *frozen, 2)
+    grad_x, = torch.autograd.grad(out.sum(), x)
+    assert float((grad_x.cpu().double() - ref[0].grad).norm()) <= 1e-4 * float(ref[0].grad.norm())
+    out, _ = _sublayer(experts, x.detach(), frozen[0], wg, *frozen[2:], 2)
+    grad_w, = torch.autograd.grad(out.sum(), wg)
+    assert torch.equal(grad_w, wg.grad)
+    h = experts.linear(x, plan, wg, ordered=False)
+    y = torch.cat([x.detach()[plan.source[a:b].long()] @ wg.detach()[e].t() for e, (a, b) in enumerate(zip(plan.offsets.tolist(), plan.offsets.tolist()[1:]))])
+    assert torch.allclose(h, y, rtol=1e-4, atol=1e-4)
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            assert _sublayer(experts, x, rest[0], wg, rest[1], rest[2], 2)[0].grad_fn is None
+
+
+def test_padding_tokens(experts):
+    """Tokens whose logits are all -infinity have no expert: outputs of zero and no gradient, and the others' results are those without them."""
+    inputs, v = _sublayer_inputs(50, 5, 40, 24, 43)
+    x, wr, wg, wu, wd = (t.cuda() for t in inputs)
+    real = torch.arange(50) % 10 < 7
+    logits = (x @ wr.t()).masked_fill(~real.cuda()[:, None], float("-inf")).requires_grad_()
+    x.requires_grad_()
+    weights, plan = experts.route(logits, 2)
+    out = experts.combine(experts.linear(experts.gated_linear(x, plan, wg, wu, "silu"), plan, wd), plan, weights)
+    out.backward(v.cuda())
+    for t in (out.detach(), x.grad, logits.grad, weights.detach()):
+        assert not bool(t[~real.cuda()].any()) and bool(torch.isfinite(t).all())
+    alone, plan2 = _sublayer(experts, x.detach()[real.cuda()], wr, wg, wu, wd, 2)
+    assert torch.equal(alone, out.detach()[real.cuda()]) and plan2.rows == 70 and int(plan.offsets[-1]) == 70
+
+
+def test_a_stash_keeps_what_relu_gates_save_compressed(experts):
+    from paper_2110_15362_amd import autograd as ag
+    inputs, v = _sublayer_inputs(512, 4, 128, 512, 44)
+    dev = [t.cuda().requires_grad_() for t in inputs]
+
+    def step():
+        grads = torch.autograd.grad(_sublayer(experts, *dev, 2, "relu")[0].square().mean(), dev)
+        return [g.clone() for g in grads]
+    plain = step()
+    stash = ag.BitmapStash(min_numel=4096)
+    with stash:
+        out = _sublayer(experts, *dev, 2, "relu")[0].square().mean()
+    kept = torch.autograd.grad(out, dev)
+    assert all(torch.equal(a, b) for a, b in zip(plain, kept))
+    assert stash.stats["compressed"] >= 3 and stash.stats["stored_bytes"] < 0.9 * stash.stats["dense_bytes"]
+
+
+def test_graph_replays(experts):
+    """The calls of a sublayer and of its gradients recorded into a graph, replayed on other tokens, that go to other experts, with other work between the replays."""
+    t, (tokens, n, chosen, d, f) = torch.bfloat16, (96, 5, 2, 264, 200)
+    inputs, v = _sublayer_inputs(tokens, n, d, f, 45)
+    x, wr, wg, wu, wd = (s.cuda().to(t) for s in inputs)
+    go = v.cuda().to(t)
+    plan = experts.new_plan(tokens, n, chosen)
+    empty = lambda *s, dtype=t: torch.empty(s, dtype=dtype, device="cuda")  # noqa: E731
+    logits, weights, grad_weights, grad_logits = empty(tokens, n), empty(tokens, chosen, dtype=torch.float32), empty(tokens, chosen, dtype=torch.float32), empty(tokens, n)
+    h, gate, up, grad_h = (empty(plan.rows, f) for _ in range(4))
+    y, grad_y, out, grad_x = empty(plan.rows, d), empty(plan.rows, d), empty(tokens, d), empty(tokens, d)
+    grads = torch.empty_like(wg), torch.empty_like(wu), torch.empty_like(wd)
+    ws = [experts.new_route_workspace(tokens, n, chosen), experts.new_gated_workspace(plan, d, f, t, backward=True), experts.new_linear_workspace(plan, f, d, t, backward=True)]
+
+    def calls():
+        torch.mm(x, wr.t(), out=logits)
+        experts.bt_route_forward(logits, plan, weights, ws[0])
+        experts.bt_expert_gated_forward(x, plan, wg, wu, "silu", h, gate, up, ws[1])
+        experts.bt_expert_linear_forward(h, plan, wd, y, ws[2])
+        experts.bt_combine_forward(y, plan, weights, out)
+        experts.bt_combine_backward(go, y, plan, weights, grad_y, grad_weights)
+        experts.bt_expert_linear_backward(grad_y, h, plan, wd, grad_h, grads[2], ws[2])
+        experts.bt_expert_gated_backward(grad_h, x, plan, wg, wu, gate, up, "silu", grad_x, grads[0], grads[1], ws[1])
+        experts.bt_route_backward(grad_weights, logits, plan, weights, grad_logits)
+    results = (weights, plan.index, plan.slots, plan.source, plan.offsets, h, y, out, grad_y, grad_weights, grad_h, grad_x, grad_logits) + grads
+    calls()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for i in range(4):
+        x.copy_(torch.randn(tokens, d, generator=torch.Generator().manual_seed(i)))
+        graph.replay()
+        got = [s.clone() for s in results]
+        torch.cuda.synchronize()
+        calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, results)), i
+
+
+def test_two_streams_with_workspaces_of_their_own(experts):
+    """Calls on two streams at once, each with its workspace, have the results of calls one after the other."""
+    cases = [Case(experts, (700, 4, 2, 520, 264), torch.bfloat16, 50 + i) for i in range(2)]
+    put = [[t.cuda() for t in (c.x, c.wg, c.wu)] for c in cases]
+    outs = [[torch.empty(c.rows, c.f, dtype=c.dtype, device="cuda") for _ in range(2)] for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for i, c in enumerate(cases):
+        experts.bt_expert_gated_forward(put[i][0], c.plan, *put[i][1:], "silu", outs[i][0], None, None, experts.new_gated_workspace(c.plan, c.d, c.f, c.dtype))
+    torch.cuda.synchronize()
+    spaces = [experts.new_gated_workspace(c.plan, c.d, c.f, c.dtype) for c in cases]
+    for _ in range(5):
+        for i, c in enumerate(cases):
+            experts.bt_expert_gated_forward(put[i][0], c.plan, *put[i][1:], "silu", outs[i][1], None, None, spaces[i], stream=streams[i])
+    torch.cuda.synchronize()
+    for a, b in outs:
+        assert torch.equal(a, b)
