@@ -798,7 +798,7 @@ constexpr uint64_t kPadEach = 128;
 // [1024, 4096], 64 rows 30 and 36, 256 rows 37 and 37; 64 experts of [2048, 768], 64 rows 50 and 33; both projections, 8 experts of [11008, 4096], 16 rows 209 and 229, 32 rows 241 and 241).
 bool few_rows(const bool pair, const uint64_t rows, const uint64_t experts, const uint64_t n, const uint64_t k, const int width) {
     if (k * width >= 8192) return rows <= experts * (pair ? 2 : 8);
-    return (rows < experts ? rows : experts) * ceil_div(n, pair ? 32 : 64) <= 256;
+    return rows <= experts * 8 && (rows < experts ? rows : experts) * ceil_div(n, pair ? 32 : 64) <= 256;
 }
 
 bool pads(const bt_expert_plan &p, const uint64_t cols, const int width) { return ragged(cols, width) && each(p) >= kPadEach; }
