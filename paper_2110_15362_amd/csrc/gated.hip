@@ -195,10 +195,9 @@ template <class T, Product K> __global__ __launch_bounds__(Small::THREADS, 2) vo
     end<T, K, Small>(a, acc, at);
 }
 
-// Bound by the matrix units (and, in the largest forward passes, by the power that they take: they are busy for 59 to 62 % of the cycles at 1.9 GHz), in 16 bits grad_x and
-// the weights' gradients by them and the full wait in every step (61 and 66 %).  bf16, tiles of 256 by 256: forward of [16384, 1024] x 4096 232 us, 1185 TFLOP/s, of
-// [16384, 2048] x 8192 with gate and up kept 977 us, 1125; grad_x of the latter 892 us, 1233, its weights' gradients 825 us, 1333 (on a
-// slower card 241, 1061, 948 and 886); instructions for 32 by 32 results, which read half as many registers, 4 % slower;
+// Bound by the matrix units, by the power that they take (the clock falls to 1.9 GHz) and, the forward pass most, by the wait for the next tile.  bf16, tiles of 256 by 256: forward of [16384, 1024] x
+// 4096 232 us, 1185 TFLOP/s, of [16384, 2048] x 8192 with gate and up kept 977 us, 1125 (on a slower card 241 and 1061); grad_x of the latter 763 us, 1441, its weights' gradients 715 us, 1538 (with a wait for all
+// fetches in every step, see `transposed`, 859 and 804); instructions for 32 by 32 results, which read half as many registers, 4 % slower;
 // four waves of 128 by 128, 667; 256 by 128, two workgroups a compute unit, 8 % slower.  Single precision, tiles of 64 by 64: [1024, 2048] x 8192 537 to 554
 // us each, 124 to 128 TFLOP/s.  Smaller sizes take smaller tiles, and parts of the sum each, so that there is work for all compute units: see plan_of.
 template <class T, Product K, class S> __global__ __launch_bounds__(S::THREADS, S::FQ == 8 ? 2 : 1) void gated_kernel(const GatedJob a) {

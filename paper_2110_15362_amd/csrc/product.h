@@ -65,6 +65,8 @@ template <class T, Order O, int N, int KB = kKBytes> struct Tile {      // N row
     }
 };
 
+// The transposing read.  __restrict, which says that no fetch writes what is read while it is: without it the compiler takes the read for one of what any fetch on its way may write, and waits for all of them in every
+// step.  That the tile has landed is for the waits in the kernels to see to, which count fetches.
 __device__ __attribute__((always_inline)) inline short4v transposed(BT_LDS short4v *__restrict from) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(from); }
 
 // A wave's fragments of a tile: F times 16 rows or columns from `first` on.  Where a lane reads depends on the fragment and the tile by constants
@@ -535,11 +537,6 @@ template <int LEFT> __device__ inline void wait_for_tiles() {
 // the L2 where that has other things to hold in between.  The forward pass in tiles of 64, whose weights nothing else reads, asks for two tiles at a time,
 // in every second one, piece by piece, and has five places (f16 forward of [37, 4096] x 11003: 50 -> 46 us); larger tiles ask for one in each and have
 // four: with two the bf16 forward pass of [16384, 2048] x 8192 took the same time, and grad_x has no registers for it.
-//
-// That holds for the forward pass and for single precision.  In 16 bits grad_x and the weights' gradients read fragments of the operands that lie across by the
-// transposing reads, which the compiler takes for reads of what any fetch may write: it waits for all of a wave's fetches behind the barrier of each step, those that
-// were asked for half a step ago too, and at a tile's start for the stores of the one before.  The waits below have to be right without that one: it says nothing of other
-// waves' fetches.
 template <int KIND, int COUNT, int PRODUCTS, int GROUPS, int G = 0> __device__ inline void spread_kind() {
     if constexpr (G < GROUPS) {
         constexpr int c = COUNT * (G + 1) / GROUPS - COUNT * G / GROUPS, m = PRODUCTS * (G + 1) / GROUPS - PRODUCTS * G / GROUPS;
