@@ -70,6 +70,8 @@ class Plan:
                 raise TypeError("%s must hold 32-bit integers (torch.int32), not %s" % (name, t.dtype))
             if not t.is_contiguous():
                 raise ValueError("%s must be contiguous" % name)
+            if t.device != index.device:
+                raise ValueError("all tables must live on one device")
         if index.dim() != 2 or slots.shape != index.shape or source.shape != (index.numel(),) or offsets.dim() != 1:
             raise ValueError("index and slots must be [tokens, chosen], source [tokens * chosen], offsets [experts + 1]")
         self.index, self.slots, self.source, self.offsets = index, slots, source, offsets

@@ -540,3 +540,69 @@ def test_two_streams_with_workspaces_of_their_own(experts):
     torch.cuda.synchronize()
     for a, b in outs:
         assert torch.equal(a, b)
+
+
+def test_no_tokens(experts):
+    """A batch without tokens goes through a whole sublayer and back: empty outputs, zeros for the weights' gradients."""
+    inputs, _ = _sublayer_inputs(3, 4, 24, 16, 60)
+    dev = [inputs[0][:0].cuda().requires_grad_()] + [t.cuda().requires_grad_() for t in inputs[1:]]
+    out, plan = _sublayer(experts, *dev, 2)
+    assert out.shape == (0, 24) and plan.rows == 0 and plan.offsets.tolist() == [0] * 5
+    out.sum().backward()
+    assert dev[0].grad.shape == (0, 24) and not any(bool(t.grad.any()) for t in dev[1:])
+    assert experts.plan_of(torch.empty(0, 2, dtype=torch.int64, device="cuda"), 4).offsets.tolist() == [0] * 5
+
+
+@pytest.mark.parametrize("dtype,tokens,chosen,d,f", [("bf16", 70001, 2, 64, 16400), ("f32", 40000, 2, 33, 27000)], ids=str)
+def test_outputs_beyond_2_to_the_31_elements(experts, dtype, tokens, chosen, d, f):
+    """Element offsets that pass 32 bits, in forward outputs, factors and gradients, aligned and through the kernel for any alignment; rows of every expert looked at."""
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("needs 120 GiB")
+    t, n = DTYPES[dtype], 3
+    g = torch.Generator(device="cuda").manual_seed(61)
+    x = torch.randn(tokens, d, generator=g, device="cuda").to(t)
+    w = (torch.randn(n, f, d, generator=g, device="cuda") / d ** 0.5).to(t)
+    index = torch.stack([torch.arange(tokens) % n, (torch.arange(tokens) + 1) % n], dim=1).int().cuda()
+    plan = experts.plan_of(index, n)
+    assert plan.rows * f > 1 << 31
+    y = torch.full((plan.rows, f), float("nan"), dtype=t, device="cuda")
+    ws = experts.new_linear_workspace(plan, d, f, t, ordered=False, backward=True)
+    experts.bt_expert_linear_forward(x, plan, w, y, ws, ordered=False)
+    o = plan.offsets.tolist()
+    for e in range(n):
+        for row in (o[e], (o[e] + o[e + 1]) // 2, o[e + 1] - 1):
+            v, m = x[plan.source[row]].double(), w[e].double()
+            within(y[row], (m @ v).cpu(), rounded((m @ v).cpu(), t, (d + 1) * SUM * (m.abs() @ v.abs()).cpu()), "row %d" % row)
+    grad_x, grad_w = torch.empty_like(x), torch.empty_like(w)
+    experts.bt_expert_linear_backward(y, x, plan, w, grad_x, grad_w, ws, ordered=False)
+    for token in (0, tokens // 2, tokens - 1):
+        want, off = torch.zeros(d, dtype=torch.float64), torch.zeros(d, dtype=torch.float64)
+        for j in range(chosen):
+            e, gy = int(index[token, j]), y[plan.slots[token, j]].double()
+            want += (gy @ w[e].double()).cpu()
+            off += (f + 3) * SUM * (gy.abs() @ w[e].double().abs()).cpu()
+        within(grad_x[token], want, rounded(want, t, off), "grad_x of token %d" % token)
+    for e in range(n):
+        gy, v = y[o[e]:o[e + 1], f - 8:].double(), x[plan.source[o[e]:o[e + 1]].long()].double()
+        within(grad_w[e, f - 8:], (gy.t() @ v).cpu(), rounded((gy.t() @ v).cpu(), t, (len(v) + 1) * SUM * (gy.abs().t() @ v.abs()).cpu()), "grad_w of expert %d" % e)
+
+
+def test_gathered_tokens_beyond_2_gib(experts):
+    """x of more bytes than a descriptor's offsets reach: gathered by 64-bit addresses."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GiB")
+    t, tokens, d, f, n = torch.bfloat16, 600000, 2048, 64, 4
+    g = torch.Generator(device="cuda").manual_seed(62)
+    x = torch.randn(tokens, d, generator=g, device="cuda", dtype=t)
+    w = (torch.randn(n, f, d, generator=g, device="cuda") / d ** 0.5).to(t)
+    index = (torch.arange(tokens, device="cuda") * 7 % 5 - 1).int()[:, None]          # (one in five has none)
+    plan = experts.plan_of(index, n)
+    y = experts.linear(x, plan, w, ordered=False)
+    o = plan.offsets.tolist()
+    assert o[n] == tokens * 4 // 5 and not bool(y[o[n]:].any())
+    for e in range(n):
+        at = plan.source[o[e]:o[e + 1]].long()
+        assert bool((index[at, 0] == e).all())
+        for part in (slice(0, 100), slice(-100, None)):
+            v, m = x[at[part]].double(), w[e].double()
+            within(y[o[e]:o[e + 1]][part], (v @ m.t()).cpu(), rounded((v @ m.t()).cpu(), t, (d + 1) * SUM * (v.abs() @ m.abs().t()).cpu()), "expert %d" % e)
