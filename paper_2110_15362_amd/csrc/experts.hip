@@ -1000,12 +1000,12 @@ bt_status operands(const Call &c, ExpertJob &a, const void *x, const void *w_gat
 }
 
 // The gradient of x, and those of the weights, of one product (du NULL) or of both projections, whose factors are dg and du: rows of `pitch_g`.
+// `copies`: what else is to be copied before.
 template <class T>
-bt_status backward(const Call &c, const T *dg, const T *du, const uint64_t pitch_g, const void *x, const void *w_gate, const void *w_up, const uint64_t d, const uint64_t f,
+bt_status backward(const Call &c, Copies<T> &copies, const T *dg, const T *du, const uint64_t pitch_g, const void *x, const void *w_gate, const void *w_up, const uint64_t d, const uint64_t f,
                    void *grad_x, void *grad_w_gate, void *grad_w_up, char *ws) {
     const bool filled_too = pads(c.plan, d, sizeof(T));
     const uint64_t pitch = filled_too ? filled(d, sizeof(T)) : d, pitch_x = c.ordered ? pitch : filled(d, sizeof(T));
-    Copies<T> copies;
     if (!c.ordered || filled_too) x = copies.add(&ws, x, c.rows(), d, pitch_x, c.ordered ? nullptr : c.plan.d_source, grad_w_gate != nullptr);
     if (filled_too) {
         w_gate = copies.add(&ws, w_gate, c.plan.experts * f, d, pitch, nullptr, grad_x != nullptr);
@@ -1139,7 +1139,8 @@ bt_status bt_expert_gated_backward(const void *d_grad_h, const void *d_x, const 
         const bt_status s = launch(gated_slopes_kernel<T>, dim3((unsigned)(blocks < 1u << 20 ? blocks : 1u << 20)), 256, c.hs, (const T *)d_grad_h, (const T *)d_gate,
                                    (const T *)d_up, dg, du, (uint32_t)f, (uint32_t)pitch, vectors, (int)activation);
         if (s != BT_OK) return s;
-        return backward<T>(c, dg, du, pitch, d_x, d_w_gate, d_w_up, d, f, d_grad_x, d_grad_w_gate, d_grad_w_up, ws);
+        Copies<T> copies;
+        return backward<T>(c, copies, dg, du, pitch, d_x, d_w_gate, d_w_up, d, f, d_grad_x, d_grad_w_gate, d_grad_w_up, ws);
     });
 }
 
@@ -1199,14 +1200,12 @@ bt_status bt_expert_linear_backward(const void *d_grad_y, const void *d_x, const
         char *ws = (char *)d_workspace;
         const T *grad_y = (const T *)d_grad_y;
         uint64_t pitch = d_out;
+        Copies<T> copies;
         if (pads(*plan, d_out, sizeof(T))) {
             pitch = filled(d_out, sizeof(T));
-            Copies<T> copy;
-            grad_y = copy.add(&ws, d_grad_y, rows, d_out, pitch);
-            const bt_status s = copy.run(c);
-            if (s != BT_OK) return s;
+            grad_y = copies.add(&ws, d_grad_y, rows, d_out, pitch);
         }
-        return backward<T>(c, grad_y, nullptr, pitch, d_x, d_w, nullptr, d_in, d_out, d_grad_x, d_grad_w, nullptr, ws);
+        return backward<T>(c, copies, grad_y, nullptr, pitch, d_x, d_w, nullptr, d_in, d_out, d_grad_x, d_grad_w, nullptr, ws);
     });
 }
 
