@@ -618,7 +618,7 @@ template <class T> __global__ __launch_bounds__(256) void gated_slopes_kernel(co
 // ---- host ------------------------------------------------------------------------------------------------------
 
 // Elements of a row that is padded to whole tiles of the summed index.
-uint64_t padded(const uint64_t cols, const int width) { return (cols * width + kKBytes - 1) / kKBytes * kKBytes / width; }
+inline uint64_t padded(const uint64_t cols, const int width) { return (cols * width + kKBytes - 1) / kKBytes * kKBytes / width; }
 
 bt_status check_sizes(const uint64_t rows, const uint64_t d, const uint64_t f, const bt_dtype dtype) {
     if (width_of(dtype) == 0) return BT_ERR_DTYPE;

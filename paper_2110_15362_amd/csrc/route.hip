@@ -222,7 +222,7 @@ __device__ inline uint32_t add_up(const RouteJob &a, const uint32_t *all, uint32
     return sum;
 }
 
-// A workgroup's 64 tokens at once, or most of them.
+// A workgroup's tokens at once, or most of them.
 constexpr int kChooseThreads = 1024;
 
 template <class T, int L, int R> __global__ __launch_bounds__(kChooseThreads) void choose_kernel(const RouteJob a) {
@@ -513,19 +513,27 @@ template <class T, int G, int K> __global__ __launch_bounds__(256) void combine_
 
 // ---- host ------------------------------------------------------------------------------------------------------
 
-constexpr uint64_t kOneChoices = 2048;      // up to which one workgroup does it all
+// Lanes that a token's logits take.
+constexpr uint32_t lanes_of(const uint64_t experts) { return experts <= 64 ? 8 : experts <= 128 ? 16 : experts <= 256 ? 32 : 64; }
 
 struct Groups {
     uint32_t a_group, groups;
 };
 
-// At least 64 tokens a workgroup, and no more than 256 workgroups, each of which reads all counts.
-Groups groups_of(const uint64_t tokens) {
-    const uint64_t a_group = tokens <= 64 * 256 ? 64 : (tokens + 255) / 256;
+// The tokens that a workgroup takes at once, up to 64, and no more than 256 workgroups, each of which reads all counts (us, bt_route_forward, bfloat16, 8 of 1024 experts: 1024 tokens with
+// 64 tokens a workgroup 57, with 16 26; 16384 tokens with at most 64, 128 and 256 workgroups 178, 102 and 71).
+Groups groups_of(const uint64_t tokens, const uint64_t experts) {
+    const uint64_t at_once = kChooseThreads / lanes_of(experts), least = at_once < 64 ? at_once : 64;
+    const uint64_t a_group = tokens <= least * 256 ? least : (tokens + 255) / 256;
     return {(uint32_t)a_group, (uint32_t)((tokens + a_group - 1) / a_group)};
 }
 
-bool one(const bt_expert_plan &p) { return p.tokens * p.chosen <= kOneChoices; }
+// One workgroup does it all: the order where it has few choices to place, the choice as well where it takes its tokens in at most two turns (us, bt_route_forward, one workgroup and two
+// launches: 8 of 64 experts, 64 tokens 7.2 and 11.3; 1 of 128, 64 tokens 6.0 and 7.6, 2048 tokens 70 and 8.9; 1 of 1024, 2048 tokens 466 and 24.
+// bt_route_order, 128 experts: 1024 choices 5.7 and 7.5, 2048 8.6 and 7.5).
+constexpr uint64_t kOneChoices = 1024;
+bool one_orders(const bt_expert_plan &p) { return p.tokens * p.chosen <= kOneChoices; }
+bool one_chooses(const bt_expert_plan &p) { return one_orders(p) && p.tokens * lanes_of(p.experts) <= 2 * kOneThreads; }
 
 RouteJob job_of(const bt_expert_plan &p, void *workspace) {
     RouteJob a = {};
@@ -537,7 +545,7 @@ RouteJob job_of(const bt_expert_plan &p, void *workspace) {
     a.tokens = (uint32_t)p.tokens;
     a.experts = (uint32_t)p.experts;
     a.chosen = (uint32_t)p.chosen;
-    const Groups g = groups_of(p.tokens);
+    const Groups g = groups_of(p.tokens, p.experts);
     a.a_group = g.a_group;
     a.groups = g.groups;
     return a;
@@ -546,9 +554,9 @@ RouteJob job_of(const bt_expert_plan &p, void *workspace) {
 // Lanes a token and logits a lane: whole vectors of either width.
 template <class Go> bt_status with_lanes(const uint32_t experts, Go go) {
     using std::integral_constant;
-    if (experts <= 64) return go(integral_constant<int, 8>{}, integral_constant<int, 8>{});
-    if (experts <= 128) return go(integral_constant<int, 16>{}, integral_constant<int, 8>{});
-    if (experts <= 256) return go(integral_constant<int, 32>{}, integral_constant<int, 8>{});
+    if (lanes_of(experts) == 8) return go(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+    if (lanes_of(experts) == 16) return go(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+    if (lanes_of(experts) == 32) return go(integral_constant<int, 32>{}, integral_constant<int, 8>{});
     if (experts <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 8>{});
     return go(integral_constant<int, 64>{}, integral_constant<int, 16>{});
 }
@@ -604,8 +612,8 @@ extern "C" {
 
 size_t bt_route_workspace_bytes(uint64_t tokens, uint64_t experts, uint64_t chosen) {
     const bt_expert_plan p = {tokens, experts, chosen, nullptr, nullptr, nullptr, nullptr};
-    if (check_plan(&p) != BT_OK || one(p)) return 0;
-    return ((size_t)groups_of(tokens).groups * experts * 4 + 127) / 128 * 128;
+    if (check_plan(&p) != BT_OK || one_chooses(p)) return 0;
+    return ((size_t)groups_of(tokens, experts).groups * experts * 4 + 127) / 128 * 128;
 }
 
 bt_status bt_route_forward(const void *d_logits, bt_dtype dtype, int normalise, const bt_expert_plan *plan, float *d_weights,
@@ -626,7 +634,7 @@ bt_status bt_route_forward(const void *d_logits, bt_dtype dtype, int normalise, 
         using T = decltype(type);
         return with_lanes(a.experts, [&](auto lanes, auto each) {
             constexpr int L = decltype(lanes)::value, R = decltype(each)::value;
-            if (one(*plan)) return launch(route_one_kernel<T, L, R>, dim3(1), kOneThreads, hs, a);
+            if (one_chooses(*plan)) return launch(route_one_kernel<T, L, R>, dim3(1), kOneThreads, hs, a);
             const bt_status s = launch(choose_kernel<T, L, R>, dim3(a.groups), kChooseThreads, hs, a);
             return s == BT_OK ? order(a, hs) : s;
         });
@@ -639,8 +647,11 @@ bt_status bt_route_order(const bt_expert_plan *plan, void *d_workspace, size_t w
     st = check_tables(*plan, d_workspace, workspace_bytes);
     if (st != BT_OK) return st;
     const hipStream_t hs = (hipStream_t)stream;
-    const RouteJob a = job_of(*plan, d_workspace);
-    if (one(*plan)) return launch(route_one_kernel<float, 8, 8>, dim3(1), kOneThreads, hs, a);
+    RouteJob a = job_of(*plan, d_workspace);
+    const Groups g = groups_of(plan->tokens, 1);      // (counting takes no lanes of a token: no more groups than the workspace has room for)
+    a.a_group = g.a_group;
+    a.groups = g.groups;
+    if (one_orders(*plan)) return launch(route_one_kernel<float, 8, 8>, dim3(1), kOneThreads, hs, a);
     st = launch(count_kernel, dim3(a.groups), 256, hs, a);
     return st == BT_OK ? order(a, hs) : st;
 }

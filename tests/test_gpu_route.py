@@ -89,6 +89,27 @@ def test_choice_and_order(experts, dtype, size):
         within(weights, *_weights(logits, index, normalise), "weights")
 
 
+@pytest.mark.parametrize("n,chosen,tokens", [(64, 8, (64, 128, 129)), (64, 7, (146, 147)), (65, 1, (64, 65)), (128, 16, (63, 64, 65)), (129, 1, (32, 33, 65)), (256, 32, (31, 32, 33)),
+                                              (257, 2, (15, 16, 17, 33)), (1024, 1, (16, 17, 1024, 1025, 4096, 4097)), (600, 32, (32, 33))], ids=str)
+def test_numbers_of_tokens_between_the_ways(experts, n, chosen, tokens):
+    """Tokens and choices around which one workgroup makes way for several, and more tokens a workgroup than it takes at once; the order alone has bounds of its own."""
+    for count in tokens:
+        logits = torch.randn(count, n, generator=torch.Generator().manual_seed(count))
+        index = _chosen(logits, chosen)
+        plan, weights = _route(experts, logits, chosen, True)
+        _check_tables(plan, index)
+        within(weights, *_weights(logits, index, True), "weights")
+        again = experts.new_plan(count, n, chosen)
+        again.index.copy_(index)
+        for t in (again.slots, again.source, again.offsets):
+            t.fill_(-7)
+        size = experts.lib().bt_route_workspace_bytes(count, n, chosen)
+        ws = torch.full((size + 128,), 0xFF, dtype=torch.uint8, device="cuda")
+        experts.bt_route_order(again, ws[:size] if size else None)
+        _check_tables(again, index)
+        assert bool((ws[size:] == 0xFF).all())
+
+
 @pytest.mark.parametrize("offset", [1, 3])
 @pytest.mark.parametrize("dtype", sorted(DTYPES))
 @pytest.mark.parametrize("n", [5, 8, 61, 128, 300])
