@@ -384,12 +384,13 @@ struct CombineJob {
 };
 
 // Tin: the rows' type.  G threads a token (a wave, or all 256), a vector of the output's type each, K rows on their way at once.  Bound by memory.
+// With few tokens the columns of one are those of several workgroups, blockIdx.y.
 template <class Tin, class T, int G, int K> __global__ __launch_bounds__(256) void combine_kernel(const CombineJob a) {
     constexpr int E = kPer<T>, H = E / kPer<Tin>;      // columns of a thread, vectors that they are
     const uint32_t t = threadIdx.x % G;
     for (uint64_t token = (uint64_t)blockIdx.x * (256 / G) + threadIdx.x / G; token < a.tokens; token += (uint64_t)gridDim.x * (256 / G)) {
         const int32_t *const slots = a.slots + token * a.chosen;
-        for (uint64_t col = (uint64_t)t * E; col < a.cols; col += G * E) {
+        for (uint64_t col = ((uint64_t)blockIdx.y * G + t) * E; col < a.cols; col += (uint64_t)gridDim.y * G * E) {
             const int left = a.cols - col < E ? (int)(a.cols - col) : E, before = col == 0 ? 0 : E;
             float sum[E] = {};
             for (uint32_t j0 = 0; j0 < a.chosen; j0 += K) {
@@ -432,13 +433,14 @@ struct CombineBackJob {
     uint32_t chosen;
 };
 
-// G threads a token (a wave, or all 256), K of its rows at a time.  The workgroups behind those of the tokens write zeros to the rows of no expert.
+// G threads a token (a wave, or all 256), K of its rows at a time, or with few tokens in each of several workgroups, blockIdx.y.  The workgroups behind those of the tokens write zeros to the rows of no
+// expert.
 template <class T, int G, int K> __global__ __launch_bounds__(256) void combine_back_kernel(const CombineBackJob a, const uint32_t groups) {
     constexpr int E = kPer<T>;
     __shared__ float sums[256 / kWave][K];
     const uint32_t t = threadIdx.x % G;
     if (blockIdx.x >= groups) {
-        if (!a.grad_y) return;
+        if (!a.grad_y || blockIdx.y != 0) return;
         const int32_t last = *a.last;
         const uint64_t first = last < 0 ? 0 : (uint64_t)last;
         for (uint64_t row = first + (blockIdx.x - groups); row < a.rows; row += gridDim.x - groups)
@@ -449,7 +451,7 @@ template <class T, int G, int K> __global__ __launch_bounds__(256) void combine_
     for (uint64_t token0 = (uint64_t)blockIdx.x * (256 / G); token0 < a.tokens; token0 += (uint64_t)groups * (256 / G)) {
         const uint64_t token = token0 + threadIdx.x / G;
         const bool real = token < a.tokens;
-        for (uint32_t j0 = 0; j0 < a.chosen; j0 += K) {
+        for (uint32_t j0 = blockIdx.y * K; j0 < a.chosen; j0 += gridDim.y * K) {
             uint64_t slot[K];
             float w[K], sum[K];
 #pragma unroll
@@ -572,6 +574,13 @@ bt_status check_tables(const bt_expert_plan &p, const void *ws, const size_t byt
 
 bt_status order(const RouteJob &a, hipStream_t hs) { return launch(order_kernel, dim3(a.groups), kOrderWaves * kWave, hs, a); }
 
+// Into how many pieces a token's work goes, of those that it has, where `groups` workgroups take the tokens: while there are no more than the 1024 that keep the card busy (us, one token, bfloat16: forward, 2 rows of 16384
+// columns 7.2 -> 2.9, 32 rows 58 -> 9.7, float32 8 rows 31 -> 4.1; backward 32 rows of 4096 24 -> 5.0).
+unsigned pieces_of(const uint64_t groups, const uint64_t there) {
+    const uint64_t wanted = 1024 / groups;
+    return (unsigned)(wanted <= 1 ? 1 : wanted < there ? wanted : there);
+}
+
 template <class Tin, class T> bt_status combine(const bt_expert_plan &p, const void *y, const float *weights, const uint64_t cols, void *out, hipStream_t hs) {
     CombineJob a = {};
     a.y = y;
@@ -584,7 +593,8 @@ template <class Tin, class T> bt_status combine(const bt_expert_plan &p, const v
     a.chosen = (uint32_t)p.chosen;
     const auto go = [&](auto kernel, const int a_group) {
         const uint64_t blocks = (a.tokens + a_group - 1) / a_group;
-        return launch(kernel, dim3((unsigned)(blocks < 1u << 20 ? blocks : 1u << 20)), 256, hs, a);
+        const uint64_t a_piece = 256 / a_group * kPer<T>;
+        return launch(kernel, dim3((unsigned)(blocks < 1u << 20 ? blocks : 1u << 20), pieces_of(blocks, (cols + a_piece - 1) / a_piece)), 256, hs, a);
     };
     const bool wide = cols > 64 * kPer<T> * 2;
     if (a.chosen <= 2) return wide ? go(combine_kernel<Tin, T, 256, 2>, 1) : go(combine_kernel<Tin, T, 64, 2>, 4);
@@ -717,14 +727,14 @@ bt_status bt_combine_backward(const void *d_grad_out, const void *d_y, const bt_
     a.chosen = (uint32_t)plan->chosen;
     return with_type(dtype, [&](auto type) {
         using T = decltype(type);
-        const auto go = [&](auto kernel, const int a_group) {
+        const auto go = [&](auto kernel, const int a_group, const uint32_t at_once) {
             const uint64_t blocks = (a.tokens + a_group - 1) / a_group;
             const uint32_t groups = (uint32_t)(blocks < 1u << 20 ? blocks : 1u << 20), rest = groups < 256 ? groups : 256;
-            return launch(kernel, dim3(groups + (d_grad_y ? rest : 0)), 256, (hipStream_t)stream, a, groups);
+            return launch(kernel, dim3(groups + (d_grad_y ? rest : 0), pieces_of(groups, (a.chosen + at_once - 1) / at_once)), 256, (hipStream_t)stream, a, groups);
         };
         const bool wide = cols > 64 * kPer<T> * 2;
-        if (a.chosen <= 2) return wide ? go(combine_back_kernel<T, 256, 2>, 1) : go(combine_back_kernel<T, 64, 2>, 4);
-        return wide ? go(combine_back_kernel<T, 256, 4>, 1) : go(combine_back_kernel<T, 64, 4>, 4);
+        if (a.chosen <= 2) return wide ? go(combine_back_kernel<T, 256, 2>, 1, 2) : go(combine_back_kernel<T, 64, 2>, 4, 2);
+        return wide ? go(combine_back_kernel<T, 256, 4>, 1, 4) : go(combine_back_kernel<T, 64, 4>, 4, 4);
     });
 }
 

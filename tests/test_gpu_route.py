@@ -247,6 +247,14 @@ def test_combine(experts, dtype, size, how):
             assert torch.equal(one, again) and not bool((one == 5.0).all(dim=1).any())
 
 
+@pytest.mark.parametrize("how", ["some", "holes", "none"])
+@pytest.mark.parametrize("size", [(1, 40, 32, 16383), (1, 1, 1, 9000), (2, 8, 8, 8192), (7, 6, 5, 4097), (130, 12, 12, 1030), (513, 9, 9, 264), (1025, 4, 3, 1025)], ids=str)
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+def test_few_tokens_in_pieces(experts, dtype, size, how):
+    """A token's columns, and backward its choices, in several workgroups; pieces that the last column or choice ends in."""
+    test_combine(experts, dtype, size, how)
+
+
 @pytest.mark.parametrize("dtype", sorted(DTYPES))
 def test_combine_of_nothing(experts, dtype):
     t = DTYPES[dtype]
