@@ -231,6 +231,12 @@ def route(logits, chosen, normalise=True):
     return weights, plan
 
 
+def _numbers(index, experts):
+    """The experts of `index` in 32 bits, -1 where there is none."""
+    index = index.long()      # (a type of few bits holds neither -1 nor the number of experts for sure)
+    return torch.where((index >= 0) & (index < experts), index, -1).int()
+
+
 def plan_of(index, experts):
     """The plan for experts that were chosen otherwise: index [tokens, chosen], integers; a number that is no expert's stands for none."""
     if index.dim() != 2 or index.dtype.is_floating_point or index.dtype.is_complex or index.dtype == torch.bool:
@@ -241,7 +247,7 @@ def plan_of(index, experts):
     def make():
         tokens, chosen = index.shape
         plan = new_plan(tokens, experts, chosen, index.device)
-        plan.index.copy_(torch.where((index >= 0) & (index < experts), index, -1))
+        plan.index.copy_(_numbers(index, experts))
         bt_route_order(plan, new_route_workspace(tokens, experts, chosen, index.device))
         return plan
     return _on(index, make)

@@ -249,3 +249,14 @@ def test_tables_of_the_definition():
     assert offsets.tolist() == [0, 2, 3, 6, 6]
     assert slots.tolist() == [[3, 0], [-1, 4], [2, 5], [1, -1]]
     assert source.tolist() == [0, 3, 2, 0, 1, 2, -1, -1]
+
+
+@pytest.mark.parametrize("dtype,n", [(torch.uint8, 7), (torch.uint8, 256), (torch.uint8, 300), (torch.int8, 100), (torch.int8, 128), (torch.int8, 200), (torch.int16, 1000), (torch.uint16, 7),
+                                     (torch.int32, 7), (torch.int64, 300)], ids=str)
+def test_given_choices_of_any_integer_type(experts, dtype, n):
+    """Numbers that are no expert's are -1, whatever the type that they come in can hold."""
+    info = torch.iinfo(dtype)
+    numbers = sorted({v for v in (0, 1, 5, 6, 7, n - 1, n, 127, 128, 255, -1, -7, info.min, info.max) if info.min <= v <= info.max})
+    got = experts._numbers(torch.tensor([numbers, numbers[::-1]], dtype=torch.int64).to(dtype), n)
+    want = [v if 0 <= v < n else -1 for v in numbers]
+    assert got.dtype == torch.int32 and got.tolist() == [want, want[::-1]]

@@ -265,3 +265,14 @@ def test_combine_of_nothing(experts, dtype):
         experts.bt_combine_forward(y, plan, None, out)
         experts.bt_combine_backward(out, y, plan, None, torch.empty_like(y), grad_w)
         assert not bool(grad_w.any())
+
+
+@pytest.mark.parametrize("dtype,n", [(torch.uint8, 256), (torch.uint8, 300), (torch.uint8, 50), (torch.int8, 128), (torch.int8, 200), (torch.int16, 1024), (torch.uint16, 40)], ids=str)
+def test_given_choices_in_few_bits(experts, dtype, n):
+    """Integers that hold neither the number of experts nor -1; some numbers that are no expert's."""
+    info = torch.iinfo(dtype)
+    index = torch.stack([torch.randperm(min(n, info.max + 1), generator=torch.Generator().manual_seed(i))[:3] for i in range(90)])
+    index[::7, 1] = info.max if info.max >= n else info.min
+    want = torch.where((index >= 0) & (index < n), index, -1).int()
+    plan = experts.plan_of(index.to(dtype).cuda(), n)
+    _check_tables(plan, want)
