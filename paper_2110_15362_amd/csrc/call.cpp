@@ -951,19 +951,34 @@ static PyObject *py_route_backward(PyObject *self, PyObject *const *args, Py_ssi
 /* Of a weight [experts, f, d] f and d; the experts have to be the plan's. */
 static int expert_weight(const tensor *w, const char *name, const uint64_t n, uint64_t *f, uint64_t *d) {
     uint64_t size[3];
-    PyObject *const shape = PyObject_GetAttrString(w->t, "shape"), *const items = shape != NULL ? PySequence_Tuple(shape) : NULL;
-    Py_XDECREF(shape);
-    if (items == NULL) return -1;
-    bool fits = PyTuple_GET_SIZE(items) == 3;
-    for (int i = 0; i < 3 && fits; ++i) {
-        size[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(items, i));
-        fits = size[i] != (uint64_t)-1;
+    bool fits;
+    if (THPVariable_Check(w->t)) {
+        const at::Tensor &t = THPVariable_Unpack(w->t);
+        fits = t.dim() == 3;
+        for (int i = 0; i < 3 && fits; ++i) size[i] = (uint64_t)t.size(i);
+    } else {
+        PyObject *const shape = PyObject_GetAttrString(w->t, "shape"), *const items = shape != NULL ? PySequence_Tuple(shape) : NULL;
+        Py_XDECREF(shape);
+        if (items == NULL) return -1;
+        fits = PyTuple_GET_SIZE(items) == 3;
+        for (int i = 0; i < 3 && fits; ++i) {
+            size[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(items, i));
+            fits = size[i] != (uint64_t)-1;
+        }
+        Py_DECREF(items);
+        if (PyErr_Occurred()) return -1;
     }
-    Py_DECREF(items);
-    if (PyErr_Occurred()) return -1;
     if (!fits || size[0] != n) return refuse(name, "must be a matrix for each of the plan's experts");
     *f = size[1];
     *d = size[2];
+    return 0;
+}
+
+/* Both weights are [experts, f, d]. */
+static int expert_weights(const tensor *gate, const tensor *up, const uint64_t n, uint64_t *f, uint64_t *d) {
+    uint64_t f2, d2;
+    if (expert_weight(gate, "w_gate", n, f, d) != 0 || expert_weight(up, "w_up", n, &f2, &d2) != 0) return -1;
+    if (f2 != *f || d2 != *d) return refuse("w_up", "must have the shape of w_gate");
     return 0;
 }
 
@@ -987,7 +1002,7 @@ static PyObject *py_expert_gated_forward(PyObject *self, PyObject *const *args, 
     uint64_t rows, f, d;
     int ordered;
     if (expect_experts(nargs, 14) != 0 || needed(args, names, 8) != 0 || take_some(a, args, names, 11) != 0 || plan_of(a + 4, &plan, &rows) != 0 ||
-        flag(args[12], &ordered) != 0 || expert_weight(&a[1], "w_gate", plan.experts, &f, &d) != 0 || check_x(&a[0], "x", d, &plan, ordered) != 0)
+        flag(args[12], &ordered) != 0 || expert_weights(&a[1], &a[2], plan.experts, &f, &d) != 0 || check_x(&a[0], "x", d, &plan, ordered) != 0)
         return NULL;
     const uint64_t weight = plan.experts * f * d, first[] = {a[0].numel, weight, weight, rows * f}, kept[] = {rows * f, rows * f};
     if (check_all(a, names, 4, &a[0], first) != 0 || check_all(a + 8, names + 8, 2, &a[0], kept) != 0 || code_of(&a[0], &code) != 0) return NULL;
@@ -1010,7 +1025,7 @@ static PyObject *py_expert_gated_backward(PyObject *self, PyObject *const *args,
     uint64_t rows, f, d;
     int ordered;
     if (expect_experts(nargs, 17) != 0 || needed(args, names, 10) != 0 || take_some(a, args, names, 14) != 0 || plan_of(a + 6, &plan, &rows) != 0 ||
-        flag(args[15], &ordered) != 0 || expert_weight(&a[2], "w_gate", plan.experts, &f, &d) != 0 || check_x(&a[1], "x", d, &plan, ordered) != 0)
+        flag(args[15], &ordered) != 0 || expert_weights(&a[2], &a[3], plan.experts, &f, &d) != 0 || check_x(&a[1], "x", d, &plan, ordered) != 0)
         return NULL;
     const uint64_t weight = plan.experts * f * d, x = a[1].numel;
     const uint64_t before[] = {rows * f, x, weight, weight, rows * f, rows * f}, behind[] = {x, weight, weight};

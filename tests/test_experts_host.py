@@ -260,3 +260,14 @@ def test_given_choices_of_any_integer_type(experts, dtype, n):
     got = experts._numbers(torch.tensor([numbers, numbers[::-1]], dtype=torch.int64).to(dtype), n)
     want = [v if 0 <= v < n else -1 for v in numbers]
     assert got.dtype == torch.int32 and got.tolist() == [want, want[::-1]]
+
+
+def test_both_weights_have_one_shape(experts):
+    """As many elements in another order are not the same weight."""
+    x, wg, wu = _Fake(6, 16), _Fake(4, 24, 16), _Fake(4, 16, 24)
+    kept = _Fake(12, 24)
+    for up in (wu, _Fake(24, 4, 16), _Fake(96, 16), _Fake(4, 384)):
+        with pytest.raises(ValueError, match="w_up"):
+            experts.bt_expert_gated_forward(x, _Tables(), wg, up, "silu", kept, None, None, None, False, 0)
+        with pytest.raises(ValueError, match="w_up"):
+            experts.bt_expert_gated_backward(kept, x, _Tables(), wg, up, kept, kept, "silu", x, wg, wg, None, False, 0)
