@@ -361,4 +361,6 @@ def combine(y, plan, weights=None):
     _check_plan(plan, y, weights)
     if y.dim() != 2:
         raise ValueError("y must be a matrix with a row for each of the plan's")
+    if weights is not None and weights.dim() > 1 and weights.shape[-1] != plan.chosen:
+        raise ValueError("weights must be [tokens, chosen]")
     return _on(y, _Combine.apply, y, weights, plan, _keep(y, weights))

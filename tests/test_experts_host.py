@@ -271,3 +271,13 @@ def test_both_weights_have_one_shape(experts):
             experts.bt_expert_gated_forward(x, _Tables(), wg, up, "silu", kept, None, None, None, False, 0)
         with pytest.raises(ValueError, match="w_up"):
             experts.bt_expert_gated_backward(kept, x, _Tables(), wg, up, kept, kept, "silu", x, wg, wg, None, False, 0)
+
+
+def test_combine_refuses_weights_of_another_shape(experts, monkeypatch):
+    """[chosen, tokens] has as many elements as [tokens, chosen]."""
+    index = choices(6, 4, 2, 1)
+    p = experts.Plan(index, *tables(index, 4))
+    monkeypatch.setattr(experts, "_check_plan", lambda *a: None)      # (the tensors are on the host)
+    for shape in ((2, 6), (1, 12), (6, 2, 1), (4, 3)):
+        with pytest.raises(ValueError, match="weights"):
+            experts.combine(torch.zeros(12, 8), p, torch.zeros(shape))
