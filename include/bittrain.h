@@ -553,7 +553,7 @@ bt_status bt_route_order(const bt_expert_plan *plan, void *d_workspace, size_t w
 
 /* The gradient of the logits from that of the weights.  With normalise w_j (g_j - sum_i w_i g_i) at a token's experts and 0 elsewhere; without it
  * p_e (g_e - sum_i w_i g_i) for every expert e, p the softmax, g_e 0 where e is not chosen.
- *   d_grad_weights   [tokens, chosen]; not looked at where index is -1
+ *   d_grad_weights   [tokens, chosen]; not looked at where index is no expert's
  *   d_logits         as in the forward pass (not read with normalise, and may be NULL then)
  *   plan             d_index is read
  *   d_weights        as bt_route_forward left them

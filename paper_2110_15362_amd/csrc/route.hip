@@ -348,12 +348,12 @@ template <class T, int L, int R> __global__ __launch_bounds__(256) void route_ba
         }
         float mean = 0.0f;
         for (uint32_t j = 0; j < a.chosen; ++j)
-            if (a.index[at + j] >= 0) mean += a.weights[at + j] * b.grad_weights[at + j];
+            if ((uint32_t)a.index[at + j] < a.experts) mean += a.weights[at + j] * b.grad_weights[at + j];
 #pragma unroll
         for (int r = 0; r < R; ++r) grad[r] = a.normalise || p[r] == 0.0f ? 0.0f : -p[r] * mean;
         for (uint32_t j = 0; j < a.chosen; ++j) {
-            const uint32_t e = (uint32_t)a.index[at + j] - lane * R;      // (of no expert: beyond R, for the lanes have fewer than 2^31 experts)
-            if (e >= (uint32_t)R) continue;
+            const uint32_t expert = (uint32_t)a.index[at + j], e = expert - lane * R;
+            if (expert >= a.experts || e >= (uint32_t)R) continue;
             const float w = a.weights[at + j], g = b.grad_weights[at + j];
 #pragma unroll
             for (int r = 0; r < R; ++r)

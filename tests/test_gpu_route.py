@@ -276,3 +276,25 @@ def test_given_choices_in_few_bits(experts, dtype, n):
     want = torch.where((index >= 0) & (index < n), index, -1).int()
     plan = experts.plan_of(index.to(dtype).cuda(), n)
     _check_tables(plan, want)
+
+
+@pytest.mark.parametrize("normalise", [True, False])
+@pytest.mark.parametrize("n", [5, 70, 1000])
+def test_gradient_where_index_is_no_expert(experts, n, normalise):
+    """A number beyond the experts counts as none, as -1 does: neither its weight nor the gradient of it is looked at."""
+    g = torch.Generator().manual_seed(n)
+    logits = torch.randn(40, n, generator=g)
+    logits[::3, 2:] = -INF                                   # two experts, for three choices
+    logits[1::3] = -INF
+    plan, weights = _route(experts, logits, 3, normalise)
+    none = plan.index < 0
+    grad_weights = torch.randn(40, 3, generator=g).cuda()
+    grad_weights[none] = NAN
+    want = torch.empty(40, n, device="cuda")
+    experts.bt_route_backward(grad_weights, logits.cuda(), plan, weights, want, normalise)
+    assert bool(torch.isfinite(want).all())
+    for number in (n, n + 1, 1 << 30, -9):
+        plan.index[none] = number
+        got = torch.empty_like(want)
+        experts.bt_route_backward(grad_weights, logits.cuda(), plan, weights, got, normalise)
+        assert torch.equal(got, want), number
