@@ -230,7 +230,8 @@ template <class T, Kind K> __device__ inline Operand operand_q(const ExpertJob &
 template <Kind K> __device__ inline uint32_t summed(const ExpertJob &a, const Group &g) { return K == kWeights ? g.rows : __builtin_amdgcn_readfirstlane(g.expert < a.experts ? a.k : 0); }
 __device__ inline Taken taken(const ExpertJob &a, const Group &g) { return {a.source ? a.source + g.first : nullptr, a.tokens}; }
 
-// Stores that a lane makes of each output in the function below, of a tile that lies inside it: at the least.
+// Stores that a lane makes of each output in the function below, of a tile that lies inside it: at the least, which is what a wait that counts them may rely on (one that counts on more than there
+// are lets a tile be read that has not landed).
 template <class T, Kind K, int FP, int FQ> constexpr int kStoresAtLeast = K == kPair ? FQ : sizeof(T) == 2 ? FQ * (FP / kTogether) : FQ * FP;
 
 // What becomes of a wave's sums: rows from m on, FQ fragments of 16; columns from n on, FP fragments, of a pair half of them columns of the gate's product and half the
@@ -246,6 +247,7 @@ template <class T, Kind K, int FP, int FQ> __device__ inline void finish(const E
         if constexpr (K != kPair && sizeof(T) == 2) {
             // Where rows begin on 64-byte boundaries four lanes write 64 bytes in a row.  All lanes take part, those beyond the last row too.
             if (!a.sums && a.pitch % 32 == 0) {
+                static_assert(kStoresAtLeast<T, K, FP, FQ> <= FQ * (FP / kTogether));
 #pragma unroll
                 for (int i = 0; i < FP; i += kTogether) {
                     uint32_t low[2] = {pack2<T>(acc[i][j][0], acc[i][j][1]), pack2<T>(acc[i][j][2], acc[i][j][3])};
@@ -260,6 +262,7 @@ template <class T, Kind K, int FP, int FQ> __device__ inline void finish(const E
         if (row >= rows) continue;
         if constexpr (K == kPair) {
             constexpr int N = 2 * FP;      // neighbours that the lane has
+            static_assert(kStoresAtLeast<T, K, FP, FQ> <= FQ * ((N + kPer<T> - 1) / kPer<T>));
             const uint32_t col = n + lane / 16 * N;
             const int left = (int)(a.n - col);
             const uint64_t at = row * a.pitch + col;
@@ -278,6 +281,7 @@ template <class T, Kind K, int FP, int FQ> __device__ inline void finish(const E
                 store_run<T, N>((T *)a.up + first + at, left, u);
             }
         } else {
+            static_assert(kStoresAtLeast<T, K, FP, FQ> <= FQ * FP);
 #pragma unroll
             for (int i = 0; i < FP; ++i) {
                 const uint32_t col = n + i * 16 + lane / 16 * 4;
