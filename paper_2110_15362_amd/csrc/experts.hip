@@ -22,7 +22,7 @@ struct ExpertJob {
     void *out[2], *gate, *up;
     float *sums;                       // kBack: [rows, n] in single precision instead of out
     uint64_t pitch;                    // of the outputs
-    const int32_t *offsets, *source;   // source: x has a row a token; else NULL
+    const int32_t *offsets, *source;   // source: forward, x has a row a token; else NULL (the weights' gradients have a copy of x in the rows' order)
     uint32_t experts, rows, tokens;
     uint32_t m, n, k;                  // kWeights: m by n of each expert, k is not used; else n columns and k summed indices
     uint32_t tiles_m, tiles_n, outputs;  // kWeights: tiles of an output, outputs; else tiles_n alone
@@ -216,7 +216,7 @@ template <Kind K, class Map> __device__ inline Place place_of(const ExpertJob &a
 
 // The operands of a tile's product, of sum `sum`; rows and summed indices that it has.
 template <class T, Kind K> __device__ inline Operand operand_p(const ExpertJob &a, const Group &g, const int sum) {
-    if constexpr (K == kWeights) return {(const T *)a.p[0] + (a.source ? 0 : g.first * a.pitch_p), a.pitch_p, g.rows, a.n};
+    if constexpr (K == kWeights) return {(const T *)a.p[0] + g.first * a.pitch_p, a.pitch_p, g.rows, a.n};
     else {
         const T *const w = (const T *)a.p[sum] + (g.expert < a.experts ? g.expert : 0) * a.step;
         if constexpr (K <= kPlain) return {w, a.pitch_p, a.n, a.k};
@@ -329,7 +329,7 @@ template <class T, Kind K> __global__ __launch_bounds__(Small::THREADS, 2) void 
     if (K == kWeights || p[0].cols < kPer<T> || q[0].cols < kPer<T>) {
         for (; t < last; ++t) {
             const uint32_t s = sum_of(t);
-            if constexpr (K == kWeights) w.staged(p[0], p[0], q[0], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, tiles[0] + W::P::BYTES, acc, rows);
+            if constexpr (K == kWeights) w.staged(p[0], p[0], q[0], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, tiles[0] + W::P::BYTES, acc);
             else if constexpr (K <= kPlain) w.staged(p[s], p[1], q[s], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, tiles[0] + W::P::BYTES, acc, InOrder{}, rows);
             else w.staged(p[s], p[1], q[s], at.n, at.m, start_of(t), tiles[0], tiles[0] + W::P::BYTES, tiles[0] + W::P::BYTES, acc);
         }
@@ -574,13 +574,10 @@ template <class T, Kind K, class S> __global__ __launch_bounds__(S::THREADS, S::
         const bool in_parts = at.slot != ~0u;
         const bool through = (K <= kPlain || K == kBack) && rest < k && (!in_parts || at.slot % r.splits + 1 == r.splits);
         if (through) {
-#pragma unroll 1
-            for (int sum = 0; sum < F::SUMS; ++sum) {
-                const Operand p = operand_p<T, K>(a, at.of, sum), q = operand_q<T, K>(a, at.of, K == kWeights ? at.part : sum);
-                if constexpr (K <= kPlain)
-                    w.staged(p, operand_p<T, K>(a, at.of, 1), q, at.n, at.m, rest, tiles, tiles + PLACES * PB, tiles, acc, InOrder{}, taken(a, at.of));
-                else w.staged(p, p, q, at.n, at.m, rest, tiles, tiles + PLACES * PB, tiles, acc);
-            }
+            const Operand p = operand_p<T, K>(a, at.of, 0), q = operand_q<T, K>(a, at.of, 0);
+            if constexpr (K <= kPlain)
+                w.staged(p, operand_p<T, K>(a, at.of, 1), q, at.n, at.m, rest, tiles, tiles + PLACES * PB, tiles, acc, InOrder{}, taken(a, at.of));
+            else if constexpr (K == kBack) w.staged(p, p, q, at.n, at.m, rest, tiles, tiles + PLACES * PB, tiles, acc);
         }
         const Place here = at;
         if (more) {
@@ -849,7 +846,8 @@ template <class T, Kind K> bt_status run_product(ExpertJob &a, hipStream_t hs) {
     bool straight = direct<T>(a.p[0], a.pitch_p) && direct<T>(a.q[0], a.pitch_q);
     if (K == kPair || K == kBackPair) straight = straight && direct<T>(a.p[1], a.pitch_p);
     if (K == kBackPair || (K == kWeights && a.outputs == 2)) straight = straight && direct<T>(a.q[1], a.pitch_q);
-    if (a.source) straight = straight && K <= kPlain && a.tokens * a.pitch_q * sizeof(T) < 1u << 31;
+    if constexpr (K <= kPlain)
+        if (a.source) straight = straight && a.tokens * a.pitch_q * sizeof(T) < 1u << 31;
     if (!straight) return go(experts_any_kernel<T, K>, Small::NQ, K == kPair ? Small::NP / 2 : Small::NP, Small::THREADS);
     const Size size = size_of(K, a.rows, a.experts, a.m, a.n, a.k, a.outputs, sizeof(T));
     if constexpr (sizeof(T) == 2) {

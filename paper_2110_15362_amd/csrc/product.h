@@ -169,7 +169,7 @@ template <class T, Order O, int N, int F, int kThreads, int KB = kKBytes> struct
                 if (r < from.rows) v[i] = load_vec((const T *)from.p + rows(r) * from.pitch + k + col, (int)(from.cols - k) - col, (int)k + col);
             } else {
                 v[i] = raw16{0, 0, 0, 0};
-                if (k + row < a.rows) v[i] = load_vec((const T *)a.p + rows(k + row) * a.pitch + n + col, (int)(a.cols - n) - col, (int)n + col);
+                if (k + row < a.rows) v[i] = load_vec((const T *)a.p + (k + row) * a.pitch + n + col, (int)(a.cols - n) - col, (int)n + col);
             }
         }
     }
