@@ -132,3 +132,40 @@ def test_few_rows_take_the_weights_straight(experts, dtype, size, kinds, ordered
                 _check_gated_forward(c, "silu", *kept)
                 assert torch.equal(_gated_forward(experts, c, "silu", keep=False, offset=offset)[0], kept[0])
             _check_linear_forward(c, _linear_forward(experts, c, offset))
+
+
+@pytest.mark.parametrize("way", ["tiles", "any"])
+def test_more_tiles_than_a_launch_takes(experts, way):  # noqa: F811
+    """Products whose tiles of 64 by 64 (of both projections 64 by 32) are more than 2^22 go in several launches: fetched straight to LDS, and at any alignment; every element looked at."""
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("needs 100 GiB")
+    tokens, n, d = (1 << 20) + 77, 3, 8
+    t, f = (torch.float32, 8200) if way == "tiles" else (torch.bfloat16, 16400)
+    g = torch.Generator(device="cuda").manual_seed(70)
+    x = torch.randn(tokens * d + 1, generator=g, device="cuda").to(t)[1 if way == "any" else 0:][:tokens * d].view(tokens, d)      # (off a 16-byte boundary, or on it)
+    wg, wu = ((torch.randn(n, f, d, generator=g, device="cuda") / d ** 0.5).to(t) for _ in range(2))
+    plan = experts.plan_of((torch.arange(tokens, device="cuda") * 7 % 10 % 4 - 1)[:, None], n)
+    cols = 32 if way == "tiles" else 64
+    o = plan.offsets.tolist()
+    assert sum(-(-(b - a) // 64) for a, b in zip(o, o[1:] + [tokens])) * -(-f // cols) > 1 << 22
+    out = torch.full((plan.rows, f), float("nan"), dtype=t, device="cuda")
+    if way == "tiles":
+        experts.bt_expert_gated_forward(x, plan, wg, wu, "relu", out, None, None, experts.new_gated_workspace(plan, d, f, t))
+    else:
+        experts.bt_expert_linear_forward(x, plan, wg, out, experts.new_linear_workspace(plan, d, f, t, ordered=False), ordered=False)
+    gamma = (d + 1) * SUM
+    for e in range(n):
+        for a in range(o[e], o[e + 1], 1 << 16):
+            b = min(a + (1 << 16), o[e + 1])
+            v = x[plan.source[a:b].long()].double()
+            want, off = v @ wg[e].double().t(), gamma * (v.abs() @ wg[e].double().abs().t())
+            if way == "tiles":
+                u, eu = v @ wu[e].double().t(), gamma * (v.abs() @ wu[e].double().abs().t())
+                want.clamp_(min=0)
+                off = off * (u.abs() + eu) + want * eu + SUM * (want * u).abs()
+                want = want * u
+            _near(out[a:b], want, off, t, "rows from %d on" % a)
+            del want, off
+    assert o[n] < tokens
+    for a in range(o[n], tokens, 1 << 16):
+        assert not bool(out[a:a + (1 << 16)].any())
