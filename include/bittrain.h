@@ -387,7 +387,7 @@ bt_status bt_workspace_status(const void *d_workspace, uint32_t *d_status, bt_st
  * answers with it: the gated projections whose output is the activation, the norms, gate and residual sum between two
  * sublayers, and the clipping of the step's gradients.  BT_F32, BT_F16 and BT_BF16.  All sums, statistics and
  * activations are computed in 32 bits or more and rounded once, to the tensors' type, where they are stored.  What a backward
- * pass takes from its forward pass is so rounded too (d_gate and d_up, d_out), and so are the factors that bt_gated_backward multiplies.
+ * pass takes from its forward pass is so rounded too (d_gate and d_up, d_out), and so are the factors that bt_gated_backward and bt_expert_gated_backward multiply.
  *
  * Tensors are row-major and contiguous, and are aligned to their elements; those that are aligned to 16 bytes and whose
  * rows are whole 16-byte vectors go faster.  A workspace is scratch memory of the call: 128-byte aligned, of the size that the
@@ -567,9 +567,10 @@ bt_status bt_route_backward(const float *d_grad_weights, const void *d_logits, b
 size_t bt_expert_gated_workspace_bytes(const bt_expert_plan *plan, uint64_t d, uint64_t f, bt_dtype dtype, int ordered, int backward);
 
 /* The gated projections, as bt_gated_forward makes them, with the weights of each row's expert.
- *   d_x               ordered == 0: [tokens, d], row r taking that of its token (d_source is read); else [rows, d], the rows' own
+ *   d_x               ordered == 0: [tokens, d], row r taking that of its token (d_source is read); else [rows, d], the rows' own.  (Of 2 GiB
+ *                     of tokens and more rows are gathered by a slower kernel; a copy of them in the plan's order, with `ordered`, is not slowed down)
  *   d_w_gate, d_w_up  [experts, f, d] each
- *   plan              d_offsets is read, and d_source
+ *   plan              d_offsets is read, and without `ordered` d_source
  *   d_h, d_gate, d_up [rows, f], rows = tokens * chosen; d_gate and d_up may be NULL both
  * Errors as for bt_gated_forward. */
 bt_status bt_expert_gated_forward(const void *d_x, const void *d_w_gate, const void *d_w_up, const bt_expert_plan *plan,

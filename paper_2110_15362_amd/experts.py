@@ -284,7 +284,7 @@ class _GatedLinear(torch.autograd.Function):
 
 def gated_linear(x, plan, w_gate, w_up, activation="relu", ordered=False):
     """act(x w_gate^T) * (x w_up^T) with the weights of each row's expert, with its gradient: [rows, f], rows of no expert zeros.  x [tokens, d], or with `ordered`
-    [rows, d] in the plan's order; weights [experts, f, d], all of one type."""
+    [rows, d] in the plan's order; weights [experts, f, d], all of one type.  In 16 bits what is kept for backward, and the factors of the gradients, are rounded to them."""
     _activation(activation)
     _check_plan(plan, x, w_gate, w_up)
     _check_weight(plan, x, w_gate, "w_gate")
