@@ -233,7 +233,8 @@ def route(logits, chosen, normalise=True):
 
 def _numbers(index, experts):
     """The experts of `index` in 32 bits, -1 where there is none."""
-    index = index.long()      # (a type of few bits holds neither -1 nor the number of experts for sure)
+    if index.dtype not in (torch.int32, torch.int64):      # (a type of few bits holds neither -1 nor the number of experts for sure)
+        index = index.long()
     return torch.where((index >= 0) & (index < experts), index, -1).int()
 
 
@@ -247,7 +248,7 @@ def plan_of(index, experts):
     def make():
         tokens, chosen = index.shape
         plan = new_plan(tokens, experts, chosen, index.device)
-        plan.index.copy_(_numbers(index, experts))
+        plan.index = _numbers(index, experts).contiguous()
         bt_route_order(plan, new_route_workspace(tokens, experts, chosen, index.device))
         return plan
     return _on(index, make)

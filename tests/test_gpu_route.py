@@ -298,3 +298,16 @@ def test_gradient_where_index_is_no_expert(experts, n, normalise):
         got = torch.empty_like(want)
         experts.bt_route_backward(grad_weights, logits.cuda(), plan, weights, got, normalise)
         assert torch.equal(got, want), number
+
+
+def test_given_choices_stay_as_they_are(experts):
+    """The plan's index is its own: strides of any kind, and what is written to it later does not reach the caller's tensor, nor the other way round."""
+    for dtype in (torch.int32, torch.int64, torch.uint8):
+        given = choices(60, 9, 3, 8).t().contiguous().to(dtype).cuda().t()
+        before = given.clone()
+        plan = experts.plan_of(given, 9)
+        _check_tables(plan, before.cpu().int())
+        plan.index.fill_(0)
+        assert torch.equal(given, before)
+        given.fill_(5)
+        assert not bool(plan.index.any())
